@@ -403,6 +403,166 @@ MICRO_API const char *micro_status_string(micro_status status);
  * stream first. */
 MICRO_API void micro_sparsify_free(micro_ctx *ctx);
 
+/* ------------------------------------------------------------------------
+ * Around the step on a language model: the global norm and clipping of a
+ * model's gradients into the flat vector that the step reads, the lookup of
+ * token rows with its gradient, and the softmax cross entropy over the token
+ * table with its gradients.
+ *
+ * Every call below is enqueued on its handle's stream and returns after the
+ * launches; device inputs must be ready on that stream and stay allocated
+ * until it has run.  Messages of a refusal come from micro_last_error(NULL) on
+ * the calling thread; a refusal (MICRO_EINVAL, MICRO_ECAPACITY, MICRO_ERANGE)
+ * comes before any device work, with nothing modified.  One handle must not be
+ * used from two threads at once.  Results are the same on every run.
+ * ------------------------------------------------------------------------ */
+
+/* Types of the tensors' values. */
+#define MICRO_TYPE_F32 0  /* IEEE binary32 */
+#define MICRO_TYPE_F16 1  /* IEEE binary16 */
+#define MICRO_TYPE_BF16 2 /* bfloat16      */
+
+/*
+ * A set of gradient tensors, in the order of the flat vector: tensor i holds
+ * sizes[i] contiguous values of types[i] at tensors[i] (device, aligned to its
+ * type; a tensor of no values may be NULL).  The set keeps the addresses: the
+ * tensors stay where they are until micro_grads_free.  No two may share
+ * memory.  `tensors`, `sizes` and `types` are host arrays of `count` entries,
+ * read during the call, which waits for its upload.  Device scratch: 16 KB and
+ * 32 bytes per 4,096 to 32,768 values.
+ */
+typedef struct micro_grads micro_grads; /* opaque, owned by the library */
+MICRO_API micro_status micro_grads_init(micro_grads **grads, int32_t count, void *const *tensors,
+                                        const int64_t *sizes, const int32_t *types, void *hip_stream);
+
+/*
+ * The global L2 norm: *sumsq = the sum of the squares of all values (device
+ * double), *norm = its square root (device float); either may be NULL.
+ * Squares and sums in binary64, in an order that only the sizes determine.
+ * Workers that hold parts of one model add their sumsq before clipping.
+ */
+MICRO_API micro_status micro_grads_norm(micro_grads *grads, double *sumsq, float *norm);
+
+/*
+ * Every value times c = min(1, max_norm / (norm + 1e-6)), in place: c in
+ * binary64, rounded to binary32 once; the product in binary32, rounded to the
+ * tensor's type once.  c == 1 writes nothing.  A norm of +inf makes c 0, a
+ * NaN makes it NaN (as the formula says).
+ *   max_norm  > 0; +inf does not clip.
+ *   sumsq     device double: the squared norm to clip by (of all workers);
+ *             NULL: this set's own, computed first.
+ *   norm      device float out: sqrt(sumsq); may be NULL.
+ */
+MICRO_API micro_status micro_grads_clip(micro_grads *grads, double max_norm, const double *sumsq, float *norm);
+
+/*
+ * The same values in binary32 into `flat` (device, as many floats as the set
+ * has values, sharing no memory with the set), tensor after tensor; the
+ * tensors stay as they are.  With max_norm = +inf and norm == NULL the values
+ * are only converted, in one pass.
+ */
+MICRO_API micro_status micro_grads_flatten(micro_grads *grads, double max_norm, const double *sumsq, float *flat,
+                                           float *norm);
+
+/* Releases the set's scratch after waiting for its stream; NULL is a no-op.
+ * The tensors are the caller's. */
+MICRO_API void micro_grads_free(micro_grads *grads);
+
+/*
+ * A token table: `vocab` rows of `dim` values of one type, with the lookup of
+ * rows, the loss over the table and the gradients of both.  Row arguments are
+ * device addresses with a row stride in values (>= dim; the values of a row
+ * are adjacent, the address aligned to the type); tokens' ids and targets are
+ * int32 or int64 (MICRO_IDS_*), one after the other, aligned to their size.
+ */
+#define MICRO_IDS_I32 0
+#define MICRO_IDS_I64 1
+
+typedef struct micro_table micro_table; /* opaque, owned by the library */
+
+typedef struct micro_table_config {
+    int64_t padding_id;  /* an id whose row gets no gradient from lookups; -1: none      (-1)   */
+    int64_t ignored;     /* the target of a token that does not count                    (-100) */
+    int64_t score_bytes; /* scratch for one token block's scores at most (at least one
+                            block of 256 tokens is held)                         (2^31) */
+} micro_table_config;
+
+/* Fills *cfg with the defaults listed above. */
+MICRO_API void micro_table_config_default(micro_table_config *cfg);
+
+/*
+ * A handle for a table of vocab x dim values of `type` and calls of up to
+ * max_tokens tokens, enqueuing on hip_stream; cfg NULL: the defaults.  Holds
+ * no scratch yet: the first call of each kind allocates what its kind needs
+ * (a lookup nothing; its gradient 16 bytes and dim/4 bytes a token; the loss a
+ * padded copy of the hidden rows, and of the table where it cannot be read in
+ * place: binary32, a dim that is no multiple of 64, or rows that are not
+ * aligned to 16 bytes; its gradients the block's scores and 64 MB).
+ * MICRO_ERANGE for vocab above 2^31 - 2, dim above 65536 or max_tokens above
+ * 2^22; MICRO_EINVAL for vocab < 1, dim < 1, max_tokens < 0 or an unknown
+ * type.
+ */
+MICRO_API micro_status micro_table_init(micro_table **table, int64_t vocab, int32_t dim, int64_t max_tokens,
+                                        int32_t type, void *hip_stream, const micro_table_config *cfg);
+
+/*
+ * out[t] = scale * weight[ids[t]] for t in [0, tokens): one binary32 product,
+ * rounded to the type once.  An id outside [0, vocab) gives a row of NaN.
+ * MICRO_ECAPACITY for tokens above max_tokens, here and below.
+ */
+MICRO_API micro_status micro_table_lookup(micro_table *table, const void *weight, int64_t weight_stride,
+                                          const void *ids, int32_t ids_type, int64_t tokens, double scale,
+                                          void *out, int64_t out_stride);
+
+/*
+ * The lookup's gradient: dweight[v] = scale * the sum of grad[t] over the
+ * tokens t with ids[t] == v, in ascending t and in binary32 (chunks of 32
+ * tokens of a row, then the chunks' sums), rounded to the type once.
+ * accumulate != 0 adds that to dweight[v] before rounding and leaves rows
+ * without a token untouched; else every row is written.  Tokens whose id is
+ * padding_id or outside [0, vocab) have no part.
+ */
+MICRO_API micro_status micro_table_lookup_grad(micro_table *table, const void *grad, int64_t grad_stride,
+                                               const void *ids, int32_t ids_type, int64_t tokens, double scale,
+                                               int32_t accumulate, void *dweight, int64_t dweight_stride);
+
+/*
+ * The softmax cross entropy of hidden rows against the table: with the logits
+ * l[t][v] = hidden[t] . weight[v], losses[t] = log(sum over v of exp(l[t][v]))
+ * - l[t][targets[t]], and *loss their sum (mean == 0) or mean over the counted
+ * tokens; 0 when none counts.  Products of the type's values are accumulated
+ * in binary32; the logits are not stored.
+ *   targets  int32 or int64; `ignored` marks a token that does not count (its
+ *            losses[t] is 0).  Any other target outside [0, vocab) does not
+ *            count either and makes losses[t] and *loss NaN.
+ *   losses   device float[tokens];  loss  device float.
+ * MICRO_ERANGE for a vocab above 2^22.
+ */
+MICRO_API micro_status micro_table_loss(micro_table *table, const void *hidden, int64_t hidden_stride,
+                                        const void *weight, int64_t weight_stride, const void *targets,
+                                        int32_t targets_type, int64_t tokens, int32_t mean, float *losses,
+                                        float *loss);
+
+/*
+ * The loss with its gradients, scaled by `scale` (and by 1 / counted tokens
+ * with mean != 0):
+ *   dhidden[t] = factor * sum over v of (p[t][v] - [v == targets[t]]) weight[v]
+ *   dweight[v] = factor * sum over t of (p[t][v] - [v == targets[t]]) hidden[t]
+ * with p the softmax of the logits.  A token that does not count has a zero
+ * row in dhidden and no part in dweight.  accumulate != 0 adds to dweight.
+ * Both are of the table's type, rounded once; between the products p - [..] is
+ * held in the table's type (binary32: to 24 bits), sums in binary32.
+ * No output may share memory with another argument.
+ */
+MICRO_API micro_status micro_table_loss_grad(micro_table *table, const void *hidden, int64_t hidden_stride,
+                                             const void *weight, int64_t weight_stride, const void *targets,
+                                             int32_t targets_type, int64_t tokens, int32_t mean, double scale,
+                                             int32_t accumulate, float *losses, float *loss, void *dhidden,
+                                             int64_t dhidden_stride, void *dweight, int64_t dweight_stride);
+
+/* Releases the handle's scratch after waiting for its stream; NULL is a no-op. */
+MICRO_API void micro_table_free(micro_table *table);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,6 +12,15 @@
 are views of the first k entries of preallocated output tensors.  Every step
 runs in the HIP library behind include/micro_sparsify.h; PyTorch only
 provides device memory and the stream.
+
+Around the step on a language model (language.py):
+
+    grads = GradientSet(tensors)                   # f32 / f16 / bf16, in the vector's order
+    norm = grads.flatten(grad, max_norm=1.0)       # global norm, clipped into the flat vector
+    table = TokenTable(vocab, dim, max_tokens, dtype=torch.bfloat16)
+    x = table.lookup(weight, ids)
+    loss, losses, dhidden, dweight = table.loss_grad(hidden, weight, targets)
+    table.lookup_grad(dx, ids, dweight, accumulate=True)
 """
 import ctypes
 
@@ -21,6 +30,7 @@ from ._lib import (MICRO_FLAG_SEPARATE_SCAN, MICRO_FLAG_TIME_KERNEL, MICRO_RULE_
                    MICRO_TOPK_ROUTE_FULL, MICRO_TOPK_ROUTE_HINT_LIST, MICRO_TOPK_ROUTE_HINT_PICK,
                    MICRO_TOPK_ROUTE_LIST, MICRO_VARIANT_STAGED, MICRO_VARIANT_TICKET, MicroError, default_config, micro_cycle, micro_estimate_threshold,
                    micro_partition, micro_threshold_f32)
+from .language import GradientSet, TokenTable
 
 __all__ = ["Sparsifier", "MicroError", "default_config", "micro_partition", "micro_cycle",
            "micro_estimate_threshold", "micro_threshold_f32", "MICRO_RULE_PROPORTIONAL",
@@ -28,7 +38,7 @@ __all__ = ["Sparsifier", "MicroError", "default_config", "micro_partition", "mic
            "MICRO_VARIANT_TICKET",
            "MICRO_VARIANT_STAGED",
            "MICRO_FLAG_TIME_KERNEL", "MICRO_FLAG_SEPARATE_SCAN", "MICRO_TOPK_ROUTE_FULL", "MICRO_TOPK_ROUTE_LIST",
-           "MICRO_TOPK_ROUTE_HINT_LIST", "MICRO_TOPK_ROUTE_HINT_PICK"]
+           "MICRO_TOPK_ROUTE_HINT_LIST", "MICRO_TOPK_ROUTE_HINT_PICK", "GradientSet", "TokenTable"]
 
 
 class Sparsifier:

@@ -13,6 +13,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmicro_sp
 MICRO_OK, MICRO_EINVAL, MICRO_ECAPACITY, MICRO_ERANGE, MICRO_ENOMEM, MICRO_EHIP = range(6)
 MICRO_RULE_PROPORTIONAL, MICRO_RULE_FIXED_STEP, MICRO_RULE_HARD_THRESHOLD, MICRO_RULE_TOPK = 0, 1, 2, 3
 MICRO_VARIANT_AUTO, MICRO_VARIANT_TICKET, MICRO_VARIANT_STAGED = 0, 1, 2
+MICRO_TYPE_F32, MICRO_TYPE_F16, MICRO_TYPE_BF16 = 0, 1, 2
+MICRO_IDS_I32, MICRO_IDS_I64 = 0, 1
 MICRO_FLAG_TIME_KERNEL = 1
 MICRO_FLAG_SEPARATE_SCAN = 2
 MICRO_TOPK_ROUTE_FULL, MICRO_TOPK_ROUTE_LIST, MICRO_TOPK_ROUTE_HINT_LIST, MICRO_TOPK_ROUTE_HINT_PICK = 1, 2, 3, 4
@@ -35,7 +37,13 @@ class micro_step_stats(ctypes.Structure):
                 ("topk_passes", ctypes.c_int32)]
 
 
+class micro_table_config(ctypes.Structure):
+    _fields_ = [("padding_id", ctypes.c_int64), ("ignored", ctypes.c_int64), ("score_bytes", ctypes.c_int64)]
+
+
 _cfgp = ctypes.POINTER(micro_config)
+_tcfgp = ctypes.POINTER(micro_table_config)
+_ptr, _i64, _i32, _dbl = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_double
 
 SIGNATURES = {
     "micro_config_default": (None, [_cfgp]),
@@ -68,6 +76,19 @@ SIGNATURES = {
     "micro_last_error": (ctypes.c_char_p, [ctypes.c_void_p]),
     "micro_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "micro_sparsify_free": (None, [ctypes.c_void_p]),
+    "micro_grads_init": (ctypes.c_int, [ctypes.POINTER(_ptr), _i32, _ptr, _ptr, _ptr, _ptr]),
+    "micro_grads_norm": (ctypes.c_int, [_ptr, _ptr, _ptr]),
+    "micro_grads_clip": (ctypes.c_int, [_ptr, _dbl, _ptr, _ptr]),
+    "micro_grads_flatten": (ctypes.c_int, [_ptr, _dbl, _ptr, _ptr, _ptr]),
+    "micro_grads_free": (None, [_ptr]),
+    "micro_table_config_default": (None, [_tcfgp]),
+    "micro_table_init": (ctypes.c_int, [ctypes.POINTER(_ptr), _i64, _i32, _i64, _i32, _ptr, _tcfgp]),
+    "micro_table_lookup": (ctypes.c_int, [_ptr, _ptr, _i64, _ptr, _i32, _i64, _dbl, _ptr, _i64]),
+    "micro_table_lookup_grad": (ctypes.c_int, [_ptr, _ptr, _i64, _ptr, _i32, _i64, _dbl, _i32, _ptr, _i64]),
+    "micro_table_loss": (ctypes.c_int, [_ptr, _ptr, _i64, _ptr, _i64, _ptr, _i32, _i64, _i32, _ptr, _ptr]),
+    "micro_table_loss_grad": (ctypes.c_int, [_ptr, _ptr, _i64, _ptr, _i64, _ptr, _i32, _i64, _i32, _dbl, _i32, _ptr,
+                                             _ptr, _ptr, _i64, _ptr, _i64]),
+    "micro_table_free": (None, [_ptr]),
 }
 
 _lib = None
@@ -252,3 +273,36 @@ def micro_sparsify_last_stats(ctx):
 
 def micro_sparsify_free(ctx):
     load().micro_sparsify_free(ctx)
+
+
+def micro_grads_init(addresses, sizes, types, stream_handle=None):
+    """Raw call with device addresses, value counts and MICRO_TYPE_* of the
+    set's tensors; returns the handle."""
+    n = len(addresses)
+    grads = ctypes.c_void_p()
+    # named, so that they outlive the call
+    at, counts, kinds = (_ptr * n)(*addresses), (_i64 * n)(*sizes), (_i32 * n)(*types)
+    check(load().micro_grads_init(ctypes.byref(grads), n, at, counts, kinds, ctypes.c_void_p(stream_handle or 0)))
+    return grads
+
+
+def micro_grads_free(grads):
+    load().micro_grads_free(grads)
+
+
+def default_table_config():
+    c = micro_table_config()
+    load().micro_table_config_default(ctypes.byref(c))
+    return c
+
+
+def micro_table_init(vocab, dim, max_tokens, value_type, stream_handle=None, cfg=None):
+    table = ctypes.c_void_p()
+    check(load().micro_table_init(ctypes.byref(table), int(vocab), int(dim), int(max_tokens), int(value_type),
+                                  ctypes.c_void_p(stream_handle or 0),
+                                  ctypes.byref(cfg) if cfg is not None else None))
+    return table
+
+
+def micro_table_free(table):
+    load().micro_table_free(table)

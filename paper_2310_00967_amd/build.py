@@ -38,7 +38,9 @@ DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-p
 # up at once, and most of its workgroups leave their tiles to the others.
 TAKEOVER_LIB = os.path.join(ROOT, "tests", "libmicro_takeover.so")
 TAKEOVER = ["-DMICRO_PASS_PATIENCE=1", "-DMICRO_PASS_ABSENT"]
-KERNEL_SOURCES = ["sparsify_kernel.hip", "union_kernel.hip", "static_scratch.hip", "topk_kernel.hip"]
+KERNEL_SOURCES = ["sparsify_kernel.hip", "union_kernel.hip", "static_scratch.hip", "topk_kernel.hip",
+                  "gradients_kernel.hip", "lookup_kernel.hip", "loss_kernel.hip"]
+HOST_SOURCES = ["micro_sparsify.cpp", "gradients.cpp", "token_table.cpp"]
 
 
 def _run(cmd, verbose):
@@ -57,15 +59,17 @@ def build_library(verbose=False, extra_device_flags=()):
         _run([cc, *COMMON, *DEVICE, *extra_device_flags, "-x", "hip", "-c",
               os.path.join(CSRC, src), "-o", obj], verbose)
         kobjs.append(obj)
-    hobj = os.path.join(BUILD_DIR, "micro_sparsify.o")
-    _run([cc, *COMMON, "-fvisibility=hidden", "-c", os.path.join(CSRC, "micro_sparsify.cpp"),
-          "-o", hobj], verbose)
+    hobjs = []
+    for src in HOST_SOURCES:
+        obj = os.path.join(BUILD_DIR, os.path.splitext(src)[0] + ".o")
+        _run([cc, *COMMON, "-fvisibility=hidden", "-c", os.path.join(CSRC, src), "-o", obj], verbose)
+        hobjs.append(obj)
     obj = os.path.join(BUILD_DIR, "sparsify_kernel_takeover.o")
     _run([cc, *COMMON, *DEVICE, *extra_device_flags, *TAKEOVER, "-x", "hip", "-c",
           os.path.join(CSRC, KERNEL_SOURCES[0]), "-o", obj], verbose)
     for lib, first in ((TAKEOVER_LIB, obj), (LIB, kobjs[0])):
         tmp = lib + ".tmp"
-        _run([cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, first, *kobjs[1:], hobj], verbose)
+        _run([cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, first, *kobjs[1:], *hobjs], verbose)
         os.replace(tmp, lib)
     return LIB
 

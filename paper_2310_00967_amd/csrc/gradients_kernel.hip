@@ -1,0 +1,163 @@
+// gfx950 kernels of a gradient set: the global norm over many tensors, and
+// their clipping in place or into the flat vector that the sparsify step
+// reads.
+//   norm    sum of squares, each product and every addition in binary64 (the
+//           product of two binary32 values is exact there);
+//   factor  c = min(1, max_norm / (norm + 1e-6)) in binary64, once rounded to
+//           binary32; a norm of +inf gives 0, a NaN gives NaN;
+//   scale   c * g in binary32, once rounded to the destination's type.
+// Both are streams, bound by HBM: the norm reads every value once, the scale
+// reads it again (no value can be scaled before the last is summed) and
+// writes it.  Tensors are cut into pieces of equal length on the host, so one
+// launch covers all of them and a workgroup's work does not depend on how a
+// model is cut into tensors.
+#include "gradients_kernel.h"
+#include "micro_sparsify.h"
+#include "value_types.h"
+
+namespace micro {
+namespace {
+
+// Loads that a thread has in flight before it uses the first.
+constexpr int kUnroll = 4;
+
+template <class T>
+__device__ double sum_squares(const T* p, int n) {
+    constexpr int kVec = 16 / sizeof(T), kStep = kGradBlock * kVec;
+    double sum[kUnroll] = {};
+    int i = threadIdx.x * kVec;
+    for (; i + (kUnroll - 1) * kStep + kVec <= n; i += kUnroll * kStep) {
+        float x[kUnroll][kVec];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) load_floats<T, kVec>(p + i + u * kStep, x[u]);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                const double d = static_cast<double>(x[u][j]);
+                sum[u] = __builtin_fma(d, d, sum[u]);
+            }
+    }
+    for (; i < n; i += kStep)
+        for (int j = i; j < n && j < i + kVec; ++j) {
+            const double d = static_cast<double>(static_cast<float>(p[j]));
+            sum[0] = __builtin_fma(d, d, sum[0]);
+        }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// The sum over the workgroup, in a fixed order; in thread 0.
+__device__ double block_sum(double x) {
+    __shared__ double waves[kGradBlock / 64];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double sum = 0.0;
+    for (int w = 0; w < kGradBlock / 64; ++w) sum += waves[w];
+    return sum;
+}
+
+// A workgroup takes every gridDim.x-th piece; the one that finishes last adds
+// the workgroups' sums in their order, so the result does not depend on when
+// each came.
+__global__ __launch_bounds__(kGradBlock) void norm_kernel(GradSetDevice set, double* sumsq, float* norm) {
+    double sum = 0.0;
+    for (int64_t i = blockIdx.x; i < set.count; i += gridDim.x) {
+        const GradPiece piece = set.pieces[i];
+        if (piece.type == MICRO_TYPE_F32)
+            sum += sum_squares(static_cast<const float*>(piece.values), piece.count);
+        else if (piece.type == MICRO_TYPE_F16)
+            sum += sum_squares(static_cast<const f16*>(piece.values), piece.count);
+        else
+            sum += sum_squares(static_cast<const bf16*>(piece.values), piece.count);
+    }
+    sum = block_sum(sum);
+    __shared__ bool last;
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(set.partials + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = __hip_atomic_fetch_add(set.arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    sum = 0.0;
+    for (uint32_t b = threadIdx.x; b < gridDim.x; b += kGradBlock)
+        sum += __hip_atomic_load(set.partials + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) {
+        if (sumsq) *sumsq = sum;
+        if (norm) *norm = static_cast<float>(sqrt(sum));
+        __hip_atomic_store(set.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+}
+
+// n values of src times c into dst, which may be src.
+template <class S, class D>
+__device__ void scale_run(const S* src, D* dst, int n, float c) {
+    // as many values a thread as make the wider side's access 16 bytes
+    constexpr int kVec = 16 / (sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D)), kStep = kGradBlock * kVec;
+    int i = threadIdx.x * kVec;
+    for (; i + (kUnroll - 1) * kStep + kVec <= n; i += kUnroll * kStep) {
+        float x[kUnroll][kVec];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) load_floats<S, kVec>(src + i + u * kStep, x[u]);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) x[u][j] *= c;
+            store_floats<D, kVec>(dst + i + u * kStep, x[u]);
+        }
+    }
+    for (; i < n; i += kStep)
+        for (int j = i; j < n && j < i + kVec; ++j) dst[j] = rounded<D>(static_cast<float>(src[j]) * c);
+}
+
+template <class T>
+__device__ void scale_piece(const GradPiece& piece, float* flat, float c) {
+    T* values = static_cast<T*>(piece.values);
+    if (flat)
+        scale_run<T, float>(values, flat + piece.offset, piece.count, c);
+    else
+        scale_run<T, T>(values, values, piece.count, c);
+}
+
+__global__ __launch_bounds__(kGradBlock) void scale_kernel(GradSetDevice set, const double* sumsq, double max_norm,
+                                                           float* flat, float* norm) {
+    float c = 1.0f;
+    if (sumsq) {
+        const double length = sqrt(*sumsq), ratio = max_norm / (length + 1e-6);
+        if (max_norm < __builtin_inf() && !(ratio >= 1.0)) c = static_cast<float>(ratio);
+        if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(length);
+    }
+    if (!flat && c == 1.0f) return;  // in place and nothing to clip
+    for (int64_t i = blockIdx.x; i < set.count; i += gridDim.x) {
+        const GradPiece piece = set.pieces[i];
+        if (piece.type == MICRO_TYPE_F32)
+            scale_piece<float>(piece, flat, c);
+        else if (piece.type == MICRO_TYPE_F16)
+            scale_piece<f16>(piece, flat, c);
+        else
+            scale_piece<bf16>(piece, flat, c);
+    }
+}
+
+uint32_t pass_grid(int64_t pieces) {
+    return static_cast<uint32_t>(pieces < 1 ? 1 : pieces > kGradGridMax ? kGradGridMax : pieces);
+}
+
+}  // namespace
+
+hipError_t launch_grads_norm(const GradSetDevice& set, double* sumsq, float* norm, hipStream_t stream) {
+    hipLaunchKernelGGL(norm_kernel, dim3(pass_grid(set.count)), dim3(kGradBlock), 0, stream, set, sumsq, norm);
+    return hipGetLastError();
+}
+
+hipError_t launch_grads_scale(const GradSetDevice& set, const double* sumsq, double max_norm, float* flat,
+                              float* norm, hipStream_t stream) {
+    hipLaunchKernelGGL(scale_kernel, dim3(pass_grid(set.count)), dim3(kGradBlock), 0, stream, set, sumsq, max_norm,
+                       flat, norm);
+    return hipGetLastError();
+}
+
+}  // namespace micro

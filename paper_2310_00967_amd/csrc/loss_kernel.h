@@ -1,0 +1,67 @@
+// Launches of the token loss and its gradients (loss_kernel.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "lookup_kernel.h"
+
+namespace micro {
+
+// Products advance 64 values of the summed axis at a time: padded axes are
+// multiples of it.
+constexpr int kProductDepth = 64;
+// binary32 operands enter the products as the sum of this many bfloat16 ones.
+constexpr int kSplitPlanes = 3;
+// Vocabulary rows that share one running maximum: what one wavefront of the
+// score product holds (with few tokens, kGranuleFew).
+constexpr int kGranule = 128, kGranuleFew = 32;
+// Calls of up to this many tokens take the narrow product tiles.
+constexpr int kFewTokens = 64;
+
+// One call's operands and scratch.  Lengths: D = dim, Dp = D rounded up to
+// kProductDepth, Vp = vocab rounded up to it, B = tokens of a block (a
+// multiple of 256), P = planes (kSplitPlanes for binary32, else 1).
+struct LossCall {
+    int32_t type;            // of hidden, table and gradients
+    int64_t vocab, vocab_padded;
+    int32_t dim, dim_padded;
+    int64_t tokens, block;   // B
+    Rows hidden, table;
+    TokenIds targets;
+    int64_t ignored;         // the target value that does not count
+    bool mean;
+    float scale;             // of the gradients
+    float* losses;           // out, one per token
+    float* loss;             // out
+    bool gradients;
+    bool accumulate;         // add to dtable
+    Rows dhidden, dtable;    // out
+    // scratch
+    int32_t* count;          // counted tokens
+    int32_t* rows;           // their positions, ascending
+    int32_t* labels;         // and targets
+    float* counted_losses;   // one per counted token
+    void* h;                 // counted rows of hidden, [P][tokens rounded up to 64][Dp]
+    void* w;                 // table rows, [P][vocab][Dp], where the table itself cannot be read in place
+    float2* stats;           // (maximum, sum of exponentials) of [granule][B]
+    float* label_logit;      // [B]
+    float2* softmax;         // (maximum, 1 / sum of exponentials) of [B]
+    void* scores;            // exponentials, then logit gradients, [B][Vp]; binary32: floats
+    void* split;             // binary32: the logit gradients as [P][B][Vp] bfloat16
+    float* partials;         // tiles of products that are split along the summed axis
+    int64_t partial_tiles;   // wide tiles it holds
+    float* carried;          // wide tiles of dtable between token blocks; null with one block
+    int compute_units;
+};
+
+// Whether the product can read the table where it is.
+bool table_in_place(const LossCall& c);
+
+hipError_t launch_loss(const LossCall& call, hipStream_t stream);
+
+// Floats of one wide product tile.
+constexpr int64_t kWideTile = 256 * 256;
+
+}  // namespace micro

@@ -1,0 +1,863 @@
+// gfx950 kernels of the softmax cross entropy over a token table and of its
+// gradients:
+//   l_tv = h_t . W_v,   lse_t = log sum_v exp l_tv,   loss_t = lse_t - l_ty
+//   g_tv = exp(l_tv - lse_t) - [v = y_t]
+//   dh = f g W,   dW = f g^T h,   f = scale, or scale / counted tokens
+// Three products of tokens, vocabulary and width on the matrix cores, in
+// blocks of tokens: a block's exponentials exist in 16 bits, the logits
+// themselves never leave the registers.  Each granule of vocabulary rows is
+// normalised by its own maximum, and the granules are joined per token
+// afterwards, so one pass over the table gives both the loss and what the
+// gradients need.  Tokens that do not count are left out before the first
+// product: everything below runs over the counted tokens only, whose number
+// stays on the device.
+//
+// binary32 operands are split into three bfloat16 terms (24 bits of
+// significand); a product is the sum of the six products of terms whose
+// weights are above 2^-24, accumulated in binary32 like the others.
+#include "loss_kernel.h"
+
+#include <algorithm>
+
+#include "micro_sparsify.h"
+#include "value_types.h"
+
+namespace micro {
+namespace {
+
+constexpr int kDepth = kProductDepth;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+template <class T>
+using Vec8 = T __attribute__((ext_vector_type(8)));
+template <class T>
+using Vec4 = T __attribute__((ext_vector_type(4)));
+using Acc = float __attribute__((ext_vector_type(16)));
+
+#define MICRO_SHARED __attribute__((address_space(3)))
+
+__device__ __forceinline__ Acc mma(Vec8<bf16> a, Vec8<bf16> b, Acc c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ Acc mma(Vec8<f16> a, Vec8<f16> b, Acc c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+template <class T>
+__device__ __forceinline__ Vec4<T> read_transposed(const T* p) {
+    return __builtin_bit_cast(Vec4<T>, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MICRO_SHARED Vec4<short>*)p));
+}
+
+// ---------------------------------------------------------------------------
+// the product C[a][b] = sum_k A[a][k] B[b][k]
+// ---------------------------------------------------------------------------
+
+// One operand.  Straight: rows of the kept axis, k adjacent.  Turned: rows of
+// k, the kept axis adjacent.
+struct Operand {
+    const void* at;
+    int64_t stride;  // values between rows
+    int64_t kept;    // valid values of the kept axis (turned: a multiple of 8)
+    int64_t depth;   // turned: valid rows of k; those behind read the last one
+    int64_t plane;   // values between the planes of a split operand
+};
+
+// A workgroup of kWavesA x kWavesB wavefronts, each with kTilesA x kTilesB
+// matrix tiles of 32 x 32.
+template <int WA, int WB, int TA, int TB>
+struct Shape {
+    static constexpr int kWavesA = WA, kWavesB = WB, kTilesA = TA, kTilesB = TB;
+    static constexpr int kThreads = 64 * WA * WB;
+    static constexpr int kA = WA * TA * 32, kB = WB * TB * 32;  // the tile of C
+    static constexpr int kPerUnit = 160 * 1024 / (2 * (kA + kB) * kDepth * 2);  // workgroups of a compute unit
+};
+using Wide = Shape<2, 4, 4, 2>;
+using Narrow32 = Shape<4, 1, 1, 1>;
+using Narrow64 = Shape<4, 1, 1, 2>;
+
+// The tile of an operand in shared memory: kR values of the kept axis by
+// kDepth of k, filled by loads that go from global to shared memory without
+// registers, 16 bytes a lane and the lanes of a wavefront in order.  So that
+// fragments are read without bank conflicts the 16-byte units of a row are
+// permuted where they come from: straight rows by the row, turned rows (in
+// pairs of units) by k.
+template <class T, int kR, bool kTurned, int kThreads>
+struct Stage {
+    static constexpr int kLoads = kR * kDepth / 8 / kThreads;
+    static_assert(kLoads * kThreads * 8 == kR * kDepth, "a tile is a whole number of loads");
+    uint32_t offset[kLoads];  // bytes from the tile's first value
+
+    // The four rows of k that a group of lanes reads together lie 2 kR bytes
+    // apart; what to permute a turned row's pairs by so that they do not meet
+    // in the same 256 bytes of banks.
+    static constexpr uint32_t swizzle(uint32_t k) { return kR >= 128 ? (k & 3) * 2 : kR == 64 ? (k & 2) : 0; }
+
+    // What this thread loads of the tile at `first` of the kept axis.  depth:
+    // valid rows of k from the tile's first.
+    __device__ void place(const Operand& op, int64_t first, int64_t depth) {
+        const uint32_t kept = static_cast<uint32_t>(op.kept - first < kR ? op.kept - first : kR);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t unit = i * kThreads + threadIdx.x;
+            if constexpr (kTurned) {
+                uint32_t k = unit / (kR / 8), c = unit % (kR / 8) ^ swizzle(k) * 2;
+                c = c * 8 + 8 <= kept ? c * 8 : kept - 8;
+                k = k < depth ? k : static_cast<uint32_t>(depth - 1);
+                offset[i] = (k * static_cast<uint32_t>(op.stride) + c) * sizeof(T);
+            } else {
+                uint32_t row = unit / 8;
+                const uint32_t c = (unit % 8) ^ ((row >> 1) & 7);
+                row = row < kept ? row : kept - 1;
+                offset[i] = (row * static_cast<uint32_t>(op.stride) + c * 8) * sizeof(T);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void load(const char* from, char* to) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)(from + offset[i]),
+                (MICRO_SHARED void*)(to + (i * kThreads + (threadIdx.x & ~63u)) * 16), 16, 0, 0);
+    }
+
+    // Values [base, base + 32) of the kept axis by k [kk * 16, + 16): lane l
+    // holds value l % 32 and the eight k from 8 * (l / 32).
+    static __device__ __forceinline__ Vec8<T> fragment(const char* tile, int base, int kk) {
+        const int lane = threadIdx.x & 63;
+        if constexpr (kTurned) {
+            // four k by 16 values transposed by each group of 16 lanes, twice
+            const int k = kk * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
+            const int pair = (base >> 4) + ((lane >> 4) & 1);
+            const T* row = reinterpret_cast<const T*>(tile) + k * kR + ((pair ^ swizzle(k)) * 16) + (lane & 3) * 4;
+            const Vec4<T> lo = read_transposed(row), hi = read_transposed(row + 4 * kR);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            const int row = base + (lane & 31), c = kk * 2 + (lane >> 5);
+            return *reinterpret_cast<const Vec8<T>*>(tile + row * (kDepth * 2) + ((c ^ ((row >> 1) & 7)) * 16));
+        }
+    }
+};
+
+// The planes of a and b of a split operand's six products, four bits each;
+// the first is that of a plain one.
+constexpr uint32_t kPlanesA = 0x201100, kPlanesB = 0x021010;
+
+// acc += the steps [step, end) of the tile at (a, b): step s is block s %
+// blocks of k of term pair s / blocks.  Two stages of shared memory: while the
+// matrix cores work on one, the loads of the next step fill the other.
+template <class S, class T, int kTerms, bool kTurnA, bool kTurnB>
+__device__ void product(const Operand& A, int64_t a, const Operand& B, int64_t b, int64_t blocks, int64_t step,
+                        int64_t end, char* stage0, char* stage1, Acc (&acc)[S::kTilesA][S::kTilesB]) {
+    using StageA = Stage<T, S::kA, kTurnA, S::kThreads>;
+    using StageB = Stage<T, S::kB, kTurnB, S::kThreads>;
+    constexpr int kSecond = S::kA * kDepth * 2;
+    StageA sa;
+    StageB sb;
+    sa.place(A, a, kDepth);
+    sb.place(B, b, kDepth);
+    const char* at_a = static_cast<const char*>(A.at) + (kTurnA ? a : a * A.stride) * int64_t(sizeof(T));
+    const char* at_b = static_cast<const char*>(B.at) + (kTurnB ? b : b * B.stride) * int64_t(sizeof(T));
+    const int64_t step_a = (kTurnA ? A.stride * kDepth : kDepth) * int64_t(sizeof(T));
+    const int64_t step_b = (kTurnB ? B.stride * kDepth : kDepth) * int64_t(sizeof(T));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave_a = wave / S::kWavesB * (S::kTilesA * 32), wave_b = wave % S::kWavesB * (S::kTilesB * 32);
+
+    const auto load = [&](int64_t s, char* stage) {
+        const int term = kTerms == 1 ? 0 : static_cast<int>(s / blocks);
+        const int64_t k = s - term * blocks;
+        const char* from_a = at_a + (kPlanesA >> 4 * term & 15) * A.plane * int64_t(sizeof(T)) + k * step_a;
+        const char* from_b = at_b + (kPlanesB >> 4 * term & 15) * B.plane * int64_t(sizeof(T)) + k * step_b;
+        if (kTurnA && (k + 1) * kDepth > A.depth) {
+            StageA tail;
+            tail.place(A, a, A.depth - k * kDepth);
+            tail.load(from_a, stage);
+        } else {
+            sa.load(from_a, stage);
+        }
+        if (kTurnB && (k + 1) * kDepth > B.depth) {
+            StageB tail;
+            tail.place(B, b, B.depth - k * kDepth);
+            tail.load(from_b, stage + kSecond);
+        } else {
+            sb.load(from_b, stage + kSecond);
+        }
+    };
+    const auto compute = [&](const char* stage) {
+#pragma unroll
+        for (int kk = 0; kk < kDepth / 16; ++kk) {
+            Vec8<T> fa[S::kTilesA], fb[S::kTilesB];
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i) fa[i] = StageA::fragment(stage, wave_a + i * 32, kk);
+#pragma unroll
+            for (int j = 0; j < S::kTilesB; ++j) fb[j] = StageB::fragment(stage + kSecond, wave_b + j * 32, kk);
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kTilesB; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
+        }
+    };
+    const auto arrived = [] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    __syncthreads();  // the stages are free
+    if (step < end) load(step, stage0);
+    while (step < end) {
+        arrived();
+        if (step + 1 < end) load(step + 1, stage1);
+        compute(stage0);
+        if (++step >= end) break;
+        arrived();
+        if (step + 1 < end) load(step + 1, stage0);
+        compute(stage1);
+        ++step;
+    }
+}
+
+template <class S>
+__device__ void clear(Acc (&acc)[S::kTilesA][S::kTilesB]) {
+#pragma unroll
+    for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kTilesB; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+}
+
+// Where a lane's four adjacent values acc[i][j][4 q .. 4 q + 3] lie in C.
+template <class S>
+struct Place {
+    int a, b;  // of the lane's first value in the tile
+    __device__ Place() {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        a = wave / S::kWavesB * (S::kTilesA * 32) + (lane >> 5) * 4;
+        b = wave % S::kWavesB * (S::kTilesB * 32) + (lane & 31);
+    }
+    __device__ int row(int i, int q) const { return a + i * 32 + q * 8; }
+    __device__ int column(int j) const { return b + j * 32; }
+};
+
+// Tiles of C for a grid of workgroups that each take several.  Workgroups go
+// to the eight dies in turn, and each die has its own L2: a die takes a run of
+// neighbouring tiles, ordered so that those in flight at once (four along a by
+// the rest along b) share their operands.
+struct TileOrder {
+    int64_t tiles_a, tiles_b, splits;
+    int64_t per_die, at, stride;
+    static constexpr int kDies = 8, kGroup = 4;
+    __device__ TileOrder(int64_t ta, int64_t tb, int64_t s) : tiles_a(ta), tiles_b(tb), splits(s) {
+        const int64_t total = ta * tb * s;
+        per_die = (total + kDies - 1) / kDies;
+        at = blockIdx.x / kDies;
+        stride = gridDim.x / kDies;
+    }
+    __device__ bool next(int64_t* a, int64_t* b, int64_t* split) {
+        const int64_t linear = (blockIdx.x % kDies) * per_die + at;
+        if (at >= per_die || linear >= tiles_a * tiles_b * splits) return false;
+        at += stride;
+        *split = linear / (tiles_a * tiles_b);
+        const int64_t in = linear % (tiles_a * tiles_b), group = in / (kGroup * tiles_b);
+        const int64_t rest = in % (kGroup * tiles_b);
+        const int64_t width = tiles_a - group * kGroup < kGroup ? tiles_a - group * kGroup : kGroup;
+        *a = group * kGroup + rest % width;
+        *b = rest / width;
+        return true;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// before the products
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ int64_t target_of(const TokenIds& ids, int64_t t) {
+    return ids.wide ? static_cast<const int64_t*>(ids.at)[t] : static_cast<const int32_t*>(ids.at)[t];
+}
+
+constexpr int kSelectBlock = 1024;
+
+// The counted tokens in ascending order.  losses: 0 for an ignored token, NaN
+// for a target outside the vocabulary (which does not count either).
+__global__ __launch_bounds__(kSelectBlock) void select_kernel(TokenIds targets, int64_t tokens, int64_t ignored, int64_t vocab,
+                                                              int32_t* count, int32_t* rows, int32_t* labels, float* losses) {
+    __shared__ int32_t waves[kSelectBlock / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int32_t before = 0;
+    for (int64_t first = 0; first < tokens; first += kSelectBlock) {
+        const int64_t t = first + threadIdx.x;
+        const int64_t y = t < tokens ? target_of(targets, t) : ignored;
+        const bool counted = t < tokens && y != ignored && y >= 0 && y < vocab;
+        const uint64_t all = __ballot(counted);
+        __syncthreads();
+        if (lane == 0) waves[wave] = __popcll(all);
+        __syncthreads();
+        int32_t at = before;
+        for (int w = 0; w < kSelectBlock / 64; ++w) {
+            if (w < wave) at += waves[w];
+            before += waves[w];
+        }
+        if (counted) {
+            at += __popcll(all & ((uint64_t(1) << lane) - 1));
+            rows[at] = static_cast<int32_t>(t);
+            labels[at] = static_cast<int32_t>(y);
+        } else if (t < tokens) {
+            losses[t] = y == ignored ? 0.0f : __builtin_nanf("");
+        }
+    }
+    if (threadIdx.x == 0) *count = before;
+}
+
+// x as a + b + c.  A first term that would round past bfloat16's range is cut
+// instead.  An infinity or a NaN goes into the last term, which meets only the
+// other operand's first: its product is what x's own would be, and no term of
+// zero meets it.
+__device__ __forceinline__ void split3(float x, bf16& a, bf16& b, bf16& c) {
+    const uint32_t bits = __float_as_uint(x);
+    a = static_cast<bf16>(x);
+    if (!__builtin_isfinite(static_cast<float>(a))) a = __builtin_bit_cast(bf16, static_cast<uint16_t>(bits >> 16));
+    const float r = x - static_cast<float>(a);
+    b = static_cast<bf16>(r);
+    c = static_cast<bf16>(r - static_cast<float>(b));
+    if ((bits & 0x7f800000u) == 0x7f800000u) {
+        c = static_cast<bf16>(x);
+        a = b = static_cast<bf16>(0.0f);
+    }
+}
+
+// One row of `dim` values into `padded` values of each plane, zeros behind.
+template <class T>
+__device__ void copy_row(const T* from, int dim, T* to, int padded, int64_t) {
+    for (int c = threadIdx.x * 8; c < padded; c += blockDim.x * 8) {
+        Pack<T, 8> x;
+        if (c + 8 <= dim)
+            x = *reinterpret_cast<const Pack<T, 8>*>(from + c);
+        else
+            for (int j = 0; j < 8; ++j) x.v[j] = c + j < dim ? from[c + j] : static_cast<T>(0.0f);
+        *reinterpret_cast<Pack<T, 8>*>(to + c) = x;
+    }
+}
+__device__ void copy_row(const float* from, int dim, bf16* to, int padded, int64_t plane) {
+    for (int c = threadIdx.x * 4; c < padded; c += blockDim.x * 4) {
+        Pack<bf16, 4> p[kSplitPlanes];
+        for (int j = 0; j < 4; ++j)
+            split3(c + j < dim ? from[c + j] : 0.0f, p[0].v[j], p[1].v[j], p[2].v[j]);
+        for (int q = 0; q < kSplitPlanes; ++q) *reinterpret_cast<Pack<bf16, 4>*>(to + q * plane + c) = p[q];
+    }
+}
+
+constexpr int kRowBlock = 256;
+
+// The counted rows of hidden, padded, with zero rows up to a multiple of
+// kDepth; and zeros into dhidden's rows of tokens that do not count.
+template <class In, class T>
+__global__ __launch_bounds__(kRowBlock) void gather_kernel(const In* hidden, int64_t stride, int64_t tokens, int dim,
+                                                           const int32_t* count, const int32_t* rows, T* h, int padded,
+                                                           int64_t plane, TokenIds targets, int64_t ignored, int64_t vocab,
+                                                           In* dhidden, int64_t dstride) {
+    const int64_t n = *count, r = blockIdx.x;
+    if (r < n) {
+        copy_row(hidden + rows[r] * stride, dim, h + r * padded, padded, plane);
+    } else if (r < (n + kDepth - 1) / kDepth * kDepth) {
+        copy_row(hidden, 0, h + r * padded, padded, plane);
+    }
+    if (dhidden && r < tokens) {
+        const int64_t y = target_of(targets, r);
+        if (y == ignored || y < 0 || y >= vocab)
+            for (int c = threadIdx.x; c < dim; c += kRowBlock) dhidden[r * dstride + c] = static_cast<In>(0.0f);
+    }
+}
+
+template <class In, class T>
+__global__ __launch_bounds__(kRowBlock) void table_kernel(const In* table, int64_t stride, int dim, T* w, int padded,
+                                                          int64_t plane) {
+    copy_row(table + blockIdx.x * stride, dim, w + blockIdx.x * int64_t(padded), padded, plane);
+}
+
+// ---------------------------------------------------------------------------
+// scores: the first product, with the softmax's partial sums
+// ---------------------------------------------------------------------------
+
+// A block's exponentials and logit gradients, none above 1, are held times
+// this: binary16, whose smallest normal number is 2^-14 and whose range ends
+// at 65504, keeps its full precision down to 2^-28 that way.
+template <class E>
+constexpr float kHeldUnit = 1.0f;
+template <>
+constexpr float kHeldUnit<f16> = 16384.0f;
+
+struct ScoreOut {
+    const int32_t* count;
+    const int32_t* labels;
+    int64_t first, block;      // the token block and B
+    int64_t vocab, padded;
+    float2* stats;
+    float* label_logit;
+    void* scores;              // null: the loss alone
+};
+
+// a: vocabulary, b: tokens, so a lane holds one token's logits and reduces
+// them without shuffles but the one between its two halves.
+template <class S, class T, class E, int kTerms>
+__global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Operand h, int64_t blocks, ScoreOut out) {
+    __shared__ __attribute__((aligned(1024))) char stage0[(S::kA + S::kB) * kDepth * 2];
+    __shared__ __attribute__((aligned(1024))) char stage1[(S::kA + S::kB) * kDepth * 2];
+    const int64_t counted = *out.count - out.first;
+    const int64_t n = counted < out.block ? counted : out.block;
+    if (n <= 0) return;
+    h.kept = n;
+    TileOrder order((out.vocab + S::kA - 1) / S::kA, (n + S::kB - 1) / S::kB, 1);
+    const Place<S> place;
+    int64_t ta, tb, split;
+    while (order.next(&ta, &tb, &split)) {
+        Acc acc[S::kTilesA][S::kTilesB];
+        clear<S>(acc);
+        product<S, T, kTerms, false, false>(table, ta * S::kA, h, tb * S::kB, blocks, 0, kTerms * blocks, stage0, stage1, acc);
+#pragma unroll
+        for (int j = 0; j < S::kTilesB; ++j) {
+            const int64_t token = tb * S::kB + place.column(j);
+            const int64_t v0 = ta * S::kA + place.row(0, 0);
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (v0 + i * 32 + (r >> 2) * 8 + (r & 3) >= out.vocab) acc[i][j][r] = -__builtin_inff();
+                    most = fmaxf(most, acc[i][j][r]);
+                }
+            most = fmaxf(most, __shfl_xor(most, 32));
+            const int64_t label = token < n ? out.labels[out.first + token] - v0 : -1;
+            if (label >= 0 && label < S::kTilesA * 32 && (label & 4) == 0) {
+#pragma unroll
+                for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (label == i * 32 + (r >> 2) * 8 + (r & 3)) out.label_logit[token] = acc[i][j][r];
+            }
+            // a granule without a finite maximum keeps its logits' own limits
+            const float base = most == -__builtin_inff() ? 0.0f : most;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float e[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        e[r] = __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - base) * kLog2e);
+                        sum += e[r];
+                        e[r] *= kHeldUnit<E>;
+                    }
+                    const int64_t v = ta * S::kA + place.row(i, q);
+                    if (out.scores && token < n && v < out.padded)
+                        store_floats<E, 4>(static_cast<E*>(out.scores) + token * out.padded + v, e);
+                }
+            sum += __shfl_xor(sum, 32);
+            if ((threadIdx.x & 32) == 0 && token < n) {
+                const int64_t granule = (ta * S::kA + place.row(0, 0)) / (S::kTilesA * 32);
+                out.stats[granule * out.block + token] = make_float2(most, sum);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// between the products
+// ---------------------------------------------------------------------------
+
+constexpr int kJoinTokens = 32, kJoinSlices = 16;
+
+// Maximum, inverse sum and loss of every counted token of the block, from its
+// granules.
+__global__ __launch_bounds__(kJoinTokens* kJoinSlices) void softmax_kernel(const int32_t* count, int64_t first, int64_t block,
+                                                                           const float2* stats, int64_t granules,
+                                                                           const float* label_logit, const int32_t* rows,
+                                                                           float2* softmax, float* counted_losses, float* losses) {
+    __shared__ float2 part[kJoinSlices][kJoinTokens];
+    const int64_t counted = *count - first, n = counted < block ? counted : block;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * kJoinTokens + (threadIdx.x % kJoinTokens);
+    const int slice = threadIdx.x / kJoinTokens;
+    if (static_cast<int64_t>(blockIdx.x) * kJoinTokens >= n) return;
+    const int64_t at = token < n ? token : n - 1;
+    float most = -__builtin_inff(), sum = 0.0f;
+    const auto join = [&](float2 s) {
+        const float to = fmaxf(most, s.x);
+        if (to == -__builtin_inff()) {
+            sum += s.y;  // both sums are 0, or NaN
+            return;
+        }
+        sum = sum * __builtin_amdgcn_exp2f((most - to) * kLog2e) + s.y * __builtin_amdgcn_exp2f((s.x - to) * kLog2e);
+        most = to;
+    };
+    for (int64_t g = slice; g < granules; g += 4 * kJoinSlices) {
+        float2 s[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            s[u] = g + u * kJoinSlices < granules ? stats[(g + u * kJoinSlices) * block + at]
+                                                  : make_float2(-__builtin_inff(), 0.0f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) join(s[u]);
+    }
+    part[slice][threadIdx.x % kJoinTokens] = make_float2(most, sum);
+    __syncthreads();
+    if (slice != 0 || token >= n) return;
+    most = -__builtin_inff(), sum = 0.0f;
+    for (int s = 0; s < kJoinSlices; ++s) join(part[s][threadIdx.x]);
+    // (the label's logit is often the maximum itself, and their difference exact)
+    const float loss = (most - label_logit[token]) + logf(sum);
+    softmax[token] = make_float2(most, 1.0f / sum);
+    counted_losses[first + token] = loss;
+    losses[rows[first + token]] = loss;
+}
+
+constexpr int kTurnBlock = 256, kTurnRows = 16;
+
+// The exponentials of a block become the logit gradients, in place (binary32:
+// into three planes): times exp(granule's maximum - lse), less one at the
+// label.  There p - 1 comes from the token's binary32 loss, so a token that is
+// nearly certain keeps its small gradient.  Zero rows up to a multiple
+// of kDepth.
+template <class E, class T>
+__global__ __launch_bounds__(kTurnBlock) void gradient_kernel(const int32_t* count, int64_t first, int64_t block, E* scores,
+                                                              int64_t padded, const float2* stats, int granule,
+                                                              const float2* softmax, const float* counted_losses,
+                                                              const int32_t* labels, T* split) {
+    constexpr int kVec = 16 / sizeof(E);
+    const int64_t counted = *count - first, n = counted < block ? counted : block;
+    if (n <= 0) return;
+    const int64_t rows = (n + kDepth - 1) / kDepth * kDepth, plane = block * padded;
+    const int64_t v = (static_cast<int64_t>(blockIdx.x) * kTurnBlock + threadIdx.x) * kVec;
+    if (v >= padded) return;
+    const int64_t g = v / granule;
+    for (int64_t token = static_cast<int64_t>(blockIdx.y) * kTurnRows; token < rows;
+         token += static_cast<int64_t>(gridDim.y) * kTurnRows)
+#pragma unroll 4
+        for (int u = 0; u < kTurnRows; ++u) {
+            const int64_t t = token + u;
+            if (t >= rows) break;
+            E* at = scores + t * padded + v;
+            float x[kVec] = {};
+            if (t < n) {
+                load_floats<E, kVec>(at, x);
+                const float2 of = softmax[t];
+                const float factor = of.y * __builtin_amdgcn_exp2f((stats[g * block + t].x - of.x) * kLog2e);
+                const int64_t label = labels[first + t] - v;
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) x[j] *= factor;
+                if (label >= 0 && label < kVec) {
+                    const float p = kHeldUnit<E> * expm1f(-counted_losses[first + t]);
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j)
+                        if (label == j) x[j] = p;
+                }
+            }
+            if constexpr (sizeof(E) == 4) {
+                Pack<T, kVec> p[kSplitPlanes];
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) split3(x[j], p[0].v[j], p[1].v[j], p[2].v[j]);
+#pragma unroll
+                for (int q = 0; q < kSplitPlanes; ++q)
+                    *reinterpret_cast<Pack<T, kVec>*>(split + q * plane + t * padded + v) = p[q];
+            } else {
+                store_floats<E, kVec>(at, x);
+            }
+        }
+}
+
+// ---------------------------------------------------------------------------
+// the gradients: the second and third product
+// ---------------------------------------------------------------------------
+
+struct GradientOut {
+    const int32_t* count;
+    int64_t first, block;      // of the token block
+    bool table;                // dtable (b: vocabulary, k: tokens), else dhidden (b: tokens, k: vocabulary)
+    int64_t vocab;
+    int32_t dim;
+    const int32_t* rows;
+    float scale;
+    bool mean;
+    float unit;                // kHeldUnit
+    void* to;                  // output rows
+    int64_t stride;
+    bool accumulate;
+    float* partials;
+    int64_t partial_tiles;
+    float* carried;
+    int grid;                  // workgroups, by which the sum is split
+};
+
+struct GradientPlan {
+    int64_t n;          // tokens of the block
+    int64_t tiles_a, tiles_b, blocks, splits;
+    bool last;          // no token block after this one
+};
+
+// The same on every workgroup of the product and of its join: how many parts
+// the summed axis is cut into, so that a product of few tiles fills the device.
+template <class S>
+__device__ GradientPlan gradient_plan(const GradientOut& o) {
+    GradientPlan p;
+    const int64_t counted = *o.count - o.first;
+    p.n = counted < 0 ? 0 : counted < o.block ? counted : o.block;
+    p.last = counted <= o.block;
+    const int64_t columns = o.table ? o.vocab : p.n;
+    p.tiles_a = (o.dim + S::kA - 1) / S::kA;
+    p.tiles_b = (columns + S::kB - 1) / S::kB;
+    p.blocks = ((o.table ? p.n : o.vocab) + kDepth - 1) / kDepth;
+    const int64_t tiles = p.tiles_a * p.tiles_b;
+    p.splits = 1;
+    if (tiles > 0 && tiles < o.grid) {
+        int64_t most = o.grid / tiles;
+        if (most > p.blocks / 8) most = p.blocks / 8;
+        if (most * tiles * S::kA * S::kB > o.partial_tiles * kWideTile) most = o.partial_tiles * kWideTile / (tiles * S::kA * S::kB);
+        if (most > 1) p.splits = most;
+    }
+    return p;
+}
+
+// A token block with nothing counted leaves the table's gradient to the block
+// before it; the first block always writes.
+__device__ __forceinline__ bool nothing_to_do(const GradientOut& o, const GradientPlan& p) {
+    return p.n == 0 && (!o.table || o.first > 0);
+}
+
+template <class S>
+__device__ float4* tile_at(float* tiles, int64_t index) {
+    return reinterpret_cast<float4*>(tiles + index * (S::kA * S::kB)) + threadIdx.x;
+}
+
+template <class S>
+__device__ void store_tile(float4* to, const Acc (&acc)[S::kTilesA][S::kTilesB]) {
+#pragma unroll
+    for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kTilesB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                to[((i * S::kTilesB + j) * 4 + q) * S::kThreads] =
+                    make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+}
+
+template <class S>
+__device__ void add_tile(const float4* from, Acc (&acc)[S::kTilesA][S::kTilesB]) {
+#pragma unroll
+    for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kTilesB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 x = from[((i * S::kTilesB + j) * 4 + q) * S::kThreads];
+                acc[i][j][4 * q] += x.x;
+                acc[i][j][4 * q + 1] += x.y;
+                acc[i][j][4 * q + 2] += x.z;
+                acc[i][j][4 * q + 3] += x.w;
+            }
+}
+
+// A finished tile: into the carried sums while token blocks follow, else
+// scaled and rounded into the output.
+template <class S, class Out>
+__device__ void finish(const GradientOut& o, const GradientPlan& p, int64_t ta, int64_t tb, Acc (&acc)[S::kTilesA][S::kTilesB]) {
+    if (o.table && o.first > 0) add_tile<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), acc);
+    if (o.table && !p.last) {
+        store_tile<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), acc);
+        return;
+    }
+    const int32_t all = *o.count;
+    const float factor = (o.mean ? (all > 0 ? o.scale / static_cast<float>(all) : 0.0f) : o.scale) / o.unit;
+    const Place<S> place;
+    const int64_t columns = o.table ? o.vocab : p.n;
+#pragma unroll
+    for (int j = 0; j < S::kTilesB; ++j) {
+        const int64_t b = tb * S::kB + place.column(j);
+        if (b >= columns) continue;
+        Out* row = static_cast<Out*>(o.to) + (o.table ? b : o.rows[o.first + b]) * o.stride;
+#pragma unroll
+        for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t a = ta * S::kA + place.row(i, q);
+                float x[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = factor * acc[i][j][4 * q + r];
+                if (a + 4 <= o.dim) {
+                    if (o.accumulate) {
+                        float old[4];
+                        load_floats<Out, 4>(row + a, old);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[r] += old[r];
+                    }
+                    store_floats<Out, 4>(row + a, x);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (a + r < o.dim)
+                            row[a + r] = rounded<Out>(o.accumulate ? static_cast<float>(row[a + r]) + x[r] : x[r]);
+                }
+            }
+    }
+}
+
+// kTable: dtable^T = h^T g, else dhidden^T = W^T g^T.  a is always the width,
+// so a lane's values are adjacent in an output row.
+template <class S, class T, class Out, int kTerms, bool kTable>
+__global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Operand g, GradientOut o) {
+    __shared__ __attribute__((aligned(1024))) char stage0[(S::kA + S::kB) * kDepth * 2];
+    __shared__ __attribute__((aligned(1024))) char stage1[(S::kA + S::kB) * kDepth * 2];
+    const GradientPlan p = gradient_plan<S>(o);
+    if (nothing_to_do(o, p)) return;
+    if (kTable) {
+        wide.depth = g.depth = p.blocks * kDepth;  // zero rows behind the last token
+    } else {
+        g.kept = p.n;
+    }
+    TileOrder order(p.tiles_a, p.tiles_b, p.splits);
+    const int64_t steps = kTerms * p.blocks;
+    int64_t ta, tb, split;
+    while (order.next(&ta, &tb, &split)) {
+        Acc acc[S::kTilesA][S::kTilesB];
+        clear<S>(acc);
+        product<S, T, kTerms, true, kTable>(wide, ta * S::kA, g, tb * S::kB, p.blocks, steps * split / p.splits,
+                                    steps * (split + 1) / p.splits, stage0, stage1, acc);
+        if (p.splits == 1)
+            finish<S, Out>(o, p, ta, tb, acc);
+        else
+            store_tile<S>(tile_at<S>(o.partials, (split * p.tiles_b + tb) * p.tiles_a + ta), acc);
+    }
+}
+
+// Adds the parts of a split product, in their order.
+template <class S, class Out>
+__global__ __launch_bounds__(S::kThreads) void join_parts_kernel(GradientOut o) {
+    const GradientPlan p = gradient_plan<S>(o);
+    if (nothing_to_do(o, p) || p.splits == 1) return;
+    for (int64_t t = blockIdx.x; t < p.tiles_a * p.tiles_b; t += gridDim.x) {
+        Acc acc[S::kTilesA][S::kTilesB];
+        clear<S>(acc);
+        for (int64_t s = 0; s < p.splits; ++s)
+            add_tile<S>(tile_at<S>(o.partials, s * p.tiles_a * p.tiles_b + t), acc);
+        finish<S, Out>(o, p, t % p.tiles_a, t / p.tiles_a, acc);
+    }
+}
+
+constexpr int kTotalBlock = 1024;
+
+// The sum or mean of the losses, in binary64 and a fixed order.
+__global__ __launch_bounds__(kTotalBlock) void total_kernel(const int32_t* count, const float* losses, bool mean, const float* all,
+                                                            int64_t tokens, TokenIds targets, int64_t ignored, int64_t vocab,
+                                                            float* loss) {
+    __shared__ double waves[kTotalBlock / 64];
+    const int64_t n = *count;
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += kTotalBlock) sum += static_cast<double>(losses[i]);
+    // a target outside the vocabulary makes the loss NaN
+    for (int64_t i = threadIdx.x; i < tokens; i += kTotalBlock) {
+        const int64_t y = target_of(targets, i);
+        if (y != ignored && (y < 0 || y >= vocab)) sum = all[i];
+    }
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = 0.0;
+    for (int w = 0; w < kTotalBlock / 64; ++w) sum += waves[w];
+    *loss = static_cast<float>(mean && n > 0 ? sum / static_cast<double>(n) : sum);
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+
+uint32_t ceil_div(int64_t a, int64_t b) { return static_cast<uint32_t>((a + b - 1) / b); }
+
+template <class S>
+int product_grid(const LossCall& c) {
+    return c.compute_units * S::kPerUnit / TileOrder::kDies * TileOrder::kDies;
+}
+
+// In: the tensors' type; T: the products'; E: the exponentials'; S: the tiles.
+template <class In, class T, class E, int kTerms, class S>
+hipError_t run(const LossCall& c, hipStream_t stream) {
+    constexpr bool kSplit = sizeof(In) == 4;
+    const int64_t rows_h = (std::max<int64_t>(c.tokens, 1) + kDepth - 1) / kDepth * kDepth;
+    hipLaunchKernelGGL(select_kernel, dim3(1), dim3(kSelectBlock), 0, stream, c.targets, c.tokens, c.ignored, c.vocab, c.count,
+                       c.rows, c.labels, c.losses);
+    hipLaunchKernelGGL((gather_kernel<In, T>), dim3(static_cast<uint32_t>(rows_h)), dim3(kRowBlock), 0, stream,
+                       static_cast<const In*>(c.hidden.at), c.hidden.stride, c.tokens, c.dim, c.count, c.rows,
+                       static_cast<T*>(c.h), c.dim_padded, rows_h * c.dim_padded, c.targets, c.ignored, c.vocab,
+                       c.gradients ? static_cast<In*>(c.dhidden.at) : nullptr, c.dhidden.stride);
+    Operand table{c.table.at, c.table.stride, c.vocab, 0, 0};
+    if (!table_in_place(c)) {
+        table = {c.w, c.dim_padded, c.vocab, 0, c.vocab * c.dim_padded};
+        hipLaunchKernelGGL((table_kernel<In, T>), dim3(static_cast<uint32_t>(c.vocab)), dim3(kRowBlock), 0, stream,
+                           static_cast<const In*>(c.table.at), c.table.stride, c.dim, static_cast<T*>(c.w), c.dim_padded,
+                           table.plane);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int granule = S::kTilesA * 32;
+    // a call of few tokens has more granules, and room for them in a shorter block
+    const int64_t block = S::kB < Wide::kB ? kFewTokens : c.block;
+    const int64_t granules = (c.vocab + S::kA - 1) / S::kA * S::kWavesA;
+    const int grid = product_grid<S>(c);
+    for (int64_t first = 0; first < c.tokens || first == 0; first += block) {
+        const int64_t most = std::max<int64_t>(std::min(c.tokens - first, block), 1);
+        const Operand h{static_cast<const T*>(c.h) + first * c.dim_padded, c.dim_padded, 0, 0, rows_h * c.dim_padded};
+        hipLaunchKernelGGL((scores_kernel<S, T, E, kTerms>), dim3(grid), dim3(S::kThreads), 0, stream, table, h,
+                           int64_t(c.dim_padded / kDepth),
+                           ScoreOut{c.count, c.labels, first, block, c.vocab, c.vocab_padded, c.stats, c.label_logit,
+                                    c.gradients ? c.scores : nullptr});
+        hipLaunchKernelGGL(softmax_kernel, dim3(ceil_div(most, kJoinTokens)), dim3(kJoinTokens * kJoinSlices), 0, stream,
+                           c.count, first, block, c.stats, granules, c.label_logit, c.rows, c.softmax, c.counted_losses,
+                           c.losses);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (!c.gradients) continue;
+        const uint32_t turns = ceil_div(c.vocab_padded, kTurnBlock * (16 / int(sizeof(E))));
+        const uint32_t turn_rows = ceil_div((most + kDepth - 1) / kDepth * kDepth, kTurnRows);
+        hipLaunchKernelGGL((gradient_kernel<E, T>), dim3(turns, turn_rows), dim3(kTurnBlock), 0, stream, c.count, first,
+                           block, static_cast<E*>(c.scores), c.vocab_padded, c.stats, granule, c.softmax, c.counted_losses,
+                           c.labels, static_cast<T*>(c.split));
+        // g as the operand of both products
+        Operand g{kSplit ? c.split : c.scores, c.vocab_padded, 0, 0, block * c.vocab_padded};
+        GradientOut o{c.count, first, block, false, c.vocab, c.dim, c.rows, c.scale, c.mean, kHeldUnit<T>,
+                      c.dhidden.at, c.dhidden.stride, false, c.partials, c.partial_tiles, c.carried, grid};
+        Operand wide{table.at, table.stride, c.dim_padded, c.vocab, table.plane};
+        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o);
+        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o);
+        o.table = true;
+        o.to = c.dtable.at;
+        o.stride = c.dtable.stride;
+        o.accumulate = c.accumulate;
+        wide = {h.at, h.stride, c.dim_padded, 0, h.plane};
+        g.kept = c.vocab_padded;
+        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, true>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o);
+        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kTotalBlock), 0, stream, c.count, c.counted_losses, c.mean, c.losses,
+                       c.tokens, c.targets, c.ignored, c.vocab, c.loss);
+    return hipGetLastError();
+}
+
+template <class In, class T, class E, int kTerms>
+hipError_t pick(const LossCall& c, hipStream_t stream) {
+    if (c.tokens <= 32) return run<In, T, E, kTerms, Narrow32>(c, stream);
+    if (c.tokens <= kFewTokens) return run<In, T, E, kTerms, Narrow64>(c, stream);
+    return run<In, T, E, kTerms, Wide>(c, stream);
+}
+
+}  // namespace
+
+// 16-byte loads of whole steps of kDepth values.
+bool table_in_place(const LossCall& c) {
+    return c.type != MICRO_TYPE_F32 && c.dim % kDepth == 0 && c.table.stride % 8 == 0 &&
+           reinterpret_cast<uintptr_t>(c.table.at) % 16 == 0 && c.table.stride < (int64_t(1) << 22);
+}
+
+hipError_t launch_loss(const LossCall& c, hipStream_t stream) {
+    if (c.type == MICRO_TYPE_F32) return pick<float, bf16, float, 6>(c, stream);
+    if (c.type == MICRO_TYPE_F16) return pick<f16, f16, f16, 1>(c, stream);
+    return pick<bf16, bf16, bf16, 1>(c, stream);
+}
+
+}  // namespace micro

@@ -17,6 +17,7 @@
 #include <new>
 #include <string>
 
+#include "host_util.h"
 #include "sparsify_kernel.h"
 #include "static_scratch.h"
 #include "topk_kernel.h"
@@ -146,6 +147,19 @@ void set_error(micro_ctx* ctx, const char* fmt, ...) {
     else
         g_init_error = buf;
 }
+
+}  // namespace
+
+void micro::set_thread_error(const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    std::vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    g_init_error = buf;
+}
+
+namespace {
 
 micro_status hip_fail(micro_ctx* ctx, hipError_t err, const char* what) {
     set_error(ctx, "%s failed: %s", what, hipGetErrorString(err));
