@@ -50,8 +50,7 @@ struct LossCall {
     float2* softmax;         // (maximum, 1 / sum of exponentials) of [B]
     void* scores;            // exponentials, then logit gradients, [B][Vp]; binary32: floats
     void* split;             // binary32: the logit gradients as [P][B][Vp] bfloat16
-    float* partials;         // tiles of products that are split along the summed axis
-    int64_t partial_tiles;   // wide tiles it holds
+    float* partials;         // a wide tile per compute unit: parts of products cut along the summed axis
     float* carried;          // wide tiles of dtable between token blocks; null with one block
     int compute_units;
 };

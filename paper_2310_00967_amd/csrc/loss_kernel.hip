@@ -35,6 +35,8 @@ using Vec4 = T __attribute__((ext_vector_type(4)));
 using Acc = float __attribute__((ext_vector_type(16)));
 
 #define MICRO_SHARED __attribute__((address_space(3)))
+// The last word of a raw buffer's descriptor: untyped, 32-bit elements.
+constexpr int kRawBuffer = 0x00027000;
 
 __device__ __forceinline__ Acc mma(Vec8<bf16> a, Vec8<bf16> b, Acc c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -43,7 +45,7 @@ __device__ __forceinline__ Acc mma(Vec8<f16> a, Vec8<f16> b, Acc c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 template <class T>
-__device__ __forceinline__ Vec4<T> read_transposed(const T* p) {
+__device__ __forceinline__ Vec4<T> read_transposed(MICRO_SHARED char* p) {
     return __builtin_bit_cast(Vec4<T>, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MICRO_SHARED Vec4<short>*)p));
 }
 
@@ -84,56 +86,65 @@ template <class T, int kR, bool kTurned, int kThreads>
 struct Stage {
     static constexpr int kLoads = kR * kDepth / 8 / kThreads;
     static_assert(kLoads * kThreads * 8 == kR * kDepth, "a tile is a whole number of loads");
-    uint32_t offset[kLoads];  // bytes from the tile's first value
+    static constexpr int kRowUnits = kTurned ? kR / 8 : kDepth / 8;
+    static constexpr uint32_t kRowsPerLoad = kThreads / kRowUnits;
+    // a thread's unit has the same place in each of its rows
+    static_assert(kThreads % kRowUnits == 0 && kRowsPerLoad % 16 == 0, "rows of a load");
 
     // The four rows of k that a group of lanes reads together lie 2 kR bytes
     // apart; what to permute a turned row's pairs by so that they do not meet
     // in the same 256 bytes of banks.
-    static constexpr uint32_t swizzle(uint32_t k) { return kR >= 128 ? (k & 3) * 2 : kR == 64 ? (k & 2) : 0; }
+    static constexpr __device__ uint32_t swizzle(uint32_t k) { return kR >= 128 ? (k & 3) * 2 : kR == 64 ? (k & 2) : 0; }
 
-    // What this thread loads of the tile at `first` of the kept axis.  depth:
-    // valid rows of k from the tile's first.
-    __device__ void place(const Operand& op, int64_t first, int64_t depth) {
+    uint32_t row, unit;     // this thread's first row, and the bytes of its unit in a row
+    uint32_t stride, last;  // bytes between rows; straight: the last valid row
+
+    __device__ void place(const Operand& op, int64_t first) {
         const uint32_t kept = static_cast<uint32_t>(op.kept - first < kR ? op.kept - first : kR);
+        row = threadIdx.x / kRowUnits;
+        uint32_t u = threadIdx.x % kRowUnits;
+        if constexpr (kTurned) {
+            u ^= swizzle(row) * 2;
+            u = u * 8 + 8 <= kept ? u : kept / 8 - 1;
+        } else {
+            u ^= (row >> 1) & 7;
+        }
+        unit = u * 16;
+        stride = static_cast<uint32_t>(op.stride * sizeof(T));
+        last = kept - 1;
+    }
+
+    // last_row: of this step.  Rows behind it are read from it: what they are
+    // multiplied with is zero (k), or the result is not used (the kept axis).
+    // Both factors have at most 24 bits.
+    __device__ __forceinline__ void load(const char* from, MICRO_SHARED char* to, uint32_t last_row) const {
+        const __amdgpu_buffer_rsrc_t rows =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, -1, kRawBuffer);
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const uint32_t unit = i * kThreads + threadIdx.x;
-            if constexpr (kTurned) {
-                uint32_t k = unit / (kR / 8), c = unit % (kR / 8) ^ swizzle(k) * 2;
-                c = c * 8 + 8 <= kept ? c * 8 : kept - 8;
-                k = k < depth ? k : static_cast<uint32_t>(depth - 1);
-                offset[i] = (k * static_cast<uint32_t>(op.stride) + c) * sizeof(T);
-            } else {
-                uint32_t row = unit / 8;
-                const uint32_t c = (unit % 8) ^ ((row >> 1) & 7);
-                row = row < kept ? row : kept - 1;
-                offset[i] = (row * static_cast<uint32_t>(op.stride) + c * 8) * sizeof(T);
-            }
+            const uint32_t r = row + i * kRowsPerLoad;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, to + (i * kThreads + wave * 64) * 16, 16,
+                                                     __umul24(r < last_row ? r : last_row, stride) + unit, 0, 0, 0);
         }
     }
 
-    __device__ __forceinline__ void load(const char* from, char* to) const {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void*)(from + offset[i]),
-                (MICRO_SHARED void*)(to + (i * kThreads + (threadIdx.x & ~63u)) * 16), 16, 0, 0);
-    }
-
-    // Values [base, base + 32) of the kept axis by k [kk * 16, + 16): lane l
-    // holds value l % 32 and the eight k from 8 * (l / 32).
-    static __device__ __forceinline__ Vec8<T> fragment(const char* tile, int base, int kk) {
+    // Of the tile `tile` bytes into a stage: values [base, base + 32) of the kept
+    // axis by k [kk * 16, + 16).  Lane l holds value l % 32 and the eight k from
+    // 8 * (l / 32).  (One offset from the stage: through a chain of them the
+    // compiler loses sight of which stage is read, and waits for the other's loads.)
+    static __device__ __forceinline__ Vec8<T> fragment(MICRO_SHARED char* stage, int tile, int base, int kk) {
         const int lane = threadIdx.x & 63;
         if constexpr (kTurned) {
             // four k by 16 values transposed by each group of 16 lanes, twice
             const int k = kk * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
             const int pair = (base >> 4) + ((lane >> 4) & 1);
-            const T* row = reinterpret_cast<const T*>(tile) + k * kR + ((pair ^ swizzle(k)) * 16) + (lane & 3) * 4;
-            const Vec4<T> lo = read_transposed(row), hi = read_transposed(row + 4 * kR);
+            const int at = tile + (k * kR + (pair ^ swizzle(k)) * 16 + (lane & 3) * 4) * int(sizeof(T));
+            const Vec4<T> lo = read_transposed<T>(stage + at), hi = read_transposed<T>(stage + (at + 4 * kR * int(sizeof(T))));
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         } else {
-            const int row = base + (lane & 31), c = kk * 2 + (lane >> 5);
-            return *reinterpret_cast<const Vec8<T>*>(tile + row * (kDepth * 2) + ((c ^ ((row >> 1) & 7)) * 16));
+            const int r = base + (lane & 31), c = kk * 2 + (lane >> 5);
+            return *(MICRO_SHARED Vec8<T>*)(stage + (tile + r * (kDepth * 2) + (c ^ ((r >> 1) & 7)) * 16));
         }
     }
 };
@@ -146,15 +157,17 @@ constexpr uint32_t kPlanesA = 0x201100, kPlanesB = 0x021010;
 // blocks of k of term pair s / blocks.  Two stages of shared memory: while the
 // matrix cores work on one, the loads of the next step fill the other.
 template <class S, class T, int kTerms, bool kTurnA, bool kTurnB>
-__device__ void product(const Operand& A, int64_t a, const Operand& B, int64_t b, int64_t blocks, int64_t step,
-                        int64_t end, char* stage0, char* stage1, Acc (&acc)[S::kTilesA][S::kTilesB]) {
+__device__ __forceinline__ void product(const Operand& A, int64_t a, const Operand& B, int64_t b, int64_t blocks,
+                                        int64_t step, int64_t end, MICRO_SHARED char* stage0, MICRO_SHARED char* stage1,
+                                        Acc (&acc)[S::kTilesA][S::kTilesB]) {
     using StageA = Stage<T, S::kA, kTurnA, S::kThreads>;
     using StageB = Stage<T, S::kB, kTurnB, S::kThreads>;
     constexpr int kSecond = S::kA * kDepth * 2;
+    if (step >= end) return;
     StageA sa;
     StageB sb;
-    sa.place(A, a, kDepth);
-    sb.place(B, b, kDepth);
+    sa.place(A, a);
+    sb.place(B, b);
     const char* at_a = static_cast<const char*>(A.at) + (kTurnA ? a : a * A.stride) * int64_t(sizeof(T));
     const char* at_b = static_cast<const char*>(B.at) + (kTurnB ? b : b * B.stride) * int64_t(sizeof(T));
     const int64_t step_a = (kTurnA ? A.stride * kDepth : kDepth) * int64_t(sizeof(T));
@@ -162,57 +175,82 @@ __device__ void product(const Operand& A, int64_t a, const Operand& B, int64_t b
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_a = wave / S::kWavesB * (S::kTilesA * 32), wave_b = wave % S::kWavesB * (S::kTilesB * 32);
 
-    const auto load = [&](int64_t s, char* stage) {
+    const auto last_of = [](int64_t depth, int64_t k) {
+        const int64_t left = depth - k * kDepth;
+        return static_cast<uint32_t>(left < kDepth ? left : kDepth) - 1;
+    };
+    const auto load = [&](int64_t s, MICRO_SHARED char* stage) {
         const int term = kTerms == 1 ? 0 : static_cast<int>(s / blocks);
         const int64_t k = s - term * blocks;
         const char* from_a = at_a + (kPlanesA >> 4 * term & 15) * A.plane * int64_t(sizeof(T)) + k * step_a;
         const char* from_b = at_b + (kPlanesB >> 4 * term & 15) * B.plane * int64_t(sizeof(T)) + k * step_b;
-        if (kTurnA && (k + 1) * kDepth > A.depth) {
-            StageA tail;
-            tail.place(A, a, A.depth - k * kDepth);
-            tail.load(from_a, stage);
-        } else {
-            sa.load(from_a, stage);
-        }
-        if (kTurnB && (k + 1) * kDepth > B.depth) {
-            StageB tail;
-            tail.place(B, b, B.depth - k * kDepth);
-            tail.load(from_b, stage + kSecond);
-        } else {
-            sb.load(from_b, stage + kSecond);
-        }
+        sa.load(from_a, stage, kTurnA ? last_of(A.depth, k) : sa.last);
+        sb.load(from_b, stage + kSecond, kTurnB ? last_of(B.depth, k) : sb.last);
     };
-    const auto compute = [&](const char* stage) {
+    // The fragments of 16 k, read while the matrix cores work on the 16 before.
+    struct Fragments {
+        Vec8<T> a[S::kTilesA], b[S::kTilesB];
+    };
+    const auto read = [&](MICRO_SHARED char* stage, int kk, Fragments& f) {
 #pragma unroll
-        for (int kk = 0; kk < kDepth / 16; ++kk) {
-            Vec8<T> fa[S::kTilesA], fb[S::kTilesB];
+        for (int j = 0; j < S::kTilesB; ++j) f.b[j] = StageB::fragment(stage, kSecond, wave_b + j * 32, kk);
 #pragma unroll
-            for (int i = 0; i < S::kTilesA; ++i) fa[i] = StageA::fragment(stage, wave_a + i * 32, kk);
+        for (int i = 0; i < S::kTilesA; ++i) f.a[i] = StageA::fragment(stage, 0, wave_a + i * 32, kk);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto multiply = [&](const Fragments& f) {
 #pragma unroll
-            for (int j = 0; j < S::kTilesB; ++j) fb[j] = StageB::fragment(stage + kSecond, wave_b + j * 32, kk);
+        for (int i = 0; i < S::kTilesA; ++i)
 #pragma unroll
-            for (int i = 0; i < S::kTilesA; ++i)
-#pragma unroll
-                for (int j = 0; j < S::kTilesB; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
-        }
+            for (int j = 0; j < S::kTilesB; ++j) acc[i][j] = mma(f.a[i], f.b[j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
     };
     const auto arrived = [] {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
-
-    __syncthreads();  // the stages are free
-    if (step < end) load(step, stage0);
-    while (step < end) {
+    static_assert(kDepth == 64, "four fragments a step");
+    Fragments even, odd;
+    // All of a step but its last product.
+    const auto work = [&](MICRO_SHARED char* stage) {
+        read(stage, 1, odd);
+        multiply(even);
+        read(stage, 2, even);
+        multiply(odd);
+        read(stage, 3, odd);
+        multiply(even);
+    };
+    int64_t left = end - step;
+    const int64_t last = end - 1;
+    load(step, stage0);
+    arrived();
+    load(step + 1 < last ? step + 1 : last, stage1);
+    read(stage0, 0, even);
+    // A step's last fragments are in registers before the barrier, so behind it
+    // the loads of the step after next may overwrite its stage, and the next
+    // step's first fragments are read, both under the step's last product.  A
+    // load past the end reads the last step again.
+    for (; left > 2; left -= 2, step += 2) {
+        work(stage0);
         arrived();
-        if (step + 1 < end) load(step + 1, stage1);
-        compute(stage0);
-        if (++step >= end) break;
+        load(step + 2, stage0);
+        read(stage1, 0, even);
+        multiply(odd);
+        work(stage1);
         arrived();
-        if (step + 1 < end) load(step + 1, stage0);
-        compute(stage1);
-        ++step;
+        load(step + 3 < last ? step + 3 : last, stage1);
+        read(stage0, 0, even);
+        multiply(odd);
     }
+    work(stage0);
+    if (left == 2) {
+        arrived();
+        read(stage1, 0, even);
+        multiply(odd);
+        work(stage1);
+    }
+    multiply(odd);
+    arrived();  // the stages are free
 }
 
 template <class S>
@@ -238,30 +276,46 @@ struct Place {
     __device__ int column(int j) const { return b + j * 32; }
 };
 
-// Tiles of C for a grid of workgroups that each take several.  Workgroups go
-// to the eight dies in turn, and each die has its own L2: a die takes a run of
-// neighbouring tiles, ordered so that those in flight at once (four along a by
-// the rest along b) share their operands.
+// The tiles of C for a grid of workgroups that each take several, in rounds of
+// one tile a workgroup.  The tiles behind the last full round are cut into
+// `splits` parts of the summed axis, so that they too keep the grid busy.
+// Workgroups go to the eight dies in turn, and each die has its own L2: a die
+// takes a run of neighbouring tiles, ordered so that those in flight at once
+// (four along a by the rest along b) share their operands.
 struct TileOrder {
-    int64_t tiles_a, tiles_b, splits;
-    int64_t per_die, at, stride;
     static constexpr int kDies = 8, kGroup = 4;
-    __device__ TileOrder(int64_t ta, int64_t tb, int64_t s) : tiles_a(ta), tiles_b(tb), splits(s) {
-        const int64_t total = ta * tb * s;
-        per_die = (total + kDies - 1) / kDies;
-        at = blockIdx.x / kDies;
-        stride = gridDim.x / kDies;
+    int64_t tiles_a, tiles_b, full, tail, splits, round = 0;
+    __device__ TileOrder(int64_t ta, int64_t tb, int64_t most_splits) : tiles_a(ta), tiles_b(tb) {
+        const int64_t tiles = ta * tb, grid = gridDim.x;
+        full = tiles / grid * grid;
+        tail = tiles - full;
+        splits = 1;
+        if (tail > 0 && most_splits > 1) splits = grid / tail < most_splits ? grid / tail : most_splits;
     }
-    __device__ bool next(int64_t* a, int64_t* b, int64_t* split) {
-        const int64_t linear = (blockIdx.x % kDies) * per_die + at;
-        if (at >= per_die || linear >= tiles_a * tiles_b * splits) return false;
-        at += stride;
-        *split = linear / (tiles_a * tiles_b);
-        const int64_t in = linear % (tiles_a * tiles_b), group = in / (kGroup * tiles_b);
-        const int64_t rest = in % (kGroup * tiles_b);
+    __device__ void place(int64_t linear, int64_t* a, int64_t* b) const {
+        const int64_t group = linear / (kGroup * tiles_b), rest = linear - group * (kGroup * tiles_b);
         const int64_t width = tiles_a - group * kGroup < kGroup ? tiles_a - group * kGroup : kGroup;
-        *a = group * kGroup + rest % width;
         *b = rest / width;
+        *a = group * kGroup + (rest - *b * width);
+    }
+    // part: -1 for a whole tile, else its part of the sum; index: of the part
+    // among all parts.
+    __device__ bool next(int64_t* a, int64_t* b, int64_t* part, int64_t* index) {
+        const int64_t grid = gridDim.x, die = blockIdx.x % kDies, in_die = blockIdx.x / kDies;
+        if (round * grid < full) {
+            place(die * (full / kDies) + in_die + round * (grid / kDies), a, b);
+            *part = -1;
+            ++round;
+            return true;
+        }
+        if (round * grid > full) return false;
+        ++round;
+        const int64_t parts = tail * splits, per_die = (parts + kDies - 1) / kDies;
+        const int64_t at = die * per_die + in_die;
+        if (in_die >= per_die || at >= parts) return false;
+        place(full + at % tail, a, b);
+        *part = splits > 1 ? at / tail : -1;
+        *index = at;
         return true;
     }
 };
@@ -407,35 +461,45 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
     h.kept = n;
     TileOrder order((out.vocab + S::kA - 1) / S::kA, (n + S::kB - 1) / S::kB, 1);
     const Place<S> place;
-    int64_t ta, tb, split;
-    while (order.next(&ta, &tb, &split)) {
+    int64_t ta, tb, part, index;
+    while (order.next(&ta, &tb, &part, &index)) {
         Acc acc[S::kTilesA][S::kTilesB];
         clear<S>(acc);
-        product<S, T, kTerms, false, false>(table, ta * S::kA, h, tb * S::kB, blocks, 0, kTerms * blocks, stage0, stage1, acc);
-#pragma unroll
-        for (int j = 0; j < S::kTilesB; ++j) {
-            const int64_t token = tb * S::kB + place.column(j);
-            const int64_t v0 = ta * S::kA + place.row(0, 0);
-            float most = -__builtin_inff();
+        product<S, T, kTerms, false, false>(table, ta * S::kA, h, tb * S::kB, blocks, 0, kTerms * blocks, (MICRO_SHARED char*)stage0,
+                                            (MICRO_SHARED char*)stage1, acc);
+        const int64_t v0 = ta * S::kA + place.row(0, 0);
+        if ((ta + 1) * S::kA > out.vocab) {  // rows behind the vocabulary
+            const int left = static_cast<int>(out.vocab - v0);
 #pragma unroll
             for (int i = 0; i < S::kTilesA; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    if (v0 + i * 32 + (r >> 2) * 8 + (r & 3) >= out.vocab) acc[i][j][r] = -__builtin_inff();
-                    most = fmaxf(most, acc[i][j][r]);
+                    const bool in = i * 32 + (r >> 2) * 8 + (r & 3) < left;
+#pragma unroll
+                    for (int j = 0; j < S::kTilesB; ++j) acc[i][j][r] = in ? acc[i][j][r] : -__builtin_inff();
                 }
+        }
+#pragma unroll
+        for (int j = 0; j < S::kTilesB; ++j) {
+            const int64_t token = tb * S::kB + place.column(j);
+            const int64_t to_label = token < n ? out.labels[out.first + token] - v0 : -1;
+            const int label = to_label >= 0 && to_label < S::kTilesA * 32 ? static_cast<int>(to_label) : -1;
+            float most = -__builtin_inff(), at_label = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    most = fmaxf(most, acc[i][j][r]);
+                    at_label = label == i * 32 + (r >> 2) * 8 + (r & 3) ? acc[i][j][r] : at_label;
+                }
+            if (label >= 0 && (label & 4) == 0) out.label_logit[token] = at_label;
             most = fmaxf(most, __shfl_xor(most, 32));
-            const int64_t label = token < n ? out.labels[out.first + token] - v0 : -1;
-            if (label >= 0 && label < S::kTilesA * 32 && (label & 4) == 0) {
-#pragma unroll
-                for (int i = 0; i < S::kTilesA; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (label == i * 32 + (r >> 2) * 8 + (r & 3)) out.label_logit[token] = acc[i][j][r];
-            }
             // a granule without a finite maximum keeps its logits' own limits
             const float base = most == -__builtin_inff() ? 0.0f : most;
             float sum = 0.0f;
+            E* row = static_cast<E*>(out.scores) + token * out.padded + v0;
+            const int room = !out.scores || token >= n ? 0
+                             : static_cast<int>(out.padded - v0 < S::kTilesA * 32 ? out.padded - v0 : S::kTilesA * 32);
 #pragma unroll
             for (int i = 0; i < S::kTilesA; ++i)
 #pragma unroll
@@ -447,13 +511,11 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
                         sum += e[r];
                         e[r] *= kHeldUnit<E>;
                     }
-                    const int64_t v = ta * S::kA + place.row(i, q);
-                    if (out.scores && token < n && v < out.padded)
-                        store_floats<E, 4>(static_cast<E*>(out.scores) + token * out.padded + v, e);
+                    if (i * 32 + q * 8 < room) store_floats<E, 4>(row + i * 32 + q * 8, e);
                 }
             sum += __shfl_xor(sum, 32);
             if ((threadIdx.x & 32) == 0 && token < n) {
-                const int64_t granule = (ta * S::kA + place.row(0, 0)) / (S::kTilesA * 32);
+                const int64_t granule = v0 / (S::kTilesA * 32);
                 out.stats[granule * out.block + token] = make_float2(most, sum);
             }
         }
@@ -580,20 +642,18 @@ struct GradientOut {
     void* to;                  // output rows
     int64_t stride;
     bool accumulate;
-    float* partials;
-    int64_t partial_tiles;
+    float* partials;           // one tile a workgroup of the grid
     float* carried;
-    int grid;                  // workgroups, by which the sum is split
 };
 
 struct GradientPlan {
     int64_t n;          // tokens of the block
-    int64_t tiles_a, tiles_b, blocks, splits;
+    int64_t tiles_a, tiles_b, blocks;
+    int64_t most_splits;
     bool last;          // no token block after this one
 };
 
-// The same on every workgroup of the product and of its join: how many parts
-// the summed axis is cut into, so that a product of few tiles fills the device.
+// The same on every workgroup of the product and of its join.
 template <class S>
 __device__ GradientPlan gradient_plan(const GradientOut& o) {
     GradientPlan p;
@@ -604,14 +664,7 @@ __device__ GradientPlan gradient_plan(const GradientOut& o) {
     p.tiles_a = (o.dim + S::kA - 1) / S::kA;
     p.tiles_b = (columns + S::kB - 1) / S::kB;
     p.blocks = ((o.table ? p.n : o.vocab) + kDepth - 1) / kDepth;
-    const int64_t tiles = p.tiles_a * p.tiles_b;
-    p.splits = 1;
-    if (tiles > 0 && tiles < o.grid) {
-        int64_t most = o.grid / tiles;
-        if (most > p.blocks / 8) most = p.blocks / 8;
-        if (most * tiles * S::kA * S::kB > o.partial_tiles * kWideTile) most = o.partial_tiles * kWideTile / (tiles * S::kA * S::kB);
-        if (most > 1) p.splits = most;
-    }
+    p.most_splits = p.blocks / 8;  // a part shorter than that is not worth its partial tile
     return p;
 }
 
@@ -711,32 +764,38 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
     } else {
         g.kept = p.n;
     }
-    TileOrder order(p.tiles_a, p.tiles_b, p.splits);
+    TileOrder order(p.tiles_a, p.tiles_b, p.most_splits);
     const int64_t steps = kTerms * p.blocks;
-    int64_t ta, tb, split;
-    while (order.next(&ta, &tb, &split)) {
+    int64_t ta, tb, part, index;
+    while (order.next(&ta, &tb, &part, &index)) {
         Acc acc[S::kTilesA][S::kTilesB];
         clear<S>(acc);
-        product<S, T, kTerms, true, kTable>(wide, ta * S::kA, g, tb * S::kB, p.blocks, steps * split / p.splits,
-                                    steps * (split + 1) / p.splits, stage0, stage1, acc);
-        if (p.splits == 1)
+        const bool whole = part < 0;
+        product<S, T, kTerms, true, kTable>(wide, ta * S::kA, g, tb * S::kB, p.blocks,
+                                            whole ? 0 : steps * part / order.splits,
+                                            whole ? steps : steps * (part + 1) / order.splits, (MICRO_SHARED char*)stage0,
+                                            (MICRO_SHARED char*)stage1, acc);
+        if (whole)
             finish<S, Out>(o, p, ta, tb, acc);
         else
-            store_tile<S>(tile_at<S>(o.partials, (split * p.tiles_b + tb) * p.tiles_a + ta), acc);
+            store_tile<S>(tile_at<S>(o.partials, index), acc);
     }
 }
 
-// Adds the parts of a split product, in their order.
+// Adds the parts of the tiles that were cut, in their order.
 template <class S, class Out>
 __global__ __launch_bounds__(S::kThreads) void join_parts_kernel(GradientOut o) {
     const GradientPlan p = gradient_plan<S>(o);
-    if (nothing_to_do(o, p) || p.splits == 1) return;
-    for (int64_t t = blockIdx.x; t < p.tiles_a * p.tiles_b; t += gridDim.x) {
+    if (nothing_to_do(o, p)) return;
+    const TileOrder order(p.tiles_a, p.tiles_b, p.most_splits);
+    if (order.splits == 1) return;
+    for (int64_t t = blockIdx.x; t < order.tail; t += gridDim.x) {
         Acc acc[S::kTilesA][S::kTilesB];
         clear<S>(acc);
-        for (int64_t s = 0; s < p.splits; ++s)
-            add_tile<S>(tile_at<S>(o.partials, s * p.tiles_a * p.tiles_b + t), acc);
-        finish<S, Out>(o, p, t % p.tiles_a, t / p.tiles_a, acc);
+        for (int64_t s = 0; s < order.splits; ++s) add_tile<S>(tile_at<S>(o.partials, s * order.tail + t), acc);
+        int64_t ta, tb;
+        order.place(order.full + t, &ta, &tb);
+        finish<S, Out>(o, p, ta, tb, acc);
     }
 }
 
@@ -820,7 +879,7 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         // g as the operand of both products
         Operand g{kSplit ? c.split : c.scores, c.vocab_padded, 0, 0, block * c.vocab_padded};
         GradientOut o{c.count, first, block, false, c.vocab, c.dim, c.rows, c.scale, c.mean, kHeldUnit<T>,
-                      c.dhidden.at, c.dhidden.stride, false, c.partials, c.partial_tiles, c.carried, grid};
+                      c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried};
         Operand wide{table.at, table.stride, c.dim_padded, c.vocab, table.plane};
         hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o);
         hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o);

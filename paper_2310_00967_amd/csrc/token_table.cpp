@@ -153,11 +153,10 @@ micro_status loss_scratch(micro_table* t, bool copy_table, bool gradients) {
                                      [&](Parts& p) { p.take(c.w, planes * t->vocab * dim * 2); }))
             return st;
     if (!gradients) return MICRO_OK;
-    c.partial_tiles = t->compute_units;
     return ensure(&t->gradient_memory, "token loss's gradients", [&](Parts& p) {
         p.take(c.scores, c.block * vocab * (split ? 4 : 2));
         if (split) p.take(c.split, planes * c.block * vocab * 2);
-        p.take(c.partials, c.partial_tiles * kWideTile * 4);
+        p.take(c.partials, t->compute_units * kWideTile * 4);
         if (t->max_tokens > c.block)
             p.take(c.carried, round_up(t->vocab, 256) * round_up(t->dim, 256) * 4);
     });
