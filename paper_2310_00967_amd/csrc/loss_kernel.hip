@@ -129,25 +129,37 @@ struct Stage {
         }
     }
 
-    // Of the tile `tile` bytes into a stage: values [base, base + 32) of the kept
-    // axis by k [kk * 16, + 16).  Lane l holds value l % 32 and the eight k from
-    // 8 * (l / 32).  (One offset from the stage: through a chain of them the
-    // compiler loses sight of which stage is read, and waits for the other's loads.)
-    static __device__ __forceinline__ Vec8<T> fragment(MICRO_SHARED char* stage, int tile, int base, int kk) {
+    // Values [base, base + 32) of the kept axis by k [kk * 16, + 16): lane l
+    // holds value l % 32 and the eight k from 8 * (l / 32).
+    static __device__ __forceinline__ Vec8<T> fragment(MICRO_SHARED char* tile, int base, int kk) {
         const int lane = threadIdx.x & 63;
         if constexpr (kTurned) {
             // four k by 16 values transposed by each group of 16 lanes, twice
             const int k = kk * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
             const int pair = (base >> 4) + ((lane >> 4) & 1);
-            const int at = tile + (k * kR + (pair ^ swizzle(k)) * 16 + (lane & 3) * 4) * int(sizeof(T));
-            const Vec4<T> lo = read_transposed<T>(stage + at), hi = read_transposed<T>(stage + (at + 4 * kR * int(sizeof(T))));
+            const int at = (k * kR + (pair ^ swizzle(k)) * 16 + (lane & 3) * 4) * int(sizeof(T));
+            const Vec4<T> lo = read_transposed<T>(tile + at), hi = read_transposed<T>(tile + (at + 4 * kR * int(sizeof(T))));
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         } else {
             const int r = base + (lane & 31), c = kk * 2 + (lane >> 5);
-            return *(MICRO_SHARED Vec8<T>*)(stage + (tile + r * (kDepth * 2) + (c ^ ((r >> 1) & 7)) * 16));
+            return *(MICRO_SHARED Vec8<T>*)(tile + (r * (kDepth * 2) + (c ^ ((r >> 1) & 7)) * 16));
         }
     }
 };
+
+// The two operands' tiles of a stage.  Each tile of each stage is a variable of
+// its own: that is how the compiler knows that reads of one stage need not wait
+// for the loads into the other.
+struct Tiles {
+    MICRO_SHARED char *a, *b;
+};
+#define MICRO_STAGES(S)                                                        \
+    __shared__ __attribute__((aligned(1024))) char tile_a0[S::kA * kDepth * 2]; \
+    __shared__ __attribute__((aligned(1024))) char tile_b0[S::kB * kDepth * 2]; \
+    __shared__ __attribute__((aligned(1024))) char tile_a1[S::kA * kDepth * 2]; \
+    __shared__ __attribute__((aligned(1024))) char tile_b1[S::kB * kDepth * 2]; \
+    const Tiles stage0{(MICRO_SHARED char*)tile_a0, (MICRO_SHARED char*)tile_b0}; \
+    const Tiles stage1{(MICRO_SHARED char*)tile_a1, (MICRO_SHARED char*)tile_b1}
 
 // The planes of a and b of a split operand's six products, four bits each;
 // the first is that of a plain one.
@@ -158,11 +170,10 @@ constexpr uint32_t kPlanesA = 0x201100, kPlanesB = 0x021010;
 // matrix cores work on one, the loads of the next step fill the other.
 template <class S, class T, int kTerms, bool kTurnA, bool kTurnB>
 __device__ __forceinline__ void product(const Operand& A, int64_t a, const Operand& B, int64_t b, int64_t blocks,
-                                        int64_t step, int64_t end, MICRO_SHARED char* stage0, MICRO_SHARED char* stage1,
+                                        int64_t step, int64_t end, const Tiles& stage0, const Tiles& stage1,
                                         Acc (&acc)[S::kTilesA][S::kTilesB]) {
     using StageA = Stage<T, S::kA, kTurnA, S::kThreads>;
     using StageB = Stage<T, S::kB, kTurnB, S::kThreads>;
-    constexpr int kSecond = S::kA * kDepth * 2;
     if (step >= end) return;
     StageA sa;
     StageB sb;
@@ -179,23 +190,23 @@ __device__ __forceinline__ void product(const Operand& A, int64_t a, const Opera
         const int64_t left = depth - k * kDepth;
         return static_cast<uint32_t>(left < kDepth ? left : kDepth) - 1;
     };
-    const auto load = [&](int64_t s, MICRO_SHARED char* stage) {
+    const auto load = [&](int64_t s, const Tiles& stage) {
         const int term = kTerms == 1 ? 0 : static_cast<int>(s / blocks);
         const int64_t k = s - term * blocks;
         const char* from_a = at_a + (kPlanesA >> 4 * term & 15) * A.plane * int64_t(sizeof(T)) + k * step_a;
         const char* from_b = at_b + (kPlanesB >> 4 * term & 15) * B.plane * int64_t(sizeof(T)) + k * step_b;
-        sa.load(from_a, stage, kTurnA ? last_of(A.depth, k) : sa.last);
-        sb.load(from_b, stage + kSecond, kTurnB ? last_of(B.depth, k) : sb.last);
+        sa.load(from_a, stage.a, kTurnA ? last_of(A.depth, k) : sa.last);
+        sb.load(from_b, stage.b, kTurnB ? last_of(B.depth, k) : sb.last);
     };
     // The fragments of 16 k, read while the matrix cores work on the 16 before.
     struct Fragments {
         Vec8<T> a[S::kTilesA], b[S::kTilesB];
     };
-    const auto read = [&](MICRO_SHARED char* stage, int kk, Fragments& f) {
+    const auto read = [&](const Tiles& stage, int kk, Fragments& f) {
 #pragma unroll
-        for (int j = 0; j < S::kTilesB; ++j) f.b[j] = StageB::fragment(stage, kSecond, wave_b + j * 32, kk);
+        for (int j = 0; j < S::kTilesB; ++j) f.b[j] = StageB::fragment(stage.b, wave_b + j * 32, kk);
 #pragma unroll
-        for (int i = 0; i < S::kTilesA; ++i) f.a[i] = StageA::fragment(stage, 0, wave_a + i * 32, kk);
+        for (int i = 0; i < S::kTilesA; ++i) f.a[i] = StageA::fragment(stage.a, wave_a + i * 32, kk);
         __builtin_amdgcn_sched_barrier(0);
     };
     const auto multiply = [&](const Fragments& f) {
@@ -212,7 +223,7 @@ __device__ __forceinline__ void product(const Operand& A, int64_t a, const Opera
     static_assert(kDepth == 64, "four fragments a step");
     Fragments even, odd;
     // All of a step but its last product.
-    const auto work = [&](MICRO_SHARED char* stage) {
+    const auto work = [&](const Tiles& stage) {
         read(stage, 1, odd);
         multiply(even);
         read(stage, 2, even);
@@ -453,8 +464,7 @@ struct ScoreOut {
 // them without shuffles but the one between its two halves.
 template <class S, class T, class E, int kTerms>
 __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Operand h, int64_t blocks, ScoreOut out) {
-    __shared__ __attribute__((aligned(1024))) char stage0[(S::kA + S::kB) * kDepth * 2];
-    __shared__ __attribute__((aligned(1024))) char stage1[(S::kA + S::kB) * kDepth * 2];
+    MICRO_STAGES(S);
     const int64_t counted = *out.count - out.first;
     const int64_t n = counted < out.block ? counted : out.block;
     if (n <= 0) return;
@@ -465,8 +475,8 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
     while (order.next(&ta, &tb, &part, &index)) {
         Acc acc[S::kTilesA][S::kTilesB];
         clear<S>(acc);
-        product<S, T, kTerms, false, false>(table, ta * S::kA, h, tb * S::kB, blocks, 0, kTerms * blocks, (MICRO_SHARED char*)stage0,
-                                            (MICRO_SHARED char*)stage1, acc);
+        product<S, T, kTerms, false, false>(table, ta * S::kA, h, tb * S::kB, blocks, 0, kTerms * blocks, stage0, stage1,
+                                            acc);
         const int64_t v0 = ta * S::kA + place.row(0, 0);
         if ((ta + 1) * S::kA > out.vocab) {  // rows behind the vocabulary
             const int left = static_cast<int>(out.vocab - v0);
@@ -755,8 +765,7 @@ __device__ void finish(const GradientOut& o, const GradientPlan& p, int64_t ta, 
 // so a lane's values are adjacent in an output row.
 template <class S, class T, class Out, int kTerms, bool kTable>
 __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Operand g, GradientOut o) {
-    __shared__ __attribute__((aligned(1024))) char stage0[(S::kA + S::kB) * kDepth * 2];
-    __shared__ __attribute__((aligned(1024))) char stage1[(S::kA + S::kB) * kDepth * 2];
+    MICRO_STAGES(S);
     const GradientPlan p = gradient_plan<S>(o);
     if (nothing_to_do(o, p)) return;
     if (kTable) {
@@ -773,8 +782,8 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
         const bool whole = part < 0;
         product<S, T, kTerms, true, kTable>(wide, ta * S::kA, g, tb * S::kB, p.blocks,
                                             whole ? 0 : steps * part / order.splits,
-                                            whole ? steps : steps * (part + 1) / order.splits, (MICRO_SHARED char*)stage0,
-                                            (MICRO_SHARED char*)stage1, acc);
+                                            whole ? steps : steps * (part + 1) / order.splits, stage0, stage1,
+                                            acc);
         if (whole)
             finish<S, Out>(o, p, ta, tb, acc);
         else
