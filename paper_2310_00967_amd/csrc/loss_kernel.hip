@@ -147,6 +147,23 @@ struct Stage {
     }
 };
 
+// Orders the instructions since the last such call: reads of shared memory and
+// loads spread between the products, whose 32 cycles each cover their issue.
+template <int kProducts, int kReads, int kLoads, int kAt = 0>
+__device__ __forceinline__ void interleave() {
+    if constexpr (kAt < kProducts) {
+        constexpr int kMma = 0x8, kVectorLoad = 0x20, kSharedRead = 0x100;
+        __builtin_amdgcn_sched_group_barrier(kMma, 1, 0);
+        constexpr int reads = (kAt + 1) * kReads / kProducts - kAt * kReads / kProducts;
+        constexpr int loads = (kAt + 1) * kLoads / kProducts - kAt * kLoads / kProducts;
+        if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(kVectorLoad, loads, 0);
+        if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(kSharedRead, reads, 0);
+        interleave<kProducts, kReads, kLoads, kAt + 1>();
+    } else {
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // The two operands' tiles of a stage.  Each tile of each stage is a variable of
 // its own: that is how the compiler knows that reads of one stage need not wait
 // for the loads into the other.
@@ -207,15 +224,15 @@ __device__ __forceinline__ void product(const Operand& A, int64_t a, const Opera
         for (int j = 0; j < S::kTilesB; ++j) f.b[j] = StageB::fragment(stage.b, wave_b + j * 32, kk);
 #pragma unroll
         for (int i = 0; i < S::kTilesA; ++i) f.a[i] = StageA::fragment(stage.a, wave_a + i * 32, kk);
-        __builtin_amdgcn_sched_barrier(0);
     };
     const auto multiply = [&](const Fragments& f) {
 #pragma unroll
         for (int i = 0; i < S::kTilesA; ++i)
 #pragma unroll
             for (int j = 0; j < S::kTilesB; ++j) acc[i][j] = mma(f.a[i], f.b[j], acc[i][j]);
-        __builtin_amdgcn_sched_barrier(0);
     };
+    constexpr int kReads = (kTurnA ? 2 : 1) * S::kTilesA + (kTurnB ? 2 : 1) * S::kTilesB;
+    constexpr int kProducts = S::kTilesA * S::kTilesB, kLoads = StageA::kLoads + StageB::kLoads;
     const auto arrived = [] {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -226,10 +243,24 @@ __device__ __forceinline__ void product(const Operand& A, int64_t a, const Opera
     const auto work = [&](const Tiles& stage) {
         read(stage, 1, odd);
         multiply(even);
+        interleave<kProducts, kReads, 0>();
         read(stage, 2, even);
         multiply(odd);
+        interleave<kProducts, kReads, 0>();
         read(stage, 3, odd);
         multiply(even);
+        interleave<kProducts, kReads, 0>();
+    };
+    // A step's last fragments are in registers before the barrier, so behind it
+    // the loads of the step after next may overwrite its stage, and the next
+    // step's first fragments are read, both under the step's last product.
+    const auto turn = [&](int64_t to_load, const Tiles& stage, const Tiles& next) {
+        arrived();
+        __builtin_amdgcn_sched_barrier(0);
+        load(to_load, stage);
+        read(next, 0, even);
+        multiply(odd);
+        interleave<kProducts, kReads, kLoads>();
     };
     int64_t left = end - step;
     const int64_t last = end - 1;
@@ -237,21 +268,12 @@ __device__ __forceinline__ void product(const Operand& A, int64_t a, const Opera
     arrived();
     load(step + 1 < last ? step + 1 : last, stage1);
     read(stage0, 0, even);
-    // A step's last fragments are in registers before the barrier, so behind it
-    // the loads of the step after next may overwrite its stage, and the next
-    // step's first fragments are read, both under the step's last product.  A
-    // load past the end reads the last step again.
+    __builtin_amdgcn_sched_barrier(0);
     for (; left > 2; left -= 2, step += 2) {
         work(stage0);
-        arrived();
-        load(step + 2, stage0);
-        read(stage1, 0, even);
-        multiply(odd);
+        turn(step + 2, stage0, stage1);
         work(stage1);
-        arrived();
-        load(step + 3 < last ? step + 3 : last, stage1);
-        read(stage0, 0, even);
-        multiply(odd);
+        turn(step + 3 < last ? step + 3 : last, stage1, stage0);  // past the end: the last step again
     }
     work(stage0);
     if (left == 2) {
