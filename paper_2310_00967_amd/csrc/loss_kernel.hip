@@ -182,109 +182,129 @@ struct Tiles {
 // the first is that of a plain one.
 constexpr uint32_t kPlanesA = 0x201100, kPlanesB = 0x021010;
 
-// acc += the steps [step, end) of the tile at (a, b): step s is block s %
-// blocks of k of term pair s / blocks.  Two stages of shared memory: while the
-// matrix cores work on one, the loads of the next step fill the other.
+// The product of one tile of C after another.  start() begins the loads of a
+// tile's first step; run() is its sum.  In between a workgroup finishes the
+// tile before, from registers.
 template <class S, class T, int kTerms, bool kTurnA, bool kTurnB>
-__device__ __forceinline__ void product(const Operand& A, int64_t a, const Operand& B, int64_t b, int64_t blocks,
-                                        int64_t step, int64_t end, const Tiles& stage0, const Tiles& stage1,
-                                        Acc (&acc)[S::kTilesA][S::kTilesB]) {
+struct Product {
     using StageA = Stage<T, S::kA, kTurnA, S::kThreads>;
     using StageB = Stage<T, S::kB, kTurnB, S::kThreads>;
-    if (step >= end) return;
-    StageA sa;
-    StageB sb;
-    sa.place(A, a);
-    sb.place(B, b);
-    const char* at_a = static_cast<const char*>(A.at) + (kTurnA ? a : a * A.stride) * int64_t(sizeof(T));
-    const char* at_b = static_cast<const char*>(B.at) + (kTurnB ? b : b * B.stride) * int64_t(sizeof(T));
-    const int64_t step_a = (kTurnA ? A.stride * kDepth : kDepth) * int64_t(sizeof(T));
-    const int64_t step_b = (kTurnB ? B.stride * kDepth : kDepth) * int64_t(sizeof(T));
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wave_a = wave / S::kWavesB * (S::kTilesA * 32), wave_b = wave % S::kWavesB * (S::kTilesB * 32);
-
-    const auto last_of = [](int64_t depth, int64_t k) {
-        const int64_t left = depth - k * kDepth;
-        return static_cast<uint32_t>(left < kDepth ? left : kDepth) - 1;
-    };
-    const auto load = [&](int64_t s, const Tiles& stage) {
-        const int term = kTerms == 1 ? 0 : static_cast<int>(s / blocks);
-        const int64_t k = s - term * blocks;
-        const char* from_a = at_a + (kPlanesA >> 4 * term & 15) * A.plane * int64_t(sizeof(T)) + k * step_a;
-        const char* from_b = at_b + (kPlanesB >> 4 * term & 15) * B.plane * int64_t(sizeof(T)) + k * step_b;
-        sa.load(from_a, stage.a, kTurnA ? last_of(A.depth, k) : sa.last);
-        sb.load(from_b, stage.b, kTurnB ? last_of(B.depth, k) : sb.last);
-    };
     // The fragments of 16 k, read while the matrix cores work on the 16 before.
     struct Fragments {
         Vec8<T> a[S::kTilesA], b[S::kTilesB];
     };
-    const auto read = [&](const Tiles& stage, int kk, Fragments& f) {
+    static constexpr int kReads = (kTurnA ? 2 : 1) * S::kTilesA + (kTurnB ? 2 : 1) * S::kTilesB;
+    static constexpr int kProducts = S::kTilesA * S::kTilesB, kLoads = StageA::kLoads + StageB::kLoads;
+    static_assert(kDepth == 64, "four fragments a step");
+
+    const Operand& A;
+    const Operand& B;
+    const int64_t blocks;
+    StageA sa;
+    StageB sb;
+    const char *at_a, *at_b;
+    int64_t step, end;
+
+    __device__ __forceinline__ Product(const Operand& a, const Operand& b, int64_t blocks_of_k)
+        : A(a), B(b), blocks(blocks_of_k) {}
+
+    static __device__ __forceinline__ uint32_t last_row(int64_t depth, int64_t k) {
+        const int64_t left = depth - k * kDepth;
+        return static_cast<uint32_t>(left < kDepth ? left : kDepth) - 1;
+    }
+    // Step s is block s % blocks of k of term pair s / blocks.
+    __device__ __forceinline__ void load(int64_t s, const Tiles& stage) const {
+        const int term = kTerms == 1 ? 0 : static_cast<int>(s / blocks);
+        const int64_t k = s - term * blocks;
+        const int64_t step_a = (kTurnA ? A.stride * kDepth : kDepth), step_b = (kTurnB ? B.stride * kDepth : kDepth);
+        sa.load(at_a + ((kPlanesA >> 4 * term & 15) * A.plane + k * step_a) * int64_t(sizeof(T)), stage.a,
+                kTurnA ? last_row(A.depth, k) : sa.last);
+        sb.load(at_b + ((kPlanesB >> 4 * term & 15) * B.plane + k * step_b) * int64_t(sizeof(T)), stage.b,
+                kTurnB ? last_row(B.depth, k) : sb.last);
+    }
+    static __device__ __forceinline__ void arrived() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    }
+    static __device__ __forceinline__ void read(const Tiles& stage, int kk, Fragments& f) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int a = wave / S::kWavesB * (S::kTilesA * 32), b = wave % S::kWavesB * (S::kTilesB * 32);
 #pragma unroll
-        for (int j = 0; j < S::kTilesB; ++j) f.b[j] = StageB::fragment(stage.b, wave_b + j * 32, kk);
+        for (int j = 0; j < S::kTilesB; ++j) f.b[j] = StageB::fragment(stage.b, b + j * 32, kk);
 #pragma unroll
-        for (int i = 0; i < S::kTilesA; ++i) f.a[i] = StageA::fragment(stage.a, wave_a + i * 32, kk);
-    };
-    const auto multiply = [&](const Fragments& f) {
+        for (int i = 0; i < S::kTilesA; ++i) f.a[i] = StageA::fragment(stage.a, a + i * 32, kk);
+    }
+    static __device__ __forceinline__ void multiply(const Fragments& f, Acc (&acc)[S::kTilesA][S::kTilesB]) {
 #pragma unroll
         for (int i = 0; i < S::kTilesA; ++i)
 #pragma unroll
             for (int j = 0; j < S::kTilesB; ++j) acc[i][j] = mma(f.a[i], f.b[j], acc[i][j]);
-    };
-    constexpr int kReads = (kTurnA ? 2 : 1) * S::kTilesA + (kTurnB ? 2 : 1) * S::kTilesB;
-    constexpr int kProducts = S::kTilesA * S::kTilesB, kLoads = StageA::kLoads + StageB::kLoads;
-    const auto arrived = [] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    static_assert(kDepth == 64, "four fragments a step");
-    Fragments even, odd;
-    // All of a step but its last product.
-    const auto work = [&](const Tiles& stage) {
-        read(stage, 1, odd);
-        multiply(even);
-        interleave<kProducts, kReads, 0>();
-        read(stage, 2, even);
-        multiply(odd);
-        interleave<kProducts, kReads, 0>();
-        read(stage, 3, odd);
-        multiply(even);
-        interleave<kProducts, kReads, 0>();
-    };
-    // A step's last fragments are in registers before the barrier, so behind it
-    // the loads of the step after next may overwrite its stage, and the next
-    // step's first fragments are read, both under the step's last product.
-    const auto turn = [&](int64_t to_load, const Tiles& stage, const Tiles& next) {
+    }
+
+    // The tile at (a, b), steps [first, until).  The stages are free.
+    __device__ __forceinline__ void start(int64_t a, int64_t b, int64_t first, int64_t until, const Tiles& stage0) {
+        step = first;
+        end = until;
+        if (step >= end) return;
+        sa.place(A, a);
+        sb.place(B, b);
+        at_a = static_cast<const char*>(A.at) + (kTurnA ? a : a * A.stride) * int64_t(sizeof(T));
+        at_b = static_cast<const char*>(B.at) + (kTurnB ? b : b * B.stride) * int64_t(sizeof(T));
+        load(step, stage0);
+    }
+
+    // acc += the sum.  Two stages of shared memory: while the matrix cores work
+    // on one, the loads of the next step fill the other.
+    __device__ __forceinline__ void run(Acc (&acc)[S::kTilesA][S::kTilesB], const Tiles& stage0, const Tiles& stage1) {
+        if (step >= end) return;
+        Fragments even, odd;
+        // All of a step but its last product.
+        const auto work = [&](const Tiles& stage) {
+            read(stage, 1, odd);
+            multiply(even, acc);
+            interleave<kProducts, kReads, 0>();
+            read(stage, 2, even);
+            multiply(odd, acc);
+            interleave<kProducts, kReads, 0>();
+            read(stage, 3, odd);
+            multiply(even, acc);
+            interleave<kProducts, kReads, 0>();
+        };
+        // A step's last fragments are in registers before the barrier, so behind
+        // it the loads of the step after next may overwrite its stage, and the
+        // next step's first fragments are read, both under the step's last
+        // product.
+        const auto turn = [&](int64_t to_load, const Tiles& stage, const Tiles& next) {
+            arrived();
+            __builtin_amdgcn_sched_barrier(0);
+            load(to_load, stage);
+            read(next, 0, even);
+            multiply(odd, acc);
+            interleave<kProducts, kReads, kLoads>();
+        };
+        int64_t left = end - step;
+        const int64_t last = end - 1;
         arrived();
+        load(step + 1 < last ? step + 1 : last, stage1);
+        read(stage0, 0, even);
         __builtin_amdgcn_sched_barrier(0);
-        load(to_load, stage);
-        read(next, 0, even);
-        multiply(odd);
-        interleave<kProducts, kReads, kLoads>();
-    };
-    int64_t left = end - step;
-    const int64_t last = end - 1;
-    load(step, stage0);
-    arrived();
-    load(step + 1 < last ? step + 1 : last, stage1);
-    read(stage0, 0, even);
-    __builtin_amdgcn_sched_barrier(0);
-    for (; left > 2; left -= 2, step += 2) {
+        for (; left > 2; left -= 2, step += 2) {
+            work(stage0);
+            turn(step + 2, stage0, stage1);
+            work(stage1);
+            turn(step + 3 < last ? step + 3 : last, stage1, stage0);  // past the end: the last step again
+        }
         work(stage0);
-        turn(step + 2, stage0, stage1);
-        work(stage1);
-        turn(step + 3 < last ? step + 3 : last, stage1, stage0);  // past the end: the last step again
+        if (left == 2) {
+            arrived();
+            read(stage1, 0, even);
+            multiply(odd, acc);
+            work(stage1);
+        }
+        multiply(odd, acc);
+        arrived();  // the stages are free
     }
-    work(stage0);
-    if (left == 2) {
-        arrived();
-        read(stage1, 0, even);
-        multiply(odd);
-        work(stage1);
-    }
-    multiply(odd);
-    arrived();  // the stages are free
-}
+};
 
 template <class S>
 __device__ void clear(Acc (&acc)[S::kTilesA][S::kTilesB]) {
@@ -309,17 +329,61 @@ struct Place {
     __device__ int column(int j) const { return b + j * 32; }
 };
 
+// Eight values of a lane, 4 of one run of 8 and 4 of the next, become 8
+// adjacent ones: the lower half of the wavefront ends up with the first run,
+// the upper with the second.
+template <class V>
+__device__ __forceinline__ void swap_halves(V& first, V& second) {
+    constexpr int kWords = sizeof(V) / 4;
+    using Words = uint32_t __attribute__((ext_vector_type(kWords)));
+    Words x = __builtin_bit_cast(Words, first), y = __builtin_bit_cast(Words, second);
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        const auto both = __builtin_amdgcn_permlane32_swap(x[w], y[w], false, false);
+        x[w] = both[0];
+        y[w] = both[1];
+    }
+    first = __builtin_bit_cast(V, x);
+    second = __builtin_bit_cast(V, y);
+}
+
+// Stores the 16 values at `row` that a lane and its partner in the other half
+// of the wavefront hold 4 by 4 in turn (both have to come here).
+template <class E>
+__device__ __forceinline__ void store_sixteen(E* row, const float (&x)[8]) {
+    const int upper = threadIdx.x >> 5 & 1;
+    if constexpr (sizeof(E) == 2) {
+        Vec4<E> a, b;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            a[r] = static_cast<E>(x[r]);
+            b[r] = static_cast<E>(x[4 + r]);
+        }
+        swap_halves(a, b);
+        *reinterpret_cast<Vec8<E>*>(row + upper * 8) = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            *reinterpret_cast<Vec4<E>*>(row + q * 8 + upper * 4) = Vec4<E>{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    }
+}
+
 // The tiles of C for a grid of workgroups that each take several, in rounds of
 // one tile a workgroup.  The tiles behind the last full round are cut into
 // `splits` parts of the summed axis, so that they too keep the grid busy.
 // Workgroups go to the eight dies in turn, and each die has its own L2: a die
 // takes a run of neighbouring tiles, ordered so that those in flight at once
 // (four along a by the rest along b) share their operands.
+struct Tile {
+    int64_t a, b;
+    int64_t part;   // of its sum; -1: the whole tile
+    int64_t index;  // of the part among all parts
+};
 struct TileOrder {
     static constexpr int kDies = 8, kGroup = 4;
     int64_t tiles_a, tiles_b, full, tail, splits, round = 0;
-    __device__ TileOrder(int64_t ta, int64_t tb, int64_t most_splits) : tiles_a(ta), tiles_b(tb) {
-        const int64_t tiles = ta * tb, grid = gridDim.x;
+    __device__ TileOrder(int64_t ta, int64_t tb, int64_t most_splits, int64_t grid = gridDim.x) : tiles_a(ta), tiles_b(tb) {
+        const int64_t tiles = ta * tb;
         full = tiles / grid * grid;
         tail = tiles - full;
         splits = 1;
@@ -331,13 +395,11 @@ struct TileOrder {
         *b = rest / width;
         *a = group * kGroup + (rest - *b * width);
     }
-    // part: -1 for a whole tile, else its part of the sum; index: of the part
-    // among all parts.
-    __device__ bool next(int64_t* a, int64_t* b, int64_t* part, int64_t* index) {
+    __device__ bool next(Tile* t) {
         const int64_t grid = gridDim.x, die = blockIdx.x % kDies, in_die = blockIdx.x / kDies;
         if (round * grid < full) {
-            place(die * (full / kDies) + in_die + round * (grid / kDies), a, b);
-            *part = -1;
+            place(die * (full / kDies) + in_die + round * (grid / kDies), &t->a, &t->b);
+            t->part = -1;
             ++round;
             return true;
         }
@@ -346,9 +408,9 @@ struct TileOrder {
         const int64_t parts = tail * splits, per_die = (parts + kDies - 1) / kDies;
         const int64_t at = die * per_die + in_die;
         if (in_die >= per_die || at >= parts) return false;
-        place(full + at % tail, a, b);
-        *part = splits > 1 ? at / tail : -1;
-        *index = at;
+        place(full + at % tail, &t->a, &t->b);
+        t->part = splits > 1 ? at / tail : -1;
+        t->index = at;
         return true;
     }
 };
@@ -492,13 +554,18 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
     if (n <= 0) return;
     h.kept = n;
     TileOrder order((out.vocab + S::kA - 1) / S::kA, (n + S::kB - 1) / S::kB, 1);
+    Product<S, T, kTerms, false, false> product(table, h, blocks);
     const Place<S> place;
-    int64_t ta, tb, part, index;
-    while (order.next(&ta, &tb, &part, &index)) {
+    Tile tile, after;
+    bool more = order.next(&tile);
+    if (more) product.start(tile.a * S::kA, tile.b * S::kB, 0, kTerms * blocks, stage0);
+    for (; more; tile = after) {
         Acc acc[S::kTilesA][S::kTilesB];
         clear<S>(acc);
-        product<S, T, kTerms, false, false>(table, ta * S::kA, h, tb * S::kB, blocks, 0, kTerms * blocks, stage0, stage1,
-                                            acc);
+        product.run(acc, stage0, stage1);
+        more = order.next(&after);
+        if (more) product.start(after.a * S::kA, after.b * S::kB, 0, kTerms * blocks, stage0);
+        const int64_t ta = tile.a, tb = tile.b;
         const int64_t v0 = ta * S::kA + place.row(0, 0);
         if ((ta + 1) * S::kA > out.vocab) {  // rows behind the vocabulary
             const int left = static_cast<int>(out.vocab - v0);
@@ -516,34 +583,41 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
             const int64_t token = tb * S::kB + place.column(j);
             const int64_t to_label = token < n ? out.labels[out.first + token] - v0 : -1;
             const int label = to_label >= 0 && to_label < S::kTilesA * 32 ? static_cast<int>(to_label) : -1;
-            float most = -__builtin_inff(), at_label = 0.0f;
+            float most = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < S::kTilesA; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    most = fmaxf(most, acc[i][j][r]);
-                    at_label = label == i * 32 + (r >> 2) * 8 + (r & 3) ? acc[i][j][r] : at_label;
-                }
-            if (label >= 0 && (label & 4) == 0) out.label_logit[token] = at_label;
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][j][r]);
+            if (__ballot(label >= 0) != 0) {  // few granules hold a label of the wavefront's tokens
+                float at_label = 0.0f;
+#pragma unroll
+                for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        at_label = label == i * 32 + (r >> 2) * 8 + (r & 3) ? acc[i][j][r] : at_label;
+                if (label >= 0 && (label & 4) == 0) out.label_logit[token] = at_label;
+            }
             most = fmaxf(most, __shfl_xor(most, 32));
             // a granule without a finite maximum keeps its logits' own limits
             const float base = most == -__builtin_inff() ? 0.0f : most;
             float sum = 0.0f;
-            E* row = static_cast<E*>(out.scores) + token * out.padded + v0;
+            // the row from the wavefront's first value on, and its room there
+            const int64_t w0 = v0 - (threadIdx.x >> 3 & 4);
+            E* row = static_cast<E*>(out.scores) + token * out.padded + w0;
             const int room = !out.scores || token >= n ? 0
-                             : static_cast<int>(out.padded - v0 < S::kTilesA * 32 ? out.padded - v0 : S::kTilesA * 32);
+                             : static_cast<int>(out.padded - w0 < S::kTilesA * 32 ? out.padded - w0 : S::kTilesA * 32);
 #pragma unroll
             for (int i = 0; i < S::kTilesA; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float e[4];
+                for (int q = 0; q < 4; q += 2) {
+                    float e[8];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
+                    for (int r = 0; r < 8; ++r) {
                         e[r] = __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - base) * kLog2e);
                         sum += e[r];
                         e[r] *= kHeldUnit<E>;
                     }
-                    if (i * 32 + q * 8 < room) store_floats<E, 4>(row + i * 32 + q * 8, e);
+                    if (i * 32 + q * 8 < room) store_sixteen<E>(row + i * 32 + q * 8, e);
                 }
             sum += __shfl_xor(sum, 32);
             if ((threadIdx.x & 32) == 0 && token < n) {
@@ -711,75 +785,65 @@ __device__ float4* tile_at(float* tiles, int64_t index) {
     return reinterpret_cast<float4*>(tiles + index * (S::kA * S::kB)) + threadIdx.x;
 }
 
+// The part (i, j) of a tile held as one float4 a thread and four rows.
 template <class S>
-__device__ void store_tile(float4* to, const Acc (&acc)[S::kTilesA][S::kTilesB]) {
+__device__ __forceinline__ void store_part(float4* to, int i, int j, const Acc& acc) {
 #pragma unroll
-    for (int i = 0; i < S::kTilesA; ++i)
-#pragma unroll
-        for (int j = 0; j < S::kTilesB; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                to[((i * S::kTilesB + j) * 4 + q) * S::kThreads] =
-                    make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    for (int q = 0; q < 4; ++q)
+        to[((i * S::kTilesB + j) * 4 + q) * S::kThreads] =
+            make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
 }
 
 template <class S>
-__device__ void add_tile(const float4* from, Acc (&acc)[S::kTilesA][S::kTilesB]) {
+__device__ __forceinline__ void add_part(const float4* from, int i, int j, Acc& acc) {
 #pragma unroll
-    for (int i = 0; i < S::kTilesA; ++i)
-#pragma unroll
-        for (int j = 0; j < S::kTilesB; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 x = from[((i * S::kTilesB + j) * 4 + q) * S::kThreads];
-                acc[i][j][4 * q] += x.x;
-                acc[i][j][4 * q + 1] += x.y;
-                acc[i][j][4 * q + 2] += x.z;
-                acc[i][j][4 * q + 3] += x.w;
-            }
+    for (int q = 0; q < 4; ++q) {
+        const float4 x = from[((i * S::kTilesB + j) * 4 + q) * S::kThreads];
+        acc[4 * q] += x.x;
+        acc[4 * q + 1] += x.y;
+        acc[4 * q + 2] += x.z;
+        acc[4 * q + 3] += x.w;
+    }
 }
 
-// A finished tile: into the carried sums while token blocks follow, else
-// scaled and rounded into the output.
+// A finished part of a tile: into the carried sums while token blocks follow,
+// else scaled and rounded into the output.
 template <class S, class Out>
-__device__ void finish(const GradientOut& o, const GradientPlan& p, int64_t ta, int64_t tb, Acc (&acc)[S::kTilesA][S::kTilesB]) {
-    if (o.table && o.first > 0) add_tile<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), acc);
+__device__ __forceinline__ void finish(const GradientOut& o, const GradientPlan& p, int64_t ta, int64_t tb, int i, int j,
+                                       Acc& acc) {
+    if (o.table && o.first > 0) add_part<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), i, j, acc);
     if (o.table && !p.last) {
-        store_tile<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), acc);
+        store_part<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), i, j, acc);
         return;
     }
     const int32_t all = *o.count;
     const float factor = (o.mean ? (all > 0 ? o.scale / static_cast<float>(all) : 0.0f) : o.scale) / o.unit;
     const Place<S> place;
-    const int64_t columns = o.table ? o.vocab : p.n;
+    const int64_t columns = o.table ? o.vocab : p.n, b = tb * S::kB + place.column(j);
+    const int upper = threadIdx.x >> 5 & 1;
+    Out* row = b < columns ? static_cast<Out*>(o.to) + (o.table ? b : o.rows[o.first + b]) * o.stride : nullptr;
 #pragma unroll
-    for (int j = 0; j < S::kTilesB; ++j) {
-        const int64_t b = tb * S::kB + place.column(j);
-        if (b >= columns) continue;
-        Out* row = static_cast<Out*>(o.to) + (o.table ? b : o.rows[o.first + b]) * o.stride;
+    for (int q = 0; q < 4; q += 2) {
+        float4 lo{factor * acc[4 * q], factor * acc[4 * q + 1], factor * acc[4 * q + 2], factor * acc[4 * q + 3]};
+        float4 hi{factor * acc[4 * q + 4], factor * acc[4 * q + 5], factor * acc[4 * q + 6], factor * acc[4 * q + 7]};
+        swap_halves(lo, hi);
+        float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        const int64_t a = ta * S::kA + place.row(i, q) + upper * 4;  // place counts 4 for the upper half
+        if (!row || a >= o.dim) continue;
+        if (a + 8 <= o.dim) {
+            if (o.accumulate) {
+                float old[8];
+                load_floats<Out, 8>(row + a, old);
 #pragma unroll
-        for (int i = 0; i < S::kTilesA; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t a = ta * S::kA + place.row(i, q);
-                float x[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = factor * acc[i][j][4 * q + r];
-                if (a + 4 <= o.dim) {
-                    if (o.accumulate) {
-                        float old[4];
-                        load_floats<Out, 4>(row + a, old);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) x[r] += old[r];
-                    }
-                    store_floats<Out, 4>(row + a, x);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (a + r < o.dim)
-                            row[a + r] = rounded<Out>(o.accumulate ? static_cast<float>(row[a + r]) + x[r] : x[r]);
-                }
+                for (int r = 0; r < 8; ++r) x[r] += old[r];
             }
+            store_floats<Out, 8>(row + a, x);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (a + r < o.dim)
+                    row[a + r] = rounded<Out>(o.accumulate ? static_cast<float>(row[a + r]) + x[r] : x[r]);
+        }
     }
 }
 
@@ -796,37 +860,53 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
         g.kept = p.n;
     }
     TileOrder order(p.tiles_a, p.tiles_b, p.most_splits);
+    Product<S, T, kTerms, true, kTable> product(wide, g, p.blocks);
     const int64_t steps = kTerms * p.blocks;
-    int64_t ta, tb, part, index;
-    while (order.next(&ta, &tb, &part, &index)) {
+    const auto start = [&](const Tile& t) {
+        product.start(t.a * S::kA, t.b * S::kB, t.part < 0 ? 0 : steps * t.part / order.splits,
+                      t.part < 0 ? steps : steps * (t.part + 1) / order.splits, stage0);
+    };
+    Tile tile, after;
+    bool more = order.next(&tile);
+    if (more) start(tile);
+    for (; more; tile = after) {
         Acc acc[S::kTilesA][S::kTilesB];
         clear<S>(acc);
-        const bool whole = part < 0;
-        product<S, T, kTerms, true, kTable>(wide, ta * S::kA, g, tb * S::kB, p.blocks,
-                                            whole ? 0 : steps * part / order.splits,
-                                            whole ? steps : steps * (part + 1) / order.splits, stage0, stage1,
-                                            acc);
-        if (whole)
-            finish<S, Out>(o, p, ta, tb, acc);
-        else
-            store_tile<S>(tile_at<S>(o.partials, index), acc);
+        product.run(acc, stage0, stage1);
+        more = order.next(&after);
+        if (more) start(after);
+#pragma unroll
+        for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kTilesB; ++j) {
+                if (tile.part < 0)
+                    finish<S, Out>(o, p, tile.a, tile.b, i, j, acc[i][j]);
+                else
+                    store_part<S>(tile_at<S>(o.partials, tile.index), i, j, acc[i][j]);
+            }
     }
 }
 
-// Adds the parts of the tiles that were cut, in their order.
+// Adds the parts of the tiles that were cut, in their order; a workgroup a 32 x
+// 32 part of each wavefront's, so that a few tiles occupy many.
 template <class S, class Out>
-__global__ __launch_bounds__(S::kThreads) void join_parts_kernel(GradientOut o) {
+__global__ __launch_bounds__(S::kThreads) void join_parts_kernel(GradientOut o, int grid) {
     const GradientPlan p = gradient_plan<S>(o);
     if (nothing_to_do(o, p)) return;
-    const TileOrder order(p.tiles_a, p.tiles_b, p.most_splits);
+    const TileOrder order(p.tiles_a, p.tiles_b, p.most_splits, grid);
     if (order.splits == 1) return;
-    for (int64_t t = blockIdx.x; t < order.tail; t += gridDim.x) {
-        Acc acc[S::kTilesA][S::kTilesB];
-        clear<S>(acc);
-        for (int64_t s = 0; s < order.splits; ++s) add_tile<S>(tile_at<S>(o.partials, s * order.tail + t), acc);
+    constexpr int kParts = S::kTilesA * S::kTilesB;
+    for (int64_t u = blockIdx.x; u < order.tail * kParts; u += gridDim.x) {
+        const int64_t t = u / kParts;
+        const int i = static_cast<int>(u % kParts) / S::kTilesB, j = static_cast<int>(u % kParts) % S::kTilesB;
+        Acc acc;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+#pragma unroll 4
+        for (int64_t s = 0; s < order.splits; ++s) add_part<S>(tile_at<S>(o.partials, s * order.tail + t), i, j, acc);
         int64_t ta, tb;
         order.place(order.full + t, &ta, &tb);
-        finish<S, Out>(o, p, ta, tb, acc);
+        finish<S, Out>(o, p, ta, tb, i, j, acc);
     }
 }
 
@@ -913,7 +993,7 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
                       c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried};
         Operand wide{table.at, table.stride, c.dim_padded, c.vocab, table.plane};
         hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o);
-        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o);
+        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o, grid);
         o.table = true;
         o.to = c.dtable.at;
         o.stride = c.dtable.stride;
@@ -921,7 +1001,7 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         wide = {h.at, h.stride, c.dim_padded, 0, h.plane};
         g.kept = c.vocab_padded;
         hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, true>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o);
-        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o);
+        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o, grid);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kTotalBlock), 0, stream, c.count, c.counted_losses, c.mean, c.losses,
