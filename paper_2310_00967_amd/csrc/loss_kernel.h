@@ -14,11 +14,12 @@ namespace micro {
 constexpr int kProductDepth = 64;
 // binary32 operands enter the products as the sum of this many bfloat16 ones.
 constexpr int kSplitPlanes = 3;
+// Calls of up to so many tokens take narrow product tiles, and up to so many
+// middle ones.
+constexpr int kFewTokens = 64, kSomeTokens = 512;
 // Vocabulary rows that share one running maximum: what one wavefront of the
-// score product holds (with few tokens, kGranuleFew).
-constexpr int kGranule = 128, kGranuleFew = 32;
-// Calls of up to this many tokens take the narrow product tiles.
-constexpr int kFewTokens = 64;
+// score product holds, in wide, middle and narrow tiles.
+constexpr int kGranule = 128, kGranuleSome = 64, kGranuleFew = 32;
 
 // One call's operands and scratch.  Lengths: D = dim, Dp = D rounded up to
 // kProductDepth, Vp = vocab rounded up to it, B = tokens of a block (a
@@ -39,7 +40,7 @@ struct LossCall {
     bool accumulate;         // add to dtable
     Rows dhidden, dtable;    // out
     // scratch
-    int32_t* count;          // counted tokens
+    int32_t* count;          // counted tokens; then whether a target lies outside the vocabulary
     int32_t* rows;           // their positions, ascending
     int32_t* labels;         // and targets
     float* counted_losses;   // one per counted token

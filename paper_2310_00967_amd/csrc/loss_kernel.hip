@@ -70,9 +70,11 @@ struct Shape {
     static constexpr int kWavesA = WA, kWavesB = WB, kTilesA = TA, kTilesB = TB;
     static constexpr int kThreads = 64 * WA * WB;
     static constexpr int kA = WA * TA * 32, kB = WB * TB * 32;  // the tile of C
+    static_assert(kA * kDepth * 2 >= WA * WB * 4096, "the exchange fits a tile of a");
     static constexpr int kPerUnit = 160 * 1024 / (2 * (kA + kB) * kDepth * 2);  // workgroups of a compute unit
 };
 using Wide = Shape<2, 4, 4, 2>;
+using Middle = Shape<2, 2, 2, 2>;
 using Narrow32 = Shape<4, 1, 1, 1>;
 using Narrow64 = Shape<4, 1, 1, 2>;
 
@@ -164,7 +166,9 @@ __device__ __forceinline__ void interleave() {
     }
 }
 
-// The two operands' tiles of a stage.  Each tile of each stage is a variable of
+// The two operands' tiles of a stage.  While a tile of C is finished, the first
+// stage is already being filled for the next and the second one's tile of a
+// serves the exchange.  Each tile of each stage is a variable of
 // its own: that is how the compiler knows that reads of one stage need not wait
 // for the loads into the other.
 struct Tiles {
@@ -319,11 +323,14 @@ __device__ void clear(Acc (&acc)[S::kTilesA][S::kTilesB]) {
 // Where a lane's four adjacent values acc[i][j][4 q .. 4 q + 3] lie in C.
 template <class S>
 struct Place {
-    int a, b;  // of the lane's first value in the tile
+    int wave_a, wave_b;  // the wavefront's first value in the tile
+    int a, b;            // the lane's
     __device__ Place() {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        a = wave / S::kWavesB * (S::kTilesA * 32) + (lane >> 5) * 4;
-        b = wave % S::kWavesB * (S::kTilesB * 32) + (lane & 31);
+        wave_a = wave / S::kWavesB * (S::kTilesA * 32);
+        wave_b = wave % S::kWavesB * (S::kTilesB * 32);
+        a = wave_a + (lane >> 5) * 4;
+        b = wave_b + (lane & 31);
     }
     __device__ int row(int i, int q) const { return a + i * 32 + q * 8; }
     __device__ int column(int j) const { return b + j * 32; }
@@ -347,25 +354,26 @@ __device__ __forceinline__ void swap_halves(V& first, V& second) {
     second = __builtin_bit_cast(V, y);
 }
 
-// Stores the 16 values at `row` that a lane and its partner in the other half
-// of the wavefront hold 4 by 4 in turn (both have to come here).
-template <class E>
-__device__ __forceinline__ void store_sixteen(E* row, const float (&x)[8]) {
-    const int upper = threadIdx.x >> 5 & 1;
-    if constexpr (sizeof(E) == 2) {
-        Vec4<E> a, b;
+using Chunk = uint32_t __attribute__((ext_vector_type(4)));  // 16 bytes
+constexpr int kExchange = 4096;                               // shared memory of a wavefront's exchange
+
+// 32 rows of C by 128 bytes change hands within a wavefront.  In: lane l holds
+// of row l % 32 the chunks 2 m + l / 32.  Out: chunk l % 8 of the rows 8 k + l /
+// 8, so that a store covers whole 128-byte lines of eight rows.  The chunks are
+// permuted like a straight tile's.  `area` is the wavefront's own.
+__device__ __forceinline__ void exchange(MICRO_SHARED char* area, const Chunk (&in)[4], Chunk (&out)[4]) {
+    const int lane = threadIdx.x & 63;
+    const int row = lane & 31, upper = lane >> 5;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            a[r] = static_cast<E>(x[r]);
-            b[r] = static_cast<E>(x[4 + r]);
-        }
-        swap_halves(a, b);
-        *reinterpret_cast<Vec8<E>*>(row + upper * 8) = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
+    for (int m = 0; m < 4; ++m)
+        *(MICRO_SHARED Chunk*)(area + row * 128 + ((2 * m + upper) ^ ((row >> 1) & 7)) * 16) = in[m];
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-            *reinterpret_cast<Vec4<E>*>(row + q * 8 + upper * 4) = Vec4<E>{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    for (int k = 0; k < 4; ++k) {
+        const int r = 8 * k + (lane >> 3);
+        out[k] = *(MICRO_SHARED Chunk*)(area + r * 128 + ((lane & 7) ^ ((r >> 1) & 7)) * 16);
     }
+    __builtin_amdgcn_wave_barrier();
 }
 
 // The tiles of C for a grid of workgroups that each take several, in rounds of
@@ -423,37 +431,68 @@ __device__ __forceinline__ int64_t target_of(const TokenIds& ids, int64_t t) {
     return ids.wide ? static_cast<const int64_t*>(ids.at)[t] : static_cast<const int32_t*>(ids.at)[t];
 }
 
-constexpr int kSelectBlock = 1024;
+constexpr int kSelectBlock = 1024, kSelectEach = 8, kSelectWaves = kSelectBlock / 64;
 
-// The counted tokens in ascending order.  losses: 0 for an ignored token, NaN
-// for a target outside the vocabulary (which does not count either).
+// The counted tokens in ascending order, kSelectEach runs of kSelectBlock
+// tokens at a time.  losses: 0 for an ignored token, NaN for a target outside
+// the vocabulary (which does not count either).  count[1]: whether there is one.
 __global__ __launch_bounds__(kSelectBlock) void select_kernel(TokenIds targets, int64_t tokens, int64_t ignored, int64_t vocab,
                                                               int32_t* count, int32_t* rows, int32_t* labels, float* losses) {
-    __shared__ int32_t waves[kSelectBlock / 64];
+    __shared__ int32_t starts[kSelectEach * kSelectWaves];
+    __shared__ int32_t total;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t before = 0;
-    for (int64_t first = 0; first < tokens; first += kSelectBlock) {
-        const int64_t t = first + threadIdx.x;
-        const int64_t y = t < tokens ? target_of(targets, t) : ignored;
-        const bool counted = t < tokens && y != ignored && y >= 0 && y < vocab;
-        const uint64_t all = __ballot(counted);
-        __syncthreads();
-        if (lane == 0) waves[wave] = __popcll(all);
-        __syncthreads();
-        int32_t at = before;
-        for (int w = 0; w < kSelectBlock / 64; ++w) {
-            if (w < wave) at += waves[w];
-            before += waves[w];
+    bool outside = false;
+    for (int64_t first = 0; first < tokens; first += kSelectBlock * kSelectEach) {
+        const int64_t t0 = first + threadIdx.x;
+        int64_t y[kSelectEach];
+        uint64_t all[kSelectEach];
+#pragma unroll
+        for (int u = 0; u < kSelectEach; ++u) {
+            const int64_t t = t0 + u * kSelectBlock;
+            y[u] = target_of(targets, t < tokens ? t : tokens - 1);
         }
-        if (counted) {
-            at += __popcll(all & ((uint64_t(1) << lane) - 1));
-            rows[at] = static_cast<int32_t>(t);
-            labels[at] = static_cast<int32_t>(y);
-        } else if (t < tokens) {
-            losses[t] = y == ignored ? 0.0f : __builtin_nanf("");
+#pragma unroll
+        for (int u = 0; u < kSelectEach; ++u) {
+            const int64_t t = t0 + u * kSelectBlock;
+            const bool inside = y[u] != ignored && y[u] >= 0 && y[u] < vocab, counted = t < tokens && inside;
+            all[u] = __ballot(counted);
+            if (lane == 0) starts[u * kSelectWaves + wave] = __popcll(all[u]);
+            if (!inside && t < tokens) {
+                losses[t] = y[u] == ignored ? 0.0f : __builtin_nanf("");
+                outside |= y[u] != ignored;
+            }
         }
+        __syncthreads();
+        if (wave == 0) {  // exclusive scan of the wavefronts' counts, in the tokens' order
+            static_assert(kSelectEach * kSelectWaves == 128, "two counts a lane");
+            const int32_t x = starts[2 * lane], sum = x + starts[2 * lane + 1];
+            int32_t up = sum;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int32_t z = __shfl_up(up, d);
+                if (lane >= d) up += z;
+            }
+            starts[2 * lane] = up - sum;
+            starts[2 * lane + 1] = up - sum + x;
+            if (lane == 63) total = up;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kSelectEach; ++u)
+            if (all[u] >> lane & 1) {
+                const int32_t at = before + starts[u * kSelectWaves + wave] + __popcll(all[u] & ((uint64_t(1) << lane) - 1));
+                rows[at] = static_cast<int32_t>(t0 + u * kSelectBlock);
+                labels[at] = static_cast<int32_t>(y[u]);
+            }
+        before += total;
+        __syncthreads();
     }
-    if (threadIdx.x == 0) *count = before;
+    const int any = __syncthreads_or(outside);
+    if (threadIdx.x == 0) {
+        count[0] = before;
+        count[1] = any != 0;
+    }
 }
 
 // x as a + b + c.  A first term that would round past bfloat16's range is cut
@@ -556,6 +595,8 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
     TileOrder order((out.vocab + S::kA - 1) / S::kA, (n + S::kB - 1) / S::kB, 1);
     Product<S, T, kTerms, false, false> product(table, h, blocks);
     const Place<S> place;
+    MICRO_SHARED char* const area = stage1.a + (threadIdx.x >> 6) * kExchange;
+    constexpr int kRun = 2;  // matrix tiles along a whose 16-bit values fill 128 bytes of a row
     Tile tile, after;
     bool more = order.next(&tile);
     if (more) product.start(tile.a * S::kA, tile.b * S::kB, 0, kTerms * blocks, stage0);
@@ -567,6 +608,8 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
         if (more) product.start(after.a * S::kA, after.b * S::kB, 0, kTerms * blocks, stage0);
         const int64_t ta = tile.a, tb = tile.b;
         const int64_t v0 = ta * S::kA + place.row(0, 0);
+        // the wavefront's first row and token
+        const int64_t w0 = ta * S::kA + place.wave_a, t0 = tb * S::kB + place.wave_b;
         if ((ta + 1) * S::kA > out.vocab) {  // rows behind the vocabulary
             const int left = static_cast<int>(out.vocab - v0);
 #pragma unroll
@@ -601,24 +644,68 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
             // a granule without a finite maximum keeps its logits' own limits
             const float base = most == -__builtin_inff() ? 0.0f : most;
             float sum = 0.0f;
-            // the row from the wavefront's first value on, and its room there
-            const int64_t w0 = v0 - (threadIdx.x >> 3 & 4);
-            E* row = static_cast<E*>(out.scores) + token * out.padded + w0;
-            const int room = !out.scores || token >= n ? 0
-                             : static_cast<int>(out.padded - w0 < S::kTilesA * 32 ? out.padded - w0 : S::kTilesA * 32);
+            const auto exponential = [base](float l) { return __builtin_amdgcn_exp2f((l - base) * kLog2e); };
+            if constexpr (sizeof(E) == 2) {
 #pragma unroll
-            for (int i = 0; i < S::kTilesA; ++i)
+                for (int i = 0; i < S::kTilesA; i += kRun) {
+                    Chunk in[4], to[4];
 #pragma unroll
-                for (int q = 0; q < 4; q += 2) {
-                    float e[8];
+                    for (int m = 0; m < 4; ++m) {
+                        if (i + m / 2 >= S::kTilesA) {
+                            in[m] = Chunk{0, 0, 0, 0};
+                            continue;
+                        }
+                        Vec4<E> lo, hi;
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        e[r] = __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - base) * kLog2e);
-                        sum += e[r];
-                        e[r] *= kHeldUnit<E>;
+                        for (int r = 0; r < 4; ++r) {
+                            const float x = exponential(acc[i + m / 2][j][m % 2 * 8 + r]);
+                            const float y = exponential(acc[i + m / 2][j][m % 2 * 8 + 4 + r]);
+                            sum += x;
+                            sum += y;
+                            lo[r] = static_cast<E>(x * kHeldUnit<E>);
+                            hi[r] = static_cast<E>(y * kHeldUnit<E>);
+                        }
+                        swap_halves(lo, hi);
+                        in[m] = __builtin_bit_cast(Chunk, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                     }
-                    if (i * 32 + q * 8 < room) store_sixteen<E>(row + i * 32 + q * 8, e);
+                    if (out.scores) {
+                        exchange(area, in, to);
+                        const int64_t v = w0 + i * 32 + (threadIdx.x & 7) * 8;
+                        const bool in_tile = (threadIdx.x & 7) * 8 < (S::kTilesA - i) * 32;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int64_t t = t0 + j * 32 + 8 * k + (threadIdx.x >> 3 & 7);
+                            if (t < n && v < out.padded && in_tile)
+                                *reinterpret_cast<Chunk*>(static_cast<E*>(out.scores) + t * out.padded + v) = to[k];
+                        }
+                    }
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < S::kTilesA; ++i) {
+                    Chunk in[4], to[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        Vec4<float> x;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            x[r] = exponential(acc[i][j][4 * q + r]);
+                            sum += x[r];
+                        }
+                        in[q] = __builtin_bit_cast(Chunk, x);
+                    }
+                    if (out.scores) {
+                        exchange(area, in, to);
+                        const int64_t v = w0 + i * 32 + (threadIdx.x & 7) * 4;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int64_t t = t0 + j * 32 + 8 * k + (threadIdx.x >> 3 & 7);
+                            if (t < n && v < out.padded)
+                                *reinterpret_cast<Chunk*>(static_cast<E*>(out.scores) + t * out.padded + v) = to[k];
+                        }
+                    }
+                }
+            }
             sum += __shfl_xor(sum, 32);
             if ((threadIdx.x & 32) == 0 && token < n) {
                 const int64_t granule = v0 / (S::kTilesA * 32);
@@ -632,44 +719,54 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
 // between the products
 // ---------------------------------------------------------------------------
 
-constexpr int kJoinTokens = 32, kJoinSlices = 16;
+constexpr int kJoinAhead = 8;
+constexpr int64_t kFewJoined = 2048;
 
 // Maximum, inverse sum and loss of every counted token of the block, from its
-// granules.
-__global__ __launch_bounds__(kJoinTokens* kJoinSlices) void softmax_kernel(const int32_t* count, int64_t first, int64_t block,
-                                                                           const float2* stats, int64_t granules,
-                                                                           const float* label_logit, const int32_t* rows,
-                                                                           float2* softmax, float* counted_losses, float* losses) {
-    __shared__ float2 part[kJoinSlices][kJoinTokens];
+// granules: kTokens tokens a workgroup, kSlices threads each.
+template <int kTokens, int kSlices>
+__global__ __launch_bounds__(kTokens* kSlices) void softmax_kernel(const int32_t* count, int64_t first, int64_t block,
+                                                                   const float2* stats, int64_t granules,
+                                                                   const float* label_logit, const int32_t* rows,
+                                                                   float2* softmax, float* counted_losses, float* losses) {
+    __shared__ float2 part[kSlices][kTokens];
     const int64_t counted = *count - first, n = counted < block ? counted : block;
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * kJoinTokens + (threadIdx.x % kJoinTokens);
-    const int slice = threadIdx.x / kJoinTokens;
-    if (static_cast<int64_t>(blockIdx.x) * kJoinTokens >= n) return;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * kTokens + (threadIdx.x % kTokens);
+    const int slice = threadIdx.x / kTokens;
+    if (static_cast<int64_t>(blockIdx.x) * kTokens >= n) return;
     const int64_t at = token < n ? token : n - 1;
     float most = -__builtin_inff(), sum = 0.0f;
-    const auto join = [&](float2 s) {
-        const float to = fmaxf(most, s.x);
-        if (to == -__builtin_inff()) {
-            sum += s.y;  // both sums are 0, or NaN
-            return;
-        }
-        sum = sum * __builtin_amdgcn_exp2f((most - to) * kLog2e) + s.y * __builtin_amdgcn_exp2f((s.x - to) * kLog2e);
+    const auto join = [&](const auto& s, int parts) {
+        float to = most;
+#pragma unroll
+        for (int u = 0; u < parts; ++u) to = fmaxf(to, s[u].x);
+        // of granules without any finite maximum the sums are 0, or NaN
+        const float base = to == -__builtin_inff() ? 0.0f : to;
+        sum *= __builtin_amdgcn_exp2f((most == to ? 0.0f : most - base) * kLog2e);
+#pragma unroll
+        for (int u = 0; u < parts; ++u) sum += s[u].y * __builtin_amdgcn_exp2f((s[u].x == to ? 0.0f : s[u].x - base) * kLog2e);
         most = to;
     };
-    for (int64_t g = slice; g < granules; g += 4 * kJoinSlices) {
-        float2 s[4];
+    for (int64_t g = slice; g < granules; g += kJoinAhead * kSlices) {
+        float2 s[kJoinAhead];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            s[u] = g + u * kJoinSlices < granules ? stats[(g + u * kJoinSlices) * block + at]
-                                                  : make_float2(-__builtin_inff(), 0.0f);
+        for (int u = 0; u < kJoinAhead; ++u)
+            s[u] = stats[(g + u * kSlices < granules ? g + u * kSlices : granules - 1) * block + at];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) join(s[u]);
+        for (int u = 0; u < kJoinAhead; ++u)
+            if (g + u * kSlices >= granules) s[u] = make_float2(-__builtin_inff(), 0.0f);
+        join(s, kJoinAhead);
     }
-    part[slice][threadIdx.x % kJoinTokens] = make_float2(most, sum);
-    __syncthreads();
+    part[slice][threadIdx.x % kTokens] = make_float2(most, sum);
+    for (int half = kSlices / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (slice < half) {
+            const float2 other[1] = {part[slice + half][threadIdx.x % kTokens]};
+            join(other, 1);
+            part[slice][threadIdx.x % kTokens] = make_float2(most, sum);
+        }
+    }
     if (slice != 0 || token >= n) return;
-    most = -__builtin_inff(), sum = 0.0f;
-    for (int s = 0; s < kJoinSlices; ++s) join(part[s][threadIdx.x]);
     // (the label's logit is often the maximum itself, and their difference exact)
     const float loss = (most - label_logit[token]) + logf(sum);
     softmax[token] = make_float2(most, 1.0f / sum);
@@ -806,43 +903,105 @@ __device__ __forceinline__ void add_part(const float4* from, int i, int j, Acc& 
     }
 }
 
-// A finished part of a tile: into the carried sums while token blocks follow,
-// else scaled and rounded into the output.
-template <class S, class Out>
-__device__ __forceinline__ void finish(const GradientOut& o, const GradientPlan& p, int64_t ta, int64_t tb, int i, int j,
-                                       Acc& acc) {
-    if (o.table && o.first > 0) add_part<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), i, j, acc);
+// The factor of both gradients.
+__device__ __forceinline__ float gradient_factor(const GradientOut& o) {
+    const int32_t all = *o.count;
+    return (o.mean ? (all > 0 ? o.scale / static_cast<float>(all) : 0.0f) : o.scale) / o.unit;
+}
+
+// A finished tile: into the carried sums while token blocks follow, else scaled
+// and rounded into the output.  16-bit values change hands rounded, two matrix
+// tiles along a at a time; binary32 ones, and those that are added to, in 32
+// bits.
+template <class S, class Out, int kParts>
+__device__ __forceinline__ void finish(const GradientOut& o, const GradientPlan& p, MICRO_SHARED char* area, int64_t ta,
+                                       int64_t tb, int i0, int j, Acc (&acc)[kParts]) {
+    if (o.table && o.first > 0)
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) add_part<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), i0 + i, j, acc[i]);
     if (o.table && !p.last) {
-        store_part<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), i, j, acc);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) store_part<S>(tile_at<S>(o.carried, tb * p.tiles_a + ta), i0 + i, j, acc[i]);
         return;
     }
-    const int32_t all = *o.count;
-    const float factor = (o.mean ? (all > 0 ? o.scale / static_cast<float>(all) : 0.0f) : o.scale) / o.unit;
+    const float factor = gradient_factor(o);
     const Place<S> place;
-    const int64_t columns = o.table ? o.vocab : p.n, b = tb * S::kB + place.column(j);
-    const int upper = threadIdx.x >> 5 & 1;
-    Out* row = b < columns ? static_cast<Out*>(o.to) + (o.table ? b : o.rows[o.first + b]) * o.stride : nullptr;
+    const int64_t columns = o.table ? o.vocab : p.n;
+    const int64_t b0 = tb * S::kB + place.wave_b + j * 32 + (threadIdx.x >> 3 & 7);
+    const int64_t a0 = ta * S::kA + place.wave_a + i0 * 32;
+    Chunk in[4], to[4];
+    const auto row = [&](int k) -> Out* {
+        const int64_t b = b0 + 8 * k;
+        if (b >= columns) return nullptr;
+        return static_cast<Out*>(o.to) + (o.table ? b : o.rows[o.first + b]) * o.stride;
+    };
+    if constexpr (sizeof(Out) == 2) {
+        if (!o.accumulate) {
 #pragma unroll
-    for (int q = 0; q < 4; q += 2) {
-        float4 lo{factor * acc[4 * q], factor * acc[4 * q + 1], factor * acc[4 * q + 2], factor * acc[4 * q + 3]};
-        float4 hi{factor * acc[4 * q + 4], factor * acc[4 * q + 5], factor * acc[4 * q + 6], factor * acc[4 * q + 7]};
-        swap_halves(lo, hi);
-        float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-        const int64_t a = ta * S::kA + place.row(i, q) + upper * 4;  // place counts 4 for the upper half
-        if (!row || a >= o.dim) continue;
-        if (a + 8 <= o.dim) {
-            if (o.accumulate) {
-                float old[8];
-                load_floats<Out, 8>(row + a, old);
+            for (int i = 0; i < kParts; i += 2) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) x[r] += old[r];
+                for (int m = 0; m < 4; ++m) {
+                    Vec4<Out> lo{}, hi{};
+                    if (i + m / 2 < kParts) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            lo[r] = rounded<Out>(factor * acc[i + m / 2][m % 2 * 8 + r]);
+                            hi[r] = rounded<Out>(factor * acc[i + m / 2][m % 2 * 8 + 4 + r]);
+                        }
+                    }
+                    swap_halves(lo, hi);
+                    in[m] = __builtin_bit_cast(Chunk, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+                exchange(area, in, to);
+                const int64_t a = a0 + i * 32 + (threadIdx.x & 7) * 8;
+                if ((threadIdx.x & 4) != 0 && i + 1 >= kParts) continue;  // the second matrix tile is not there
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    Out* at = row(k);
+                    if (!at) break;
+                    const Pack<Out, 8> x = __builtin_bit_cast(Pack<Out, 8>, to[k]);
+                    if (a + 8 <= o.dim) {
+                        *reinterpret_cast<Pack<Out, 8>*>(at + a) = x;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            if (a + r < o.dim) at[a + r] = x.v[r];
+                    }
+                }
             }
-            store_floats<Out, 8>(row + a, x);
-        } else {
+            return;
+        }
+    }
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if (a + r < o.dim)
-                    row[a + r] = rounded<Out>(o.accumulate ? static_cast<float>(row[a + r]) + x[r] : x[r]);
+    for (int i = 0; i < kParts; ++i) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            in[q] = __builtin_bit_cast(Chunk, Vec4<float>{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]});
+        exchange(area, in, to);
+        const int64_t a = a0 + i * 32 + (threadIdx.x & 7) * 4;
+        if (a >= o.dim) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            Out* at = row(k);
+            if (!at) break;
+            at += a;
+            const Vec4<float> sums = __builtin_bit_cast(Vec4<float>, to[k]);
+            float x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = factor * sums[r];
+            if (a + 4 <= o.dim) {
+                if (o.accumulate) {
+                    float old[4];
+                    load_floats<Out, 4>(at, old);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] += old[r];
+                }
+                store_floats<Out, 4>(at, x);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (a + r < o.dim) at[r] = rounded<Out>(o.accumulate ? static_cast<float>(at[r]) + x[r] : x[r]);
+            }
         }
     }
 }
@@ -862,6 +1021,7 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
     TileOrder order(p.tiles_a, p.tiles_b, p.most_splits);
     Product<S, T, kTerms, true, kTable> product(wide, g, p.blocks);
     const int64_t steps = kTerms * p.blocks;
+    MICRO_SHARED char* const area = stage1.a + (threadIdx.x >> 6) * kExchange;
     const auto start = [&](const Tile& t) {
         product.start(t.a * S::kA, t.b * S::kB, t.part < 0 ? 0 : steps * t.part / order.splits,
                       t.part < 0 ? steps : steps * (t.part + 1) / order.splits, stage0);
@@ -876,14 +1036,17 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
         more = order.next(&after);
         if (more) start(after);
 #pragma unroll
-        for (int i = 0; i < S::kTilesA; ++i)
+        for (int j = 0; j < S::kTilesB; ++j) {
+            Acc column[S::kTilesA];
 #pragma unroll
-            for (int j = 0; j < S::kTilesB; ++j) {
-                if (tile.part < 0)
-                    finish<S, Out>(o, p, tile.a, tile.b, i, j, acc[i][j]);
-                else
-                    store_part<S>(tile_at<S>(o.partials, tile.index), i, j, acc[i][j]);
+            for (int i = 0; i < S::kTilesA; ++i) column[i] = acc[i][j];
+            if (tile.part < 0) {
+                finish<S, Out, S::kTilesA>(o, p, area, tile.a, tile.b, 0, j, column);
+            } else {
+#pragma unroll
+                for (int i = 0; i < S::kTilesA; ++i) store_part<S>(tile_at<S>(o.partials, tile.index), i, j, column[i]);
             }
+        }
     }
 }
 
@@ -891,6 +1054,7 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
 // 32 part of each wavefront's, so that a few tiles occupy many.
 template <class S, class Out>
 __global__ __launch_bounds__(S::kThreads) void join_parts_kernel(GradientOut o, int grid) {
+    __shared__ __attribute__((aligned(1024))) char shared[S::kThreads / 64 * kExchange];
     const GradientPlan p = gradient_plan<S>(o);
     if (nothing_to_do(o, p)) return;
     const TileOrder order(p.tiles_a, p.tiles_b, p.most_splits, grid);
@@ -899,38 +1063,41 @@ __global__ __launch_bounds__(S::kThreads) void join_parts_kernel(GradientOut o, 
     for (int64_t u = blockIdx.x; u < order.tail * kParts; u += gridDim.x) {
         const int64_t t = u / kParts;
         const int i = static_cast<int>(u % kParts) / S::kTilesB, j = static_cast<int>(u % kParts) % S::kTilesB;
-        Acc acc;
+        Acc acc[1];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+        for (int r = 0; r < 16; ++r) acc[0][r] = 0.0f;
 #pragma unroll 4
-        for (int64_t s = 0; s < order.splits; ++s) add_part<S>(tile_at<S>(o.partials, s * order.tail + t), i, j, acc);
+        for (int64_t s = 0; s < order.splits; ++s) add_part<S>(tile_at<S>(o.partials, s * order.tail + t), i, j, acc[0]);
         int64_t ta, tb;
         order.place(order.full + t, &ta, &tb);
-        finish<S, Out>(o, p, ta, tb, i, j, acc);
+        finish<S, Out, 1>(o, p, (MICRO_SHARED char*)shared + (threadIdx.x >> 6) * kExchange, ta, tb, i, j, acc);
     }
 }
 
-constexpr int kTotalBlock = 1024;
+constexpr int kTotalBlock = 1024, kTotalEach = 8;
 
-// The sum or mean of the losses, in binary64 and a fixed order.
-__global__ __launch_bounds__(kTotalBlock) void total_kernel(const int32_t* count, const float* losses, bool mean, const float* all,
-                                                            int64_t tokens, TokenIds targets, int64_t ignored, int64_t vocab,
-                                                            float* loss) {
+// The sum or mean of the losses, in binary64 and a fixed order; NaN when a
+// target lies outside the vocabulary.
+__global__ __launch_bounds__(kTotalBlock) void total_kernel(const int32_t* count, const float* losses, bool mean, float* loss) {
     __shared__ double waves[kTotalBlock / 64];
-    const int64_t n = *count;
+    const int64_t n = count[0];
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kTotalBlock) sum += static_cast<double>(losses[i]);
-    // a target outside the vocabulary makes the loss NaN
-    for (int64_t i = threadIdx.x; i < tokens; i += kTotalBlock) {
-        const int64_t y = target_of(targets, i);
-        if (y != ignored && (y < 0 || y >= vocab)) sum = all[i];
+    for (int64_t i = threadIdx.x; i < n; i += kTotalEach * kTotalBlock) {
+        float x[kTotalEach];
+#pragma unroll
+        for (int u = 0; u < kTotalEach; ++u) x[u] = losses[i + u * kTotalBlock < n ? i + u * kTotalBlock : n - 1];
+#pragma unroll
+        for (int u = 0; u < kTotalEach; ++u)
+            if (i + u * kTotalBlock < n) sum += static_cast<double>(x[u]);
     }
+#pragma unroll
     for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x != 0) return;
     sum = 0.0;
     for (int w = 0; w < kTotalBlock / 64; ++w) sum += waves[w];
+    if (count[1]) sum = __builtin_nan("");
     *loss = static_cast<float>(mean && n > 0 ? sum / static_cast<double>(n) : sum);
 }
 
@@ -967,7 +1134,7 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
     if (e != hipSuccess) return e;
     const int granule = S::kTilesA * 32;
     // a call of few tokens has more granules, and room for them in a shorter block
-    const int64_t block = S::kB < Wide::kB ? kFewTokens : c.block;
+    const int64_t block = granule == kGranuleFew ? kFewTokens : granule == kGranuleSome ? std::min<int64_t>(kSomeTokens, c.block) : c.block;
     const int64_t granules = (c.vocab + S::kA - 1) / S::kA * S::kWavesA;
     const int grid = product_grid<S>(c);
     for (int64_t first = 0; first < c.tokens || first == 0; first += block) {
@@ -977,9 +1144,15 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
                            int64_t(c.dim_padded / kDepth),
                            ScoreOut{c.count, c.labels, first, block, c.vocab, c.vocab_padded, c.stats, c.label_logit,
                                     c.gradients ? c.scores : nullptr});
-        hipLaunchKernelGGL(softmax_kernel, dim3(ceil_div(most, kJoinTokens)), dim3(kJoinTokens * kJoinSlices), 0, stream,
-                           c.count, first, block, c.stats, granules, c.label_logit, c.rows, c.softmax, c.counted_losses,
-                           c.losses);
+        const auto join = [&](auto kernel, int tokens, int slices) {
+            hipLaunchKernelGGL(kernel, dim3(ceil_div(most, tokens)), dim3(tokens * slices), 0, stream, c.count, first, block,
+                               c.stats, granules, c.label_logit, c.rows, c.softmax, c.counted_losses, c.losses);
+        };
+        // few tokens: more threads for each, so that enough loads are under way
+        if (most <= kFewJoined)
+            join(softmax_kernel<8, 128>, 8, 128);
+        else
+            join(softmax_kernel<32, 16>, 32, 16);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (!c.gradients) continue;
         const uint32_t turns = ceil_div(c.vocab_padded, kTurnBlock * (16 / int(sizeof(E))));
@@ -1004,8 +1177,8 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o, grid);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kTotalBlock), 0, stream, c.count, c.counted_losses, c.mean, c.losses,
-                       c.tokens, c.targets, c.ignored, c.vocab, c.loss);
+    hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kTotalBlock), 0, stream, c.count, c.counted_losses, c.mean,
+                       c.loss);
     return hipGetLastError();
 }
 
@@ -1013,6 +1186,7 @@ template <class In, class T, class E, int kTerms>
 hipError_t pick(const LossCall& c, hipStream_t stream) {
     if (c.tokens <= 32) return run<In, T, E, kTerms, Narrow32>(c, stream);
     if (c.tokens <= kFewTokens) return run<In, T, E, kTerms, Narrow64>(c, stream);
+    if (c.tokens <= kSomeTokens) return run<In, T, E, kTerms, Middle>(c, stream);
     return run<In, T, E, kTerms, Wide>(c, stream);
 }
 

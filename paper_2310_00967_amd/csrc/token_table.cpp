@@ -134,11 +134,12 @@ micro_status loss_scratch(micro_table* t, bool copy_table, bool gradients) {
     const int64_t score = split ? 4 + 2 * kSplitPlanes : 2;
     const int64_t fits = std::max<int64_t>(t->cfg.score_bytes / (vocab * score) / 256, 1) * 256;
     c.block = std::min(fits, round_up(tokens, 256));
-    // [granule][block]; short calls have more granules (and use the same block stride)
-    const int64_t granules = std::max(round_up(t->vocab, 2 * kGranule) / kGranule * c.block,
-                                      round_up(t->vocab, 4 * kGranuleFew) / kGranuleFew * kFewTokens);
+    // [granule][block]; shorter calls have more granules and shorter blocks
+    const int64_t granules = std::max({round_up(t->vocab, 256) / kGranule * c.block,
+                                       round_up(t->vocab, 256) / kGranuleSome * kSomeTokens,
+                                       round_up(t->vocab, 256) / kGranuleFew * kFewTokens});
     if (micro_status st = ensure(&t->loss_memory, "token loss", [&](Parts& p) {
-            p.take(c.count, 4);
+            p.take(c.count, 8);
             p.take(c.rows, tokens * 4);
             p.take(c.labels, tokens * 4);
             p.take(c.counted_losses, tokens * 4);
