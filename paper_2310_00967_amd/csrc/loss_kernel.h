@@ -40,7 +40,8 @@ struct LossCall {
     bool accumulate;         // add to dtable
     Rows dhidden, dtable;    // out
     // scratch
-    int32_t* count;          // counted tokens; then whether a target lies outside the vocabulary
+    uint32_t* chunks;        // counted tokens of each 1024
+    int32_t* count;          // counted tokens, whether a target lies outside the vocabulary, arrivals
     int32_t* rows;           // their positions, ascending
     int32_t* labels;         // and targets
     float* counted_losses;   // one per counted token
@@ -51,7 +52,7 @@ struct LossCall {
     float2* softmax;         // (maximum, 1 / sum of exponentials) of [B]
     void* scores;            // exponentials, then logit gradients, [B][Vp]; binary32: floats
     void* split;             // binary32: the logit gradients as [P][B][Vp] bfloat16
-    float* partials;         // a wide tile per compute unit: parts of products cut along the summed axis
+    float* partials;         // parts of the two gradient products cut along the sum: a wide tile per compute unit each
     float* carried;          // wide tiles of dtable between token blocks; null with one block
     int compute_units;
 };

@@ -431,68 +431,29 @@ __device__ __forceinline__ int64_t target_of(const TokenIds& ids, int64_t t) {
     return ids.wide ? static_cast<const int64_t*>(ids.at)[t] : static_cast<const int32_t*>(ids.at)[t];
 }
 
-constexpr int kSelectBlock = 1024, kSelectEach = 8, kSelectWaves = kSelectBlock / 64;
+// Tokens of a chunk, whose counted ones are counted together.
+constexpr int kChunkTokens = 1024;
+// A target outside the vocabulary in a chunk, beside its count.
+constexpr uint32_t kOutside = 0x80000000u;
 
-// The counted tokens in ascending order, kSelectEach runs of kSelectBlock
-// tokens at a time.  losses: 0 for an ignored token, NaN for a target outside
-// the vocabulary (which does not count either).  count[1]: whether there is one.
-__global__ __launch_bounds__(kSelectBlock) void select_kernel(TokenIds targets, int64_t tokens, int64_t ignored, int64_t vocab,
-                                                              int32_t* count, int32_t* rows, int32_t* labels, float* losses) {
-    __shared__ int32_t starts[kSelectEach * kSelectWaves];
-    __shared__ int32_t total;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int32_t before = 0;
-    bool outside = false;
-    for (int64_t first = 0; first < tokens; first += kSelectBlock * kSelectEach) {
-        const int64_t t0 = first + threadIdx.x;
-        int64_t y[kSelectEach];
-        uint64_t all[kSelectEach];
-#pragma unroll
-        for (int u = 0; u < kSelectEach; ++u) {
-            const int64_t t = t0 + u * kSelectBlock;
-            y[u] = target_of(targets, t < tokens ? t : tokens - 1);
-        }
-#pragma unroll
-        for (int u = 0; u < kSelectEach; ++u) {
-            const int64_t t = t0 + u * kSelectBlock;
-            const bool inside = y[u] != ignored && y[u] >= 0 && y[u] < vocab, counted = t < tokens && inside;
-            all[u] = __ballot(counted);
-            if (lane == 0) starts[u * kSelectWaves + wave] = __popcll(all[u]);
-            if (!inside && t < tokens) {
-                losses[t] = y[u] == ignored ? 0.0f : __builtin_nanf("");
-                outside |= y[u] != ignored;
-            }
-        }
-        __syncthreads();
-        if (wave == 0) {  // exclusive scan of the wavefronts' counts, in the tokens' order
-            static_assert(kSelectEach * kSelectWaves == 128, "two counts a lane");
-            const int32_t x = starts[2 * lane], sum = x + starts[2 * lane + 1];
-            int32_t up = sum;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int32_t z = __shfl_up(up, d);
-                if (lane >= d) up += z;
-            }
-            starts[2 * lane] = up - sum;
-            starts[2 * lane + 1] = up - sum + x;
-            if (lane == 63) total = up;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kSelectEach; ++u)
-            if (all[u] >> lane & 1) {
-                const int32_t at = before + starts[u * kSelectWaves + wave] + __popcll(all[u] & ((uint64_t(1) << lane) - 1));
-                rows[at] = static_cast<int32_t>(t0 + u * kSelectBlock);
-                labels[at] = static_cast<int32_t>(y[u]);
-            }
-        before += total;
-        __syncthreads();
-    }
-    const int any = __syncthreads_or(outside);
-    if (threadIdx.x == 0) {
-        count[0] = before;
-        count[1] = any != 0;
-    }
+struct Targets {
+    TokenIds ids;
+    int64_t tokens, ignored, vocab;
+    __device__ bool counts(int64_t y) const { return y != ignored && y >= 0 && y < vocab; }
+    __device__ bool outside(int64_t y) const { return y != ignored && (y < 0 || y >= vocab); }
+};
+
+__global__ __launch_bounds__(kChunkTokens) void count_kernel(Targets targets, uint32_t* chunks) {
+    __shared__ int32_t waves[kChunkTokens / 64];
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * kChunkTokens + threadIdx.x;
+    const int64_t y = t < targets.tokens ? target_of(targets.ids, t) : targets.ignored;
+    const uint64_t all = __ballot(targets.counts(y));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = __popcll(all);
+    const int any = __syncthreads_or(targets.outside(y));
+    if (threadIdx.x != 0) return;
+    uint32_t sum = 0;
+    for (int w = 0; w < kChunkTokens / 64; ++w) sum += waves[w];
+    chunks[blockIdx.x] = sum | (any ? kOutside : 0);
 }
 
 // x as a + b + c.  A first term that would round past bfloat16's range is cut
@@ -512,10 +473,20 @@ __device__ __forceinline__ void split3(float x, bf16& a, bf16& b, bf16& c) {
     }
 }
 
-// One row of `dim` values into `padded` values of each plane, zeros behind.
+// One row of `dim` values into `padded` values of each plane, zeros behind, by
+// `threads` threads.
 template <class T>
-__device__ void copy_row(const T* from, int dim, T* to, int padded, int64_t) {
-    for (int c = threadIdx.x * 8; c < padded; c += blockDim.x * 8) {
+__device__ void copy_row(const T* from, int dim, T* to, int padded, int64_t, int thread, int threads) {
+    constexpr int kAhead = 4;
+    int c = thread * 8;
+    for (; c + (kAhead - 1) * threads * 8 + 8 <= dim; c += kAhead * threads * 8) {
+        Pack<T, 8> x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u] = *reinterpret_cast<const Pack<T, 8>*>(from + c + u * threads * 8);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) *reinterpret_cast<Pack<T, 8>*>(to + c + u * threads * 8) = x[u];
+    }
+    for (; c < padded; c += threads * 8) {
         Pack<T, 8> x;
         if (c + 8 <= dim)
             x = *reinterpret_cast<const Pack<T, 8>*>(from + c);
@@ -524,8 +495,8 @@ __device__ void copy_row(const T* from, int dim, T* to, int padded, int64_t) {
         *reinterpret_cast<Pack<T, 8>*>(to + c) = x;
     }
 }
-__device__ void copy_row(const float* from, int dim, bf16* to, int padded, int64_t plane) {
-    for (int c = threadIdx.x * 4; c < padded; c += blockDim.x * 4) {
+__device__ inline void copy_row(const float* from, int dim, bf16* to, int padded, int64_t plane, int thread, int threads) {
+    for (int c = thread * 4; c < padded; c += threads * 4) {
         Pack<bf16, 4> p[kSplitPlanes];
         for (int j = 0; j < 4; ++j)
             split3(c + j < dim ? from[c + j] : 0.0f, p[0].v[j], p[1].v[j], p[2].v[j]);
@@ -533,32 +504,105 @@ __device__ void copy_row(const float* from, int dim, bf16* to, int padded, int64
     }
 }
 
-constexpr int kRowBlock = 256;
+constexpr int kRowBlock = 256, kGathered = kRowBlock / 64;  // a token a wavefront
 
-// The counted rows of hidden, padded, with zero rows up to a multiple of
-// kDepth; and zeros into dhidden's rows of tokens that do not count.
+struct Selection {
+    const uint32_t* chunks;  // of count_kernel; not read for the tokens of one chunk
+    int32_t* count;          // out: counted tokens; whether a target lies outside; 0 (softmax_kernel's arrivals)
+    int32_t* rows;           // out
+    int32_t* labels;         // out
+    float* losses;           // out: 0 for an ignored token, NaN for a target outside the vocabulary
+};
+
+// The counted tokens in ascending order: their positions, targets and rows of
+// hidden, padded.  For the gradients (dhidden not null) with zero rows behind up
+// to a multiple of kDepth, and zeros into dhidden's rows of tokens that do not
+// count.  Each workgroup finds its
+// own tokens' places from the chunks before and its chunk's targets.
 template <class In, class T>
-__global__ __launch_bounds__(kRowBlock) void gather_kernel(const In* hidden, int64_t stride, int64_t tokens, int dim,
-                                                           const int32_t* count, const int32_t* rows, T* h, int padded,
-                                                           int64_t plane, TokenIds targets, int64_t ignored, int64_t vocab,
-                                                           In* dhidden, int64_t dstride) {
-    const int64_t n = *count, r = blockIdx.x;
-    if (r < n) {
-        copy_row(hidden + rows[r] * stride, dim, h + r * padded, padded, plane);
-    } else if (r < (n + kDepth - 1) / kDepth * kDepth) {
-        copy_row(hidden, 0, h + r * padded, padded, plane);
+__global__ __launch_bounds__(kRowBlock) void gather_kernel(const In* hidden, int64_t stride, int dim, Targets targets,
+                                                           Selection out, T* h, int padded, int64_t plane, In* dhidden,
+                                                           int64_t dstride) {
+    __shared__ int32_t waves[kGathered];
+    __shared__ int32_t any[kGathered];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kGathered, chunk = first / kChunkTokens;
+    const int64_t end = first + kGathered < targets.tokens ? first + kGathered : targets.tokens;
+    int32_t before = 0;  // counted tokens before the workgroup's first
+    bool outside = false;
+    for (int64_t k = threadIdx.x; k < chunk; k += kRowBlock) {
+        const uint32_t c = out.chunks[k];
+        before += static_cast<int32_t>(c & ~kOutside);
+        outside |= (c & kOutside) != 0;
     }
-    if (dhidden && r < tokens) {
-        const int64_t y = target_of(targets, r);
-        if (y == ignored || y < 0 || y >= vocab)
-            for (int c = threadIdx.x; c < dim; c += kRowBlock) dhidden[r * dstride + c] = static_cast<In>(0.0f);
+    if (end > 0) {
+        int64_t y[kChunkTokens / kRowBlock];
+#pragma unroll
+        for (int u = 0; u < kChunkTokens / kRowBlock; ++u) {
+            const int64_t t = chunk * kChunkTokens + u * kRowBlock + threadIdx.x;
+            y[u] = target_of(targets.ids, t < end ? t : end - 1);
+        }
+#pragma unroll
+        for (int u = 0; u < kChunkTokens / kRowBlock; ++u) {
+            const int64_t t = chunk * kChunkTokens + u * kRowBlock + threadIdx.x;
+            before += t < first && targets.counts(y[u]);
+            outside |= t < end && targets.outside(y[u]);
+        }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) before += __shfl_xor(before, d);
+    const uint64_t some = __ballot(outside);
+    if (lane == 0) {
+        waves[wave] = before;
+        any[wave] = some != 0;
+    }
+    __syncthreads();
+    before = 0;
+    outside = false;
+    for (int w = 0; w < kGathered; ++w) {
+        before += waves[w];
+        outside |= any[w] != 0;
+    }
+    uint32_t mine = 0;  // which of the workgroup's tokens count
+    int64_t own = targets.ignored;
+    for (int w = 0; w < kGathered; ++w) {
+        const int64_t y = first + w < end ? target_of(targets.ids, first + w) : targets.ignored;
+        mine |= static_cast<uint32_t>(targets.counts(y)) << w;
+        if (w == wave) own = y;
+    }
+    const int64_t t = first + wave;
+    if (mine >> wave & 1) {
+        const int32_t at = before + __popc(mine & ((1u << wave) - 1));
+        copy_row(hidden + t * stride, dim, h + static_cast<int64_t>(at) * padded, padded, plane, lane, 64);
+        if (lane == 0) {
+            out.rows[at] = static_cast<int32_t>(t);
+            out.labels[at] = static_cast<int32_t>(own);
+        }
+    } else if (t < end) {
+        if (lane == 0) out.losses[t] = own == targets.ignored ? 0.0f : __builtin_nanf("");
+        if (dhidden)
+            for (int c = lane; c < dim; c += 64) dhidden[t * dstride + c] = static_cast<In>(0.0f);
+    }
+    if (first + kGathered < targets.tokens) return;
+    const int32_t n = before + __popc(mine);
+    if (threadIdx.x == 0) {
+        out.count[0] = n;
+        out.count[1] = outside;
+        out.count[2] = 0;
+    }
+    if (!dhidden) return;  // the scores do without the zero rows
+    const int64_t rows = (static_cast<int64_t>(n) + kDepth - 1) / kDepth * kDepth;
+    constexpr int kPlanes = sizeof(In) == 4 ? kSplitPlanes : 1;
+    for (int q = 0; q < kPlanes; ++q) {
+        Pack<T, 8>* zeros = reinterpret_cast<Pack<T, 8>*>(h + q * plane + static_cast<int64_t>(n) * padded);
+        for (int64_t i = threadIdx.x; i < (rows - n) * padded / 8; i += kRowBlock) zeros[i] = Pack<T, 8>{};
     }
 }
 
 template <class In, class T>
 __global__ __launch_bounds__(kRowBlock) void table_kernel(const In* table, int64_t stride, int dim, T* w, int padded,
                                                           int64_t plane) {
-    copy_row(table + blockIdx.x * stride, dim, w + blockIdx.x * int64_t(padded), padded, plane);
+    copy_row(table + blockIdx.x * stride, dim, w + blockIdx.x * int64_t(padded), padded, plane, threadIdx.x, kRowBlock);
 }
 
 // ---------------------------------------------------------------------------
@@ -671,7 +715,7 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
                     if (out.scores) {
                         exchange(area, in, to);
                         const int64_t v = w0 + i * 32 + (threadIdx.x & 7) * 8;
-                        const bool in_tile = (threadIdx.x & 7) * 8 < (S::kTilesA - i) * 32;
+                        const bool in_tile = int(threadIdx.x & 7) * 8 < (S::kTilesA - i) * 32;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int64_t t = t0 + j * 32 + 8 * k + (threadIdx.x >> 3 & 7);
@@ -719,21 +763,58 @@ __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Oper
 // between the products
 // ---------------------------------------------------------------------------
 
+// The sum or mean of the counted tokens' losses, in binary64 and an order that
+// only their number and the workgroup's size determine; NaN when a target lies
+// outside the vocabulary.
+template <int kThreads>
+__device__ void total_loss(const int32_t* count, const float* losses, bool mean, float* loss) {
+    constexpr int kEach = 8;
+    __shared__ double waves[kThreads / 64];
+    const int64_t n = count[0];
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += kEach * kThreads) {
+        float x[kEach];
+#pragma unroll
+        for (int u = 0; u < kEach; ++u)
+            x[u] = __hip_atomic_load(losses + (i + u * kThreads < n ? i + u * kThreads : n - 1), __ATOMIC_RELAXED,
+                                     __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int u = 0; u < kEach; ++u)
+            if (i + u * kThreads < n) sum += static_cast<double>(x[u]);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = 0.0;
+    for (int w = 0; w < kThreads / 64; ++w) sum += waves[w];
+    if (count[1]) sum = __builtin_nan("");
+    *loss = static_cast<float>(mean && n > 0 ? sum / static_cast<double>(n) : sum);
+}
+
 constexpr int kJoinAhead = 8;
 constexpr int64_t kFewJoined = 2048;
 
 // Maximum, inverse sum and loss of every counted token of the block, from its
 // granules: kTokens tokens a workgroup, kSlices threads each.
+// loss (not null where these are all tokens and few workgroups): the workgroup
+// that finishes last adds the losses up.
 template <int kTokens, int kSlices>
-__global__ __launch_bounds__(kTokens* kSlices) void softmax_kernel(const int32_t* count, int64_t first, int64_t block,
+__global__ __launch_bounds__(kTokens* kSlices) void softmax_kernel(int32_t* count, int64_t first, int64_t block,
                                                                    const float2* stats, int64_t granules,
                                                                    const float* label_logit, const int32_t* rows,
-                                                                   float2* softmax, float* counted_losses, float* losses) {
+                                                                   float2* softmax, float* counted_losses, float* losses,
+                                                                   bool mean, float* loss) {
     __shared__ float2 part[kSlices][kTokens];
     const int64_t counted = *count - first, n = counted < block ? counted : block;
     const int64_t token = static_cast<int64_t>(blockIdx.x) * kTokens + (threadIdx.x % kTokens);
     const int slice = threadIdx.x / kTokens;
-    if (static_cast<int64_t>(blockIdx.x) * kTokens >= n) return;
+    if (static_cast<int64_t>(blockIdx.x) * kTokens >= (n > 0 || !loss ? n : 1)) return;
+    if (n <= 0) {  // nothing counts: the first workgroup says so
+        total_loss<kTokens * kSlices>(count, counted_losses, mean, loss);
+        return;
+    }
     const int64_t at = token < n ? token : n - 1;
     float most = -__builtin_inff(), sum = 0.0f;
     const auto join = [&](const auto& s, int parts) {
@@ -746,6 +827,13 @@ __global__ __launch_bounds__(kTokens* kSlices) void softmax_kernel(const int32_t
 #pragma unroll
         for (int u = 0; u < parts; ++u) sum += s[u].y * __builtin_amdgcn_exp2f((s[u].x == to ? 0.0f : s[u].x - base) * kLog2e);
         most = to;
+    };
+    const auto finish_token = [&] {
+        // (the label's logit is often the maximum itself, and their difference exact)
+        const float own = (most - label_logit[token]) + logf(sum);
+        softmax[token] = make_float2(most, 1.0f / sum);
+        __hip_atomic_store(counted_losses + first + token, own, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        losses[rows[first + token]] = own;
     };
     for (int64_t g = slice; g < granules; g += kJoinAhead * kSlices) {
         float2 s[kJoinAhead];
@@ -766,12 +854,17 @@ __global__ __launch_bounds__(kTokens* kSlices) void softmax_kernel(const int32_t
             part[slice][threadIdx.x % kTokens] = make_float2(most, sum);
         }
     }
-    if (slice != 0 || token >= n) return;
-    // (the label's logit is often the maximum itself, and their difference exact)
-    const float loss = (most - label_logit[token]) + logf(sum);
-    softmax[token] = make_float2(most, 1.0f / sum);
-    counted_losses[first + token] = loss;
-    losses[rows[first + token]] = loss;
+    if (slice == 0 && token < n) finish_token();
+    if (!loss) return;
+    // the losses of this workgroup, then its arrival
+    __shared__ bool last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int32_t groups = static_cast<int32_t>((n + kTokens - 1) / kTokens);
+        last = __hip_atomic_fetch_add(count + 2, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == groups - 1;
+    }
+    __syncthreads();
+    if (last) total_loss<kTokens * kSlices>(count, counted_losses, mean, loss);
 }
 
 constexpr int kTurnBlock = 256, kTurnRows = 16;
@@ -1006,11 +1099,36 @@ __device__ __forceinline__ void finish(const GradientOut& o, const GradientPlan&
     }
 }
 
+// Adds the parts of the tiles that were cut, in their order; a workgroup a 32 x
+// 32 part of each wavefront's, so that a few tiles occupy many.  grid: of the
+// product.
+template <class S, class Out>
+__device__ __forceinline__ void join_parts(const GradientOut& o, int64_t grid, MICRO_SHARED char* area) {
+    const GradientPlan p = gradient_plan<S>(o);
+    if (nothing_to_do(o, p)) return;
+    const TileOrder order(p.tiles_a, p.tiles_b, p.most_splits, grid);
+    if (order.splits == 1) return;
+    constexpr int kParts = S::kTilesA * S::kTilesB;
+    for (int64_t u = blockIdx.x; u < order.tail * kParts; u += gridDim.x) {
+        const int64_t t = u / kParts;
+        const int i = static_cast<int>(u % kParts) / S::kTilesB, j = static_cast<int>(u % kParts) % S::kTilesB;
+        Acc acc[1];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[0][r] = 0.0f;
+#pragma unroll 4
+        for (int64_t s = 0; s < order.splits; ++s) add_part<S>(tile_at<S>(o.partials, s * order.tail + t), i, j, acc[0]);
+        int64_t ta, tb;
+        order.place(order.full + t, &ta, &tb);
+        finish<S, Out, 1>(o, p, area, ta, tb, i, j, acc);
+    }
+}
+
 // kTable: dtable^T = h^T g, else dhidden^T = W^T g^T.  a is always the width,
 // so a lane's values are adjacent in an output row.
 template <class S, class T, class Out, int kTerms, bool kTable>
-__global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Operand g, GradientOut o) {
+__global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Operand g, GradientOut o, GradientOut hidden) {
     MICRO_STAGES(S);
+    if (kTable) join_parts<S, Out>(hidden, gridDim.x, stage1.a + (threadIdx.x >> 6) * kExchange);
     const GradientPlan p = gradient_plan<S>(o);
     if (nothing_to_do(o, p)) return;
     if (kTable) {
@@ -1050,55 +1168,16 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
     }
 }
 
-// Adds the parts of the tiles that were cut, in their order; a workgroup a 32 x
-// 32 part of each wavefront's, so that a few tiles occupy many.
 template <class S, class Out>
 __global__ __launch_bounds__(S::kThreads) void join_parts_kernel(GradientOut o, int grid) {
     __shared__ __attribute__((aligned(1024))) char shared[S::kThreads / 64 * kExchange];
-    const GradientPlan p = gradient_plan<S>(o);
-    if (nothing_to_do(o, p)) return;
-    const TileOrder order(p.tiles_a, p.tiles_b, p.most_splits, grid);
-    if (order.splits == 1) return;
-    constexpr int kParts = S::kTilesA * S::kTilesB;
-    for (int64_t u = blockIdx.x; u < order.tail * kParts; u += gridDim.x) {
-        const int64_t t = u / kParts;
-        const int i = static_cast<int>(u % kParts) / S::kTilesB, j = static_cast<int>(u % kParts) % S::kTilesB;
-        Acc acc[1];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[0][r] = 0.0f;
-#pragma unroll 4
-        for (int64_t s = 0; s < order.splits; ++s) add_part<S>(tile_at<S>(o.partials, s * order.tail + t), i, j, acc[0]);
-        int64_t ta, tb;
-        order.place(order.full + t, &ta, &tb);
-        finish<S, Out, 1>(o, p, (MICRO_SHARED char*)shared + (threadIdx.x >> 6) * kExchange, ta, tb, i, j, acc);
-    }
+    join_parts<S, Out>(o, grid, (MICRO_SHARED char*)shared + (threadIdx.x >> 6) * kExchange);
 }
 
-constexpr int kTotalBlock = 1024, kTotalEach = 8;
+constexpr int kTotalBlock = 1024;
 
-// The sum or mean of the losses, in binary64 and a fixed order; NaN when a
-// target lies outside the vocabulary.
 __global__ __launch_bounds__(kTotalBlock) void total_kernel(const int32_t* count, const float* losses, bool mean, float* loss) {
-    __shared__ double waves[kTotalBlock / 64];
-    const int64_t n = count[0];
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kTotalEach * kTotalBlock) {
-        float x[kTotalEach];
-#pragma unroll
-        for (int u = 0; u < kTotalEach; ++u) x[u] = losses[i + u * kTotalBlock < n ? i + u * kTotalBlock : n - 1];
-#pragma unroll
-        for (int u = 0; u < kTotalEach; ++u)
-            if (i + u * kTotalBlock < n) sum += static_cast<double>(x[u]);
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    sum = 0.0;
-    for (int w = 0; w < kTotalBlock / 64; ++w) sum += waves[w];
-    if (count[1]) sum = __builtin_nan("");
-    *loss = static_cast<float>(mean && n > 0 ? sum / static_cast<double>(n) : sum);
+    total_loss<kTotalBlock>(count, losses, mean, loss);
 }
 
 // ---------------------------------------------------------------------------
@@ -1117,12 +1196,14 @@ template <class In, class T, class E, int kTerms, class S>
 hipError_t run(const LossCall& c, hipStream_t stream) {
     constexpr bool kSplit = sizeof(In) == 4;
     const int64_t rows_h = (std::max<int64_t>(c.tokens, 1) + kDepth - 1) / kDepth * kDepth;
-    hipLaunchKernelGGL(select_kernel, dim3(1), dim3(kSelectBlock), 0, stream, c.targets, c.tokens, c.ignored, c.vocab, c.count,
-                       c.rows, c.labels, c.losses);
-    hipLaunchKernelGGL((gather_kernel<In, T>), dim3(static_cast<uint32_t>(rows_h)), dim3(kRowBlock), 0, stream,
-                       static_cast<const In*>(c.hidden.at), c.hidden.stride, c.tokens, c.dim, c.count, c.rows,
-                       static_cast<T*>(c.h), c.dim_padded, rows_h * c.dim_padded, c.targets, c.ignored, c.vocab,
-                       c.gradients ? static_cast<In*>(c.dhidden.at) : nullptr, c.dhidden.stride);
+    const Targets targets{c.targets, c.tokens, c.ignored, c.vocab};
+    if (c.tokens > kChunkTokens)
+        hipLaunchKernelGGL(count_kernel, dim3(ceil_div(c.tokens, kChunkTokens)), dim3(kChunkTokens), 0, stream, targets,
+                           c.chunks);
+    hipLaunchKernelGGL((gather_kernel<In, T>), dim3(ceil_div(std::max<int64_t>(c.tokens, 1), kGathered)), dim3(kRowBlock), 0,
+                       stream, static_cast<const In*>(c.hidden.at), c.hidden.stride, c.dim, targets,
+                       Selection{c.chunks, c.count, c.rows, c.labels, c.losses}, static_cast<T*>(c.h), c.dim_padded,
+                       rows_h * c.dim_padded, c.gradients ? static_cast<In*>(c.dhidden.at) : nullptr, c.dhidden.stride);
     Operand table{c.table.at, c.table.stride, c.vocab, 0, 0};
     if (!table_in_place(c)) {
         table = {c.w, c.dim_padded, c.vocab, 0, c.vocab * c.dim_padded};
@@ -1137,6 +1218,7 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
     const int64_t block = granule == kGranuleFew ? kFewTokens : granule == kGranuleSome ? std::min<int64_t>(kSomeTokens, c.block) : c.block;
     const int64_t granules = (c.vocab + S::kA - 1) / S::kA * S::kWavesA;
     const int grid = product_grid<S>(c);
+    bool total_now = false;
     for (int64_t first = 0; first < c.tokens || first == 0; first += block) {
         const int64_t most = std::max<int64_t>(std::min(c.tokens - first, block), 1);
         const Operand h{static_cast<const T*>(c.h) + first * c.dim_padded, c.dim_padded, 0, 0, rows_h * c.dim_padded};
@@ -1144,9 +1226,11 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
                            int64_t(c.dim_padded / kDepth),
                            ScoreOut{c.count, c.labels, first, block, c.vocab, c.vocab_padded, c.stats, c.label_logit,
                                     c.gradients ? c.scores : nullptr});
+        total_now = c.tokens <= std::min<int64_t>(block, kSomeTokens);
         const auto join = [&](auto kernel, int tokens, int slices) {
             hipLaunchKernelGGL(kernel, dim3(ceil_div(most, tokens)), dim3(tokens * slices), 0, stream, c.count, first, block,
-                               c.stats, granules, c.label_logit, c.rows, c.softmax, c.counted_losses, c.losses);
+                               c.stats, granules, c.label_logit, c.rows, c.softmax, c.counted_losses, c.losses, c.mean,
+                               total_now ? c.loss : nullptr);
         };
         // few tokens: more threads for each, so that enough loads are under way
         if (most <= kFewJoined)
@@ -1165,20 +1249,23 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         GradientOut o{c.count, first, block, false, c.vocab, c.dim, c.rows, c.scale, c.mean, kHeldUnit<T>,
                       c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried};
         Operand wide{table.at, table.stride, c.dim_padded, c.vocab, table.plane};
-        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o);
-        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o, grid);
+        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o, o);
+        const GradientOut of_hidden = o;  // its split tiles are joined by the next product's workgroups
         o.table = true;
         o.to = c.dtable.at;
         o.stride = c.dtable.stride;
         o.accumulate = c.accumulate;
+        o.partials += c.compute_units * kWideTile;
         wide = {h.at, h.stride, c.dim_padded, 0, h.plane};
         g.kept = c.vocab_padded;
-        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, true>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o);
+        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, true>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o,
+                           of_hidden);
         hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o, grid);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kTotalBlock), 0, stream, c.count, c.counted_losses, c.mean,
-                       c.loss);
+    if (!total_now)
+        hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kTotalBlock), 0, stream, c.count, c.counted_losses, c.mean,
+                           c.loss);
     return hipGetLastError();
 }
 

@@ -139,7 +139,8 @@ micro_status loss_scratch(micro_table* t, bool copy_table, bool gradients) {
                                        round_up(t->vocab, 256) / kGranuleSome * kSomeTokens,
                                        round_up(t->vocab, 256) / kGranuleFew * kFewTokens});
     if (micro_status st = ensure(&t->loss_memory, "token loss", [&](Parts& p) {
-            p.take(c.count, 8);
+            p.take(c.count, 12);
+            p.take(c.chunks, tokens * 4 / 1024 + 4);
             p.take(c.rows, tokens * 4);
             p.take(c.labels, tokens * 4);
             p.take(c.counted_losses, tokens * 4);
@@ -157,7 +158,7 @@ micro_status loss_scratch(micro_table* t, bool copy_table, bool gradients) {
     return ensure(&t->gradient_memory, "token loss's gradients", [&](Parts& p) {
         p.take(c.scores, c.block * vocab * (split ? 4 : 2));
         if (split) p.take(c.split, planes * c.block * vocab * 2);
-        p.take(c.partials, t->compute_units * kWideTile * 4);
+        p.take(c.partials, 2 * t->compute_units * kWideTile * 4);
         if (t->max_tokens > c.block)
             p.take(c.carried, round_up(t->vocab, 256) * round_up(t->dim, 256) * 4);
     });
