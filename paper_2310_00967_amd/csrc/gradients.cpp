@@ -14,8 +14,7 @@ struct micro_grads {
     hipStream_t stream = nullptr;
     int64_t total = 0;                                    // values of all tensors
     std::vector<std::pair<const void*, int64_t>> ranges;  // address and bytes of every tensor that has any, by address
-    void* scratch = nullptr;                              // partials, sumsq, arrived, pieces
-    double* sumsq = nullptr;
+    void* scratch = nullptr;                              // partials, pieces
     micro::GradSetDevice dev{};
 };
 
@@ -52,7 +51,7 @@ micro_status build(micro_grads* g, int32_t count, void* const* tensors, const in
             return refuse("two tensors of the set share memory");
     hipError_t e = hipGetDevice(&g->device);
     if (e != hipSuccess) return report_hip(e, "hipGetDevice");
-    const size_t head = (kGradGridMax + 2) * sizeof(double);
+    const size_t head = kGradGridMax * sizeof(double);
     e = hipMalloc(&g->scratch, head + pieces.size() * sizeof(GradPiece));
     if (e != hipSuccess) {
         g->scratch = nullptr;
@@ -61,12 +60,9 @@ micro_status build(micro_grads* g, int32_t count, void* const* tensors, const in
         return MICRO_ENOMEM;
     }
     g->dev.partials = static_cast<double*>(g->scratch);
-    g->sumsq = g->dev.partials + kGradGridMax;
-    g->dev.arrived = reinterpret_cast<uint32_t*>(g->sumsq + 1);
     g->dev.pieces = reinterpret_cast<const GradPiece*>(static_cast<char*>(g->scratch) + head);
     g->dev.count = static_cast<int64_t>(pieces.size());
-    e = hipMemsetAsync(g->scratch, 0, head, g->stream);
-    if (e == hipSuccess && !pieces.empty())
+    if (!pieces.empty())
         e = hipMemcpyAsync(const_cast<GradPiece*>(g->dev.pieces), pieces.data(), pieces.size() * sizeof(GradPiece),
                            hipMemcpyHostToDevice, g->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(g->stream);  // the host's copy of the pieces ends here
@@ -105,11 +101,10 @@ micro_status scale(micro_grads* g, double max_norm, const double* sumsq, float* 
     CallDevice scope(g->device);
     const bool needed = norm || std::isfinite(max_norm);
     if (needed && !sumsq) {
-        const hipError_t e = launch_grads_norm(g->dev, g->sumsq, nullptr, g->stream);
+        const hipError_t e = launch_grads_sums(g->dev, g->stream);
         if (e != hipSuccess) return report_hip(e, "gradient norm launch");
-        sumsq = g->sumsq;
     }
-    return report_hip(launch_grads_scale(g->dev, needed ? sumsq : nullptr, max_norm, flat, norm, g->stream),
+    return report_hip(launch_grads_scale(g->dev, needed, sumsq, max_norm, flat, norm, g->stream),
                       "gradient scale launch");
 }
 

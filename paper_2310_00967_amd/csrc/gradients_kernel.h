@@ -16,24 +16,26 @@ struct GradPiece {
 };
 
 constexpr int kGradBlock = 256;
-// Workgroups of a pass at most: the partial sums that the last one adds.
+// Workgroups of a pass at most, and so partial sums.
 constexpr int kGradGridMax = 2048;
 
 struct GradSetDevice {
     const GradPiece* pieces;
     int64_t count;         // pieces
     double* partials;      // one per workgroup, kGradGridMax
-    uint32_t* arrived;     // workgroups done; 0 between launches
 };
+
+// The workgroups' sums of squares into the partials.
+hipError_t launch_grads_sums(const GradSetDevice& set, hipStream_t stream);
 
 // *sumsq = the sum of the squares of every value; *norm = its root (either
 // may be null).
 hipError_t launch_grads_norm(const GradSetDevice& set, double* sumsq, float* norm, hipStream_t stream);
 
-// Every value times min(1, max_norm / (sqrt(*sumsq) + 1e-6)), in place
-// (flat null) or into flat; *norm = sqrt(*sumsq) unless null.  sumsq null:
-// the factor is 1.
-hipError_t launch_grads_scale(const GradSetDevice& set, const double* sumsq, double max_norm, float* flat,
+// Every value times min(1, max_norm / (sqrt(squares) + 1e-6)) (scaled false:
+// times 1), in place (flat null) or into flat, with squares = *sumsq, or where
+// that is null what launch_grads_sums left; *norm = sqrt(squares) unless null.
+hipError_t launch_grads_scale(const GradSetDevice& set, bool scaled, const double* sumsq, double max_norm, float* flat,
                               float* norm, hipStream_t stream);
 
 }  // namespace micro

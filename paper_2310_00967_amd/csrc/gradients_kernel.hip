@@ -59,10 +59,8 @@ __device__ double block_sum(double x) {
     return sum;
 }
 
-// A workgroup takes every gridDim.x-th piece; the one that finishes last adds
-// the workgroups' sums in their order, so the result does not depend on when
-// each came.
-__global__ __launch_bounds__(kGradBlock) void norm_kernel(GradSetDevice set, double* sumsq, float* norm) {
+// A workgroup takes every gridDim.x-th piece and leaves its sum.
+__global__ __launch_bounds__(kGradBlock) void norm_kernel(GradSetDevice set) {
     double sum = 0.0;
     for (int64_t i = blockIdx.x; i < set.count; i += gridDim.x) {
         const GradPiece piece = set.pieces[i];
@@ -74,22 +72,29 @@ __global__ __launch_bounds__(kGradBlock) void norm_kernel(GradSetDevice set, dou
             sum += sum_squares(static_cast<const bf16*>(piece.values), piece.count);
     }
     sum = block_sum(sum);
-    __shared__ bool last;
-    if (threadIdx.x == 0) {
-        __hip_atomic_store(set.partials + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(set.arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    if (threadIdx.x == 0) set.partials[blockIdx.x] = sum;
+}
+
+// The sum of the workgroups' sums, in their order: the same in every thread of
+// every workgroup that asks.  `count` of them, kGradGridMax at most.
+__device__ double add_partials(const double* partials, int count) {
+    constexpr int kEach = kGradGridMax / kGradBlock;
+    double x[kEach], sum = 0.0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const int i = threadIdx.x + u * kGradBlock;
+        x[u] = partials[i < count ? i : 0];
     }
-    __syncthreads();
-    if (!last) return;
-    sum = 0.0;
-    for (uint32_t b = threadIdx.x; b < gridDim.x; b += kGradBlock)
-        sum += __hip_atomic_load(set.partials + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    sum = block_sum(sum);
-    if (threadIdx.x == 0) {
-        if (sumsq) *sumsq = sum;
-        if (norm) *norm = static_cast<float>(sqrt(sum));
-        __hip_atomic_store(set.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) sum += static_cast<int>(threadIdx.x + u * kGradBlock) < count ? x[u] : 0.0;
+    return block_sum(sum);
+}
+
+__global__ __launch_bounds__(kGradBlock) void total_kernel(const double* partials, int count, double* sumsq, float* norm) {
+    const double sum = add_partials(partials, count);
+    if (threadIdx.x != 0) return;
+    if (sumsq) *sumsq = sum;
+    if (norm) *norm = static_cast<float>(sqrt(sum));
 }
 
 // n values of src times c into dst, which may be src.
@@ -122,11 +127,15 @@ __device__ void scale_piece(const GradPiece& piece, float* flat, float c) {
         scale_run<T, T>(values, values, piece.count, c);
 }
 
-__global__ __launch_bounds__(kGradBlock) void scale_kernel(GradSetDevice set, const double* sumsq, double max_norm,
-                                                           float* flat, float* norm) {
+// scaled: whether c is not simply 1.  The squared norm is *sumsq, or where that
+// is null the sum of the `sums` partial ones, which every workgroup adds for
+// itself: a microsecond, where one workgroup's adding and its signal to the
+// others take several.
+__global__ __launch_bounds__(kGradBlock) void scale_kernel(GradSetDevice set, bool scaled, const double* sumsq, int sums,
+                                                           double max_norm, float* flat, float* norm) {
     float c = 1.0f;
-    if (sumsq) {
-        const double length = sqrt(*sumsq), ratio = max_norm / (length + 1e-6);
+    if (scaled) {
+        const double length = sqrt(sumsq ? *sumsq : add_partials(set.partials, sums)), ratio = max_norm / (length + 1e-6);
         if (max_norm < __builtin_inf() && !(ratio >= 1.0)) c = static_cast<float>(ratio);
         if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(length);
     }
@@ -142,21 +151,28 @@ __global__ __launch_bounds__(kGradBlock) void scale_kernel(GradSetDevice set, co
     }
 }
 
-uint32_t pass_grid(int64_t pieces) {
-    return static_cast<uint32_t>(pieces < 1 ? 1 : pieces > kGradGridMax ? kGradGridMax : pieces);
+int pass_grid(int64_t pieces) {
+    return static_cast<int>(pieces < 1 ? 1 : pieces > kGradGridMax ? kGradGridMax : pieces);
 }
 
 }  // namespace
 
-hipError_t launch_grads_norm(const GradSetDevice& set, double* sumsq, float* norm, hipStream_t stream) {
-    hipLaunchKernelGGL(norm_kernel, dim3(pass_grid(set.count)), dim3(kGradBlock), 0, stream, set, sumsq, norm);
+hipError_t launch_grads_sums(const GradSetDevice& set, hipStream_t stream) {
+    hipLaunchKernelGGL(norm_kernel, dim3(pass_grid(set.count)), dim3(kGradBlock), 0, stream, set);
     return hipGetLastError();
 }
 
-hipError_t launch_grads_scale(const GradSetDevice& set, const double* sumsq, double max_norm, float* flat,
+hipError_t launch_grads_norm(const GradSetDevice& set, double* sumsq, float* norm, hipStream_t stream) {
+    const hipError_t e = launch_grads_sums(set, stream);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kGradBlock), 0, stream, set.partials, pass_grid(set.count), sumsq, norm);
+    return hipGetLastError();
+}
+
+hipError_t launch_grads_scale(const GradSetDevice& set, bool scaled, const double* sumsq, double max_norm, float* flat,
                               float* norm, hipStream_t stream) {
-    hipLaunchKernelGGL(scale_kernel, dim3(pass_grid(set.count)), dim3(kGradBlock), 0, stream, set, sumsq, max_norm,
-                       flat, norm);
+    hipLaunchKernelGGL(scale_kernel, dim3(pass_grid(set.count)), dim3(kGradBlock), 0, stream, set, scaled, sumsq,
+                       pass_grid(set.count), max_norm, flat, norm);
     return hipGetLastError();
 }
 
