@@ -62,6 +62,7 @@ micro_status build(micro_grads* g, int32_t count, void* const* tensors, const in
     g->dev.partials = static_cast<double*>(g->scratch);
     g->dev.pieces = reinterpret_cast<const GradPiece*>(static_cast<char*>(g->scratch) + head);
     g->dev.count = static_cast<int64_t>(pieces.size());
+    g->dev.total = g->total;
     if (!pieces.empty())
         e = hipMemcpyAsync(const_cast<GradPiece*>(g->dev.pieces), pieces.data(), pieces.size() * sizeof(GradPiece),
                            hipMemcpyHostToDevice, g->stream);

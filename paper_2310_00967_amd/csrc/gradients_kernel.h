@@ -22,6 +22,7 @@ constexpr int kGradGridMax = 2048;
 struct GradSetDevice {
     const GradPiece* pieces;
     int64_t count;         // pieces
+    int64_t total;         // values
     double* partials;      // one per workgroup, kGradGridMax
 };
 

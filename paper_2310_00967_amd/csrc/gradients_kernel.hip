@@ -18,8 +18,10 @@
 namespace micro {
 namespace {
 
-// Loads that a thread has in flight before it uses the first.
-constexpr int kUnroll = 4;
+// Loads that a thread has in flight before it uses the first.  Two, four and
+// one are within a percent of each other; eight spill the occupancy that hides
+// the rest (the norm of 11.7M values alone then takes as long as both passes).
+constexpr int kUnroll = 2;
 
 template <class T>
 __device__ double sum_squares(const T* p, int n) {
@@ -43,7 +45,9 @@ __device__ double sum_squares(const T* p, int n) {
             const double d = static_cast<double>(static_cast<float>(p[j]));
             sum[0] = __builtin_fma(d, d, sum[0]);
         }
-    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+    for (int u = 1; u < kUnroll; ++u) sum[0] += sum[u];
+    return sum[0];
 }
 
 // The sum over the workgroup, in a fixed order; in thread 0.
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(kGradBlock) void total_kernel(const double* partial
 }
 
 // n values of src times c into dst, which may be src.
-template <class S, class D>
+template <bool kPast, class S, class D>
 __device__ void scale_run(const S* src, D* dst, int n, float c) {
     // as many values a thread as make the wider side's access 16 bytes
     constexpr int kVec = 16 / (sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D)), kStep = kGradBlock * kVec;
@@ -111,7 +115,10 @@ __device__ void scale_run(const S* src, D* dst, int n, float c) {
         for (int u = 0; u < kUnroll; ++u) {
 #pragma unroll
             for (int j = 0; j < kVec; ++j) x[u][j] *= c;
-            store_floats<D, kVec>(dst + i + u * kStep, x[u]);
+            if constexpr (kPast)
+                stream_floats<D, kVec>(dst + i + u * kStep, x[u]);
+            else
+                store_floats<D, kVec>(dst + i + u * kStep, x[u]);
         }
     }
     for (; i < n; i += kStep)
@@ -119,20 +126,25 @@ __device__ void scale_run(const S* src, D* dst, int n, float c) {
 }
 
 template <class T>
-__device__ void scale_piece(const GradPiece& piece, float* flat, float c) {
+__device__ void scale_piece(const GradPiece& piece, float* flat, bool past, float c) {
     T* values = static_cast<T*>(piece.values);
-    if (flat)
-        scale_run<T, float>(values, flat + piece.offset, piece.count, c);
+    if (!flat)
+        scale_run<false, T, T>(values, values, piece.count, c);
+    else if (past)
+        scale_run<true, T, float>(values, flat + piece.offset, piece.count, c);
     else
-        scale_run<T, T>(values, values, piece.count, c);
+        scale_run<false, T, float>(values, flat + piece.offset, piece.count, c);
 }
 
 // scaled: whether c is not simply 1.  The squared norm is *sumsq, or where that
 // is null the sum of the `sums` partial ones, which every workgroup adds for
 // itself: a microsecond, where one workgroup's adding and its signal to the
-// others take several.
+// others take several.  The pieces are taken last to first: those that the norm
+// read last are still in the cache.  past: the flat vector is larger than that
+// cache.  On 335M values (671 MB of bf16) the order and the stores past the
+// cache took the two passes from 524 to 483 us.
 __global__ __launch_bounds__(kGradBlock) void scale_kernel(GradSetDevice set, bool scaled, const double* sumsq, int sums,
-                                                           double max_norm, float* flat, float* norm) {
+                                                           double max_norm, float* flat, bool past, float* norm) {
     float c = 1.0f;
     if (scaled) {
         const double length = sqrt(sumsq ? *sumsq : add_partials(set.partials, sums)), ratio = max_norm / (length + 1e-6);
@@ -140,16 +152,19 @@ __global__ __launch_bounds__(kGradBlock) void scale_kernel(GradSetDevice set, bo
         if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(length);
     }
     if (!flat && c == 1.0f) return;  // in place and nothing to clip
-    for (int64_t i = blockIdx.x; i < set.count; i += gridDim.x) {
+    for (int64_t i = set.count - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
         const GradPiece piece = set.pieces[i];
         if (piece.type == MICRO_TYPE_F32)
-            scale_piece<float>(piece, flat, c);
+            scale_piece<float>(piece, flat, past, c);
         else if (piece.type == MICRO_TYPE_F16)
-            scale_piece<f16>(piece, flat, c);
+            scale_piece<f16>(piece, flat, past, c);
         else
-            scale_piece<bf16>(piece, flat, c);
+            scale_piece<bf16>(piece, flat, past, c);
     }
 }
+
+// The memory-side cache.
+constexpr int64_t kCacheBytes = int64_t(256) << 20;
 
 int pass_grid(int64_t pieces) {
     return static_cast<int>(pieces < 1 ? 1 : pieces > kGradGridMax ? kGradGridMax : pieces);
@@ -172,7 +187,7 @@ hipError_t launch_grads_norm(const GradSetDevice& set, double* sumsq, float* nor
 hipError_t launch_grads_scale(const GradSetDevice& set, bool scaled, const double* sumsq, double max_norm, float* flat,
                               float* norm, hipStream_t stream) {
     hipLaunchKernelGGL(scale_kernel, dim3(pass_grid(set.count)), dim3(kGradBlock), 0, stream, set, scaled, sumsq,
-                       pass_grid(set.count), max_norm, flat, norm);
+                       pass_grid(set.count), max_norm, flat, set.total * 4 > kCacheBytes, norm);
     return hipGetLastError();
 }
 

@@ -53,83 +53,97 @@ __global__ __launch_bounds__(kBlock) void lookup_kernel(const T* table, int64_t 
 // ---------------------------------------------------------------------------
 
 constexpr int kSortBlock = 1024, kSortWaves = kSortBlock / 64;
+constexpr int kSortRounds = kSortTile / kSortBlock;
 constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
 
 struct SortShared {
     uint32_t keys[kSortTile];
-    uint16_t at[2][kSortTile];               // positions in the tile
-    uint16_t first[kSortWaves][kDigits];     // of a wave's run of a digit
+    uint16_t at[kSortTile];                  // positions in the tile, in the order so far
+    uint32_t first[kSortWaves][kDigits];     // of a wave's run of a digit
     uint32_t totals[kDigits];
 };
 
 // Sorts n <= kSortTile keys of one tile with `passes` stable passes of
-// kDigitBits each.  Every wave owns an equal run of the tile: it counts its
-// digits, a scan over (digit, wave) gives each wave its places, and the wave
-// places its entries 64 at a time, the lanes of one digit ranked by a match
-// over the wave.  Returns which of at[] holds the result.
-__device__ int sort_tile(SortShared& s, int n, int passes) {
+// kDigitBits each.  Every wave owns an equal run of the tile, 64 entries a
+// round, all rounds in registers: the lanes of one digit find each other by a
+// match over the wave, one of them adds their number to the wave's counter of
+// the digit, and what it held before is the group's place in the wave's run of
+// that digit.  A scan over (digit, wave) turns counters into places.
+template <int kRounds>
+__device__ void sort_passes(SortShared& s, int n, int passes) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int rounds = (n + kSortBlock - 1) / kSortBlock, base = wave * rounds * 64;
-    for (int i = threadIdx.x; i < n; i += kSortBlock) s.at[0][i] = static_cast<uint16_t>(i);
-    int from = 0;
-    for (int pass = 0; pass < passes; ++pass, from ^= 1) {
+    const int base = wave * kRounds * 64;
+    for (int i = threadIdx.x; i < n; i += kSortBlock) s.at[i] = static_cast<uint16_t>(i);
+    for (int pass = 0; pass < passes; ++pass) {
         const int shift = pass * kDigitBits;
         for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortBlock) (&s.first[0][0])[i] = 0;
         __syncthreads();
-        // twice over the wave's run: counting, then placing
-        for (int placing = 0; placing < 2; ++placing) {
-            for (int r = 0; r < rounds; ++r) {
-                const int i = base + r * 64 + lane;
-                const bool in = i < n;
-                const uint32_t at = in ? s.at[from][i] : 0;
-                const uint32_t digit = in ? (s.keys[at] >> shift) & (kDigits - 1) : 0;
-                uint64_t same = __ballot(in);
+        uint32_t at[kRounds], digit[kRounds], place[kRounds];
 #pragma unroll
-                for (int b = 0; b < kDigitBits; ++b) {
-                    const bool bit = (digit >> b) & 1;
-                    const uint64_t set = __ballot(bit);
-                    same &= bit ? set : ~set;
-                }
-                const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
-                const int start = in ? s.first[wave][digit] : 0;
-                if (in && placing) s.at[from ^ 1][start + before] = static_cast<uint16_t>(at);
-                // the last lane of a digit moves the wave's counter on
-                if (in && (same >> lane) == 1) s.first[wave][digit] = static_cast<uint16_t>(start + before + 1);
-            }
-            __syncthreads();
-            if (placing) break;
-            // counts to places: within a digit by wave, digits in order
-            if (threadIdx.x < kDigits) {
-                uint32_t sum = 0;
-                for (int w = 0; w < kSortWaves; ++w) {
-                    const uint32_t c = s.first[w][threadIdx.x];
-                    s.first[w][threadIdx.x] = static_cast<uint16_t>(sum);
-                    sum += c;
-                }
-                s.totals[threadIdx.x] = sum;
-            }
-            __syncthreads();
-            if (wave == 0) {  // exclusive scan of the digits' totals, kDigits / 64 a lane
-                uint32_t own[kDigits / 64], sum = 0;
-                for (int j = 0; j < kDigits / 64; ++j) {
-                    own[j] = sum;
-                    sum += s.totals[lane * (kDigits / 64) + j];
-                }
-                uint32_t up = sum;
-                for (int d = 1; d < 64; d <<= 1) {
-                    const uint32_t x = __shfl_up(up, d);
-                    if (lane >= d) up += x;
-                }
-                for (int j = 0; j < kDigits / 64; ++j) s.totals[lane * (kDigits / 64) + j] = up - sum + own[j];
-            }
-            __syncthreads();
-            for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortBlock)
-                (&s.first[0][0])[i] = static_cast<uint16_t>((&s.first[0][0])[i] + s.totals[i & (kDigits - 1)]);
-            __syncthreads();
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = base + r * 64 + lane;
+            at[r] = s.at[i < n ? i : 0];
         }
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) digit[r] = (s.keys[at[r]] >> shift) & (kDigits - 1);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const bool in = base + r * 64 + lane < n;
+            uint64_t same = __ballot(in);
+#pragma unroll
+            for (int b = 0; b < kDigitBits; ++b) {
+                const bool bit = (digit[r] >> b) & 1;
+                const uint64_t set = __ballot(bit);
+                same &= bit ? set : ~set;
+            }
+            const int leader = in ? __ffsll(static_cast<unsigned long long>(same)) - 1 : lane;
+            uint32_t held = 0;
+            if (in && lane == leader) held = atomicAdd(&s.first[wave][digit[r]], static_cast<uint32_t>(__popcll(same)));
+            place[r] = __shfl(held, leader) + __popcll(same & ((uint64_t(1) << lane) - 1));
+        }
+        __syncthreads();
+        // counts to places: within a digit by wave, digits in order
+        if (threadIdx.x < kDigits) {
+            uint32_t c[kSortWaves], sum = 0;
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) c[w] = s.first[w][threadIdx.x];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                s.first[w][threadIdx.x] = sum;
+                sum += c[w];
+            }
+            s.totals[threadIdx.x] = sum;
+        }
+        __syncthreads();
+        if (wave == 0) {  // exclusive scan of the digits' totals, kDigits / 64 a lane
+            uint32_t own[kDigits / 64], sum = 0;
+            for (int j = 0; j < kDigits / 64; ++j) {
+                own[j] = sum;
+                sum += s.totals[lane * (kDigits / 64) + j];
+            }
+            uint32_t up = sum;
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t x = __shfl_up(up, d);
+                if (lane >= d) up += x;
+            }
+            for (int j = 0; j < kDigits / 64; ++j) s.totals[lane * (kDigits / 64) + j] = up - sum + own[j];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+            if (base + r * 64 + lane < n)
+                s.at[s.totals[digit[r]] + s.first[wave][digit[r]] + place[r]] = static_cast<uint16_t>(at[r]);
+        __syncthreads();
     }
-    __syncthreads();
-    return from;
+}
+
+__device__ void sort_tile(SortShared& s, int n, int passes) {
+    if (n <= kSortBlock)
+        sort_passes<1>(s, n, passes);
+    else if (n <= kSortTile / 4)
+        sort_passes<kSortRounds / 4>(s, n, passes);
+    else
+        sort_passes<kSortRounds>(s, n, passes);
 }
 
 // The first workgroups sort one tile of kSortTile tokens each; the others
@@ -147,9 +161,9 @@ __global__ __launch_bounds__(kSortBlock) void sort_kernel(TokenIds ids, int64_t 
             s.keys[i] = static_cast<uint32_t>(id < 0 || id >= vocab || id == padding ? vocab : id);
         }
         __syncthreads();
-        const int in = sort_tile(s, n, passes);
+        sort_tile(s, n, passes);
         for (int i = threadIdx.x; i < n; i += kSortBlock) {
-            const uint32_t at = s.at[in][i];
+            const uint32_t at = s.at[i];
             keys[first + i] = s.keys[at];
             order[first + i] = static_cast<uint32_t>(first + at);
         }
@@ -245,42 +259,58 @@ __device__ __forceinline__ void write_partial(float* row, int c, int dim, const 
 // Rows that a thread has in flight.
 constexpr int kRowsAhead = 8;
 
+// Raw vectors: a row's values stay as they were read until they are added.
+template <class T, int kVec>
+__device__ __forceinline__ Pack<T, kVec> load_raw(const T* row, int c, int dim) {
+    Pack<T, kVec> x;
+    if (c + kVec <= dim) {
+        x = *reinterpret_cast<const Pack<T, kVec>*>(row + c);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x.v[j] = c + j < dim ? row[c + j] : static_cast<T>(0.0f);
+    }
+    return x;
+}
+
 // A group of 2^group_bits threads takes a chunk of kSumChunk sorted tokens,
-// columns [c, c + kVec) a thread.  Partial rows: chunk q's run that comes in
-// from the chunk before (or covers the whole chunk) goes to row 2q, one that
-// starts in it and goes on into the next to row 2q + 1.
-template <class T>
+// columns [c, c + kVec) a thread.  kWide: groups of whole wavefronts, whose
+// keys and positions are the same in every lane and stay in scalar registers.
+// Partial rows: chunk q's run that comes in from the chunk before (or covers
+// the whole chunk) goes to row 2q, one that starts in it and goes on into the
+// next to row 2q + 1.
+template <class T, bool kWide>
 __global__ __launch_bounds__(kBlock) void sum_kernel(const T* grad, int64_t grad_stride, int64_t tokens, const uint32_t* keys,
                                                      const uint32_t* order, uint32_t vocab, float scale, bool accumulate,
                                                      T* table, int64_t table_stride, int32_t dim, float* partials,
                                                      int group_bits) {
     constexpr int kVec = 16 / sizeof(T);
     const int group = 1 << group_bits, lane = threadIdx.x & (group - 1);
-    const int64_t chunk = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> group_bits;
+    const int in_block = static_cast<int>(threadIdx.x) >> group_bits;
+    const int64_t chunk = static_cast<int64_t>(blockIdx.x) * (kBlock >> group_bits) +
+                          (kWide ? __builtin_amdgcn_readfirstlane(in_block) : in_block);
     const int64_t first = chunk * kSumChunk;
     const int c = (static_cast<int>(blockIdx.y) * group + lane) * kVec;
     if (first >= tokens || c >= dim) return;
     const int n = static_cast<int>(tokens - first < kSumChunk ? tokens - first : kSumChunk);
     const bool from_before = first > 0 && keys[first - 1] == keys[first];
     const bool into_next = first + n < tokens && keys[first + n] == keys[first + n - 1];
+    const auto load = [&](int b, Pack<T, kVec> (&x)[kRowsAhead]) {
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u)
+            x[u] = load_raw<T, kVec>(grad + order[first + (b + u < n ? b + u : n - 1)] * grad_stride, c, dim);
+    };
     float sum[kVec] = {};
     int start = 0;  // of the run being summed
-    for (int b = 0; b < n; b += kRowsAhead) {
+    const auto add = [&](int b, const Pack<T, kVec> (&x)[kRowsAhead]) {
         uint32_t key[kRowsAhead + 1];
-        float x[kRowsAhead][kVec];
 #pragma unroll
-        for (int u = 0; u < kRowsAhead; ++u) {
-            const int i = b + u < n ? b + u : n - 1;
-            key[u] = keys[first + i];
-            load_row<T, kVec>(grad + order[first + i] * grad_stride, c, dim, x[u]);
-        }
-        key[kRowsAhead] = b + kRowsAhead < n ? keys[first + b + kRowsAhead] : vocab;
+        for (int u = 0; u <= kRowsAhead; ++u) key[u] = keys[first + (b + u < n ? b + u : n - 1)];
 #pragma unroll
         for (int u = 0; u < kRowsAhead; ++u) {
             const int i = b + u;
             if (i >= n) break;
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) sum[j] += x[u][j];
+            for (int j = 0; j < kVec; ++j) sum[j] += static_cast<float>(x[u].v[j]);
             const bool ends = i == n - 1 || key[u + 1] != key[u];
             if (!ends) continue;
             if (key[u] < vocab) {
@@ -294,6 +324,16 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(const T* grad, int64_t grad
             for (int j = 0; j < kVec; ++j) sum[j] = 0.0f;
             start = i + 1;
         }
+    };
+    static_assert(kSumChunk % (2 * kRowsAhead) == 0, "batches of rows in pairs");
+    Pack<T, kVec> even[kRowsAhead], odd[kRowsAhead];
+    load(0, even);
+#pragma unroll 1
+    for (int b = 0; b < n; b += 2 * kRowsAhead) {
+        load(b + kRowsAhead, odd);
+        add(b, even);
+        if (b + 2 * kRowsAhead < n) load(b + 2 * kRowsAhead, even);
+        add(b + kRowsAhead, odd);
     }
 }
 
@@ -367,9 +407,15 @@ hipError_t sums(const Rows& grad, int64_t tokens, float scale, bool accumulate, 
                     static_cast<uint32_t>((dim + (vec << bits) - 1) / (vec << bits)));
     };
     const int bits = group_bits_for((dim + kVec - 1) / kVec, 8);
-    hipLaunchKernelGGL(sum_kernel<T>, grid(bits, kVec), dim3(kBlock), 0, stream, static_cast<const T*>(grad.at),
-                       grad.stride, tokens, keys, order, static_cast<uint32_t>(vocab), scale, accumulate,
-                       static_cast<T*>(table.at), table.stride, dim, partials, bits);
+    const auto sum = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid(bits, kVec), dim3(kBlock), 0, stream, static_cast<const T*>(grad.at), grad.stride,
+                           tokens, keys, order, static_cast<uint32_t>(vocab), scale, accumulate,
+                           static_cast<T*>(table.at), table.stride, dim, partials, bits);
+    };
+    if (bits >= 6)
+        sum(sum_kernel<T, true>);
+    else
+        sum(sum_kernel<T, false>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks < 2) return e;
     const int join_bits = group_bits_for((dim + 3) / 4, 6);

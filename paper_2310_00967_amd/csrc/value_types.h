@@ -43,4 +43,19 @@ __device__ __forceinline__ void store_floats(T* p, const float (&in)[N]) {
     *reinterpret_cast<Pack<T, N>*>(p) = q;
 }
 
+// The same past the caches: for outputs that do not fit them, which would only
+// push out what is read next.
+template <class T, int N>
+__device__ __forceinline__ void stream_floats(T* p, const float (&in)[N]) {
+    static_assert(sizeof(T) * N == 16, "one 16-byte store");
+    using Words = uint32_t __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed, aligned(2))) Anywhere {
+        Words v;
+    };
+    Pack<T, N> q;
+#pragma unroll
+    for (int i = 0; i < N; ++i) q.v[i] = rounded<T>(in[i]);
+    __builtin_nontemporal_store(__builtin_bit_cast(Words, q), &reinterpret_cast<Anywhere*>(p)->v);
+}
+
 }  // namespace micro
