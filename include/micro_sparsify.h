@@ -494,7 +494,7 @@ MICRO_API void micro_table_config_default(micro_table_config *cfg);
  * A handle for a table of vocab x dim values of `type` and calls of up to
  * max_tokens tokens, enqueuing on hip_stream; cfg NULL: the defaults.  Holds
  * no scratch yet: the first call of each kind allocates what its kind needs
- * (a lookup nothing; its gradient 16 bytes and dim/4 bytes a token; the loss a
+ * (a lookup nothing; its gradient 16 bytes and dim/2 bytes a token; the loss a
  * padded copy of the hidden rows, and of the table where it cannot be read in
  * place: binary32, a dim that is no multiple of 64, or rows that are not
  * aligned to 16 bytes; its gradients the block's scores and 64 MB).
@@ -516,8 +516,8 @@ MICRO_API micro_status micro_table_lookup(micro_table *table, const void *weight
 
 /*
  * The lookup's gradient: dweight[v] = scale * the sum of grad[t] over the
- * tokens t with ids[t] == v, in ascending t and in binary32 (chunks of 32
- * tokens of a row, then the chunks' sums), rounded to the type once.
+ * tokens t with ids[t] == v, in ascending t and in binary32 (chunks of 16
+ * sorted tokens, then the chunks' sums), rounded to the type once.
  * accumulate != 0 adds that to dweight[v] before rounding and leaves rows
  * without a token untouched; else every row is written.  Tokens whose id is
  * padding_id or outside [0, vocab) have no part.

@@ -26,9 +26,9 @@ hipError_t launch_lookup(const Rows& table, int64_t vocab, int32_t dim, const To
                          float scale, const Rows& out, hipStream_t stream);
 
 // Tokens that one workgroup sorts in shared memory.
-constexpr int kSortTile = 16384;
+constexpr int kSortTile = 4096;
 // Sorted tokens that one thread group sums.
-constexpr int kSumChunk = 32;
+constexpr int kSumChunk = 16;
 
 // Scratch of the lookup's gradient for up to `tokens` tokens.
 struct LookupGradScratch {

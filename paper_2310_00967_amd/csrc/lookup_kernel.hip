@@ -10,6 +10,9 @@
 // one partial row per chunk, and a second kernel adds those in order.  No
 // atomics.
 #include "lookup_kernel.h"
+
+#include <algorithm>
+
 #include "micro_sparsify.h"
 #include "value_types.h"
 
@@ -89,13 +92,16 @@ __device__ void sort_passes(SortShared& s, int n, int passes) {
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const bool in = base + r * 64 + lane < n;
-            uint64_t same = __ballot(in);
+            const uint64_t ins = __ballot(in);
+            uint32_t low = static_cast<uint32_t>(ins), high = static_cast<uint32_t>(ins >> 32);
 #pragma unroll
             for (int b = 0; b < kDigitBits; ++b) {
-                const bool bit = (digit[r] >> b) & 1;
-                const uint64_t set = __ballot(bit);
-                same &= bit ? set : ~set;
+                const uint32_t bit = 0u - ((digit[r] >> b) & 1);  // all ones where it is set
+                const uint64_t set = __ballot(bit != 0);
+                low &= ~(static_cast<uint32_t>(set) ^ bit);
+                high &= ~(static_cast<uint32_t>(set >> 32) ^ bit);
             }
+            const uint64_t same = static_cast<uint64_t>(high) << 32 | low;
             const int leader = in ? __ffsll(static_cast<unsigned long long>(same)) - 1 : lane;
             uint32_t held = 0;
             if (in && lane == leader) held = atomicAdd(&s.first[wave][digit[r]], static_cast<uint32_t>(__popcll(same)));
@@ -140,79 +146,96 @@ __device__ void sort_passes(SortShared& s, int n, int passes) {
 __device__ void sort_tile(SortShared& s, int n, int passes) {
     if (n <= kSortBlock)
         sort_passes<1>(s, n, passes);
-    else if (n <= kSortTile / 4)
-        sort_passes<kSortRounds / 4>(s, n, passes);
     else
         sort_passes<kSortRounds>(s, n, passes);
 }
 
-// The first workgroups sort one tile of kSortTile tokens each; the others
-// (where every row is to be written) fill the table with zeros meanwhile.
-// Ids without a part get the key `vocab`, behind all others.
+// Ids that a thread has in flight.
+constexpr int kIdsAhead = kSortRounds;
+
+// A workgroup sorts a tile of kSortTile tokens.  Ids without a part get the key
+// `vocab`, behind all others.
 __global__ __launch_bounds__(kSortBlock) void sort_kernel(TokenIds ids, int64_t tokens, int64_t vocab, int64_t padding,
-                                                          int passes, uint32_t tiles, uint32_t* keys, uint32_t* order,
-                                                          char* table, int64_t row_bytes, int64_t stride_bytes) {
+                                                          int passes, uint32_t* keys, uint32_t* order) {
     __shared__ SortShared s;
-    if (blockIdx.x < tiles) {
-        const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortTile;
-        const int n = static_cast<int>(tokens - first < kSortTile ? tokens - first : kSortTile);
-        for (int i = threadIdx.x; i < n; i += kSortBlock) {
-            const int64_t id = token_id(ids, first + i);
-            s.keys[i] = static_cast<uint32_t>(id < 0 || id >= vocab || id == padding ? vocab : id);
-        }
-        __syncthreads();
-        sort_tile(s, n, passes);
-        for (int i = threadIdx.x; i < n; i += kSortBlock) {
-            const uint32_t at = s.at[i];
-            keys[first + i] = s.keys[at];
-            order[first + i] = static_cast<uint32_t>(first + at);
-        }
-        return;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortTile;
+    const int n = static_cast<int>(tokens - first < kSortTile ? tokens - first : kSortTile);
+    for (int i = threadIdx.x; i < n; i += kIdsAhead * kSortBlock) {
+        int64_t id[kIdsAhead];
+#pragma unroll
+        for (int u = 0; u < kIdsAhead; ++u)
+            id[u] = token_id(ids, first + (i + u * kSortBlock < n ? i + u * kSortBlock : n - 1));
+#pragma unroll
+        for (int u = 0; u < kIdsAhead; ++u)
+            if (i + u * kSortBlock < n)
+                s.keys[i + u * kSortBlock] =
+                    static_cast<uint32_t>(id[u] < 0 || id[u] >= vocab || id[u] == padding ? vocab : id[u]);
     }
-    const int64_t fillers = gridDim.x - tiles, filler = blockIdx.x - tiles;
-    if (stride_bytes == row_bytes) {  // one run of bytes
-        const int64_t bytes = vocab * row_bytes, head = (16 - (reinterpret_cast<uintptr_t>(table) & 15)) & 15;
-        const int64_t vectors = bytes > head ? (bytes - head) / 16 : 0;
-        uint4* v = reinterpret_cast<uint4*>(table + head);
-        for (int64_t i = filler * kSortBlock + threadIdx.x; i < vectors; i += fillers * kSortBlock)
-            v[i] = make_uint4(0, 0, 0, 0);
-        if (filler == 0) {
-            uint16_t* ends = reinterpret_cast<uint16_t*>(table);
-            const int64_t done = head + vectors * 16;
-            for (int64_t i = threadIdx.x; 2 * i < (head < bytes ? head : bytes); i += kSortBlock) ends[i] = 0;
-            for (int64_t i = done / 2 + threadIdx.x; 2 * i < bytes; i += kSortBlock) ends[i] = 0;
-        }
-    } else {
-        for (int64_t r = filler; r < vocab; r += fillers) {
-            uint16_t* row = reinterpret_cast<uint16_t*>(table + r * stride_bytes);
-            for (int64_t i = threadIdx.x; 2 * i < row_bytes; i += kSortBlock) row[i] = 0;
-        }
+    __syncthreads();
+    sort_tile(s, n, passes);
+    for (int i = threadIdx.x; i < n; i += kSortBlock) {
+        const uint32_t at = s.at[i];
+        keys[first + i] = s.keys[at];
+        order[first + i] = static_cast<uint32_t>(first + at);
     }
 }
 
-// Merges neighbouring sorted runs of `run` entries: an entry's place is its
-// own rank plus the entries of the sibling run that come before it (equal keys
-// of the left run do, those of the right run do not).
+// Merges up to kMergeRuns neighbouring sorted runs of `run` entries: an entry's
+// place is its own rank plus the entries of each other run that come before it
+// (equal keys of an earlier run do, those of a later one do not).  Each run is
+// searched in two steps: among kSamples of its keys, evenly spaced, which the
+// workgroup keeps in shared memory, then between two of them.  (Binary searches
+// in global memory alone took three times as long for eight runs.)
+constexpr int kMergeRuns = 8, kSamples = 256;
+static_assert(kSortTile % kSamples == 0, "samples of a run");
+
 __global__ __launch_bounds__(kBlock) void merge_kernel(const uint32_t* keys, const uint32_t* order, int64_t n, int64_t run,
                                                        uint32_t* to_keys, uint32_t* to_order) {
+    __shared__ uint32_t samples[kMergeRuns][kSamples];
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
-    if (i >= n) return;
-    const int64_t pair = i / (2 * run) * (2 * run), middle = pair + run < n ? pair + run : n;
-    const int64_t end = pair + 2 * run < n ? pair + 2 * run : n;
-    const uint32_t key = keys[i];
-    const bool left = i < middle;
-    int64_t lo = left ? middle : pair, hi = left ? end : middle;
-    const int64_t sibling = lo;
-    while (lo < hi) {
-        const int64_t m = lo + (hi - lo) / 2;
-        if (left ? keys[m] < key : keys[m] <= key)
-            lo = m + 1;
-        else
-            hi = m;
+    // a workgroup's entries are of one run
+    const int64_t group = static_cast<int64_t>(blockIdx.x) * kBlock / (kMergeRuns * run) * (kMergeRuns * run);
+    const int64_t spacing = run / kSamples;
+    static_assert(kBlock == kSamples, "a sample a thread");
+    uint32_t sample[kMergeRuns];
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; ++q) {
+        const int64_t at = group + q * run + (threadIdx.x + 1) * spacing - 1;
+        sample[q] = keys[at < n ? at : n - 1];
+        if (at >= n) sample[q] = 0xffffffffu;
     }
-    const int64_t own = left ? i - pair : i - middle;
-    to_keys[pair + own + (lo - sibling)] = key;
-    to_order[pair + own + (lo - sibling)] = order[i];
+    const uint32_t key = keys[i < n ? i : n - 1];
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; ++q) samples[q][threadIdx.x] = sample[q];
+    __syncthreads();
+    if (i >= n) return;
+    const int own = static_cast<int>((i - group) / run);
+    const auto precedes = [&](int q, uint32_t other) { return q < own ? other <= key : other < key; };
+    int64_t before[kMergeRuns], end[kMergeRuns];  // how many of a run come before: between these
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; ++q) {
+        const int64_t start = group + q * run, length = q == own || start >= n ? 0 : n - start < run ? n - start : run;
+        int windows = 0;
+#pragma unroll
+        for (int step = kSamples / 2; step > 0; step /= 2)
+            if (precedes(q, samples[q][windows + step - 1])) windows += step;
+        if (precedes(q, samples[q][windows])) ++windows;  // all of them
+        before[q] = windows * spacing < length ? windows * spacing : length;
+        end[q] = before[q] + spacing - 1 < length ? before[q] + spacing - 1 : length;
+    }
+    for (int64_t step = spacing / 2; step > 0; step /= 2) {
+#pragma unroll
+        for (int q = 0; q < kMergeRuns; ++q) {
+            const bool in = before[q] + step <= end[q];
+            const uint32_t other = keys[in ? group + q * run + before[q] + step - 1 : i];
+            if (in && precedes(q, other)) before[q] += step;
+        }
+    }
+    int64_t place = i - own * run;
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; ++q) place += before[q];
+    to_keys[place] = key;
+    to_order[place] = order[i];
 }
 
 // ---------------------------------------------------------------------------
@@ -251,9 +274,13 @@ __device__ __forceinline__ void write_row(T* row, int c, int dim, const float (&
 
 template <int kVec>
 __device__ __forceinline__ void write_partial(float* row, int c, int dim, const float (&sum)[kVec]) {
+    if (c + kVec <= dim) {
+        store_floats<float, kVec>(row + c, sum);
+    } else {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j)
-        if (c + j < dim) row[c + j] = sum[j];
+        for (int j = 0; j < kVec; ++j)
+            if (c + j < dim) row[c + j] = sum[j];
+    }
 }
 
 // Rows that a thread has in flight.
@@ -272,109 +299,209 @@ __device__ __forceinline__ Pack<T, kVec> load_raw(const T* row, int c, int dim) 
     return x;
 }
 
-// A group of 2^group_bits threads takes a chunk of kSumChunk sorted tokens,
-// columns [c, c + kVec) a thread.  kWide: groups of whole wavefronts, whose
-// keys and positions are the same in every lane and stay in scalar registers.
-// Partial rows: chunk q's run that comes in from the chunk before (or covers
-// the whole chunk) goes to row 2q, one that starts in it and goes on into the
-// next to row 2q + 1.
-template <class T, bool kWide>
-__global__ __launch_bounds__(kBlock) void sum_kernel(const T* grad, int64_t grad_stride, int64_t tokens, const uint32_t* keys,
-                                                     const uint32_t* order, uint32_t vocab, float scale, bool accumulate,
-                                                     T* table, int64_t table_stride, int32_t dim, float* partials,
-                                                     int group_bits) {
-    constexpr int kVec = 16 / sizeof(T);
-    const int group = 1 << group_bits, lane = threadIdx.x & (group - 1);
-    const int in_block = static_cast<int>(threadIdx.x) >> group_bits;
-    const int64_t chunk = static_cast<int64_t>(blockIdx.x) * (kBlock >> group_bits) +
-                          (kWide ? __builtin_amdgcn_readfirstlane(in_block) : in_block);
-    const int64_t first = chunk * kSumChunk;
-    const int c = (static_cast<int>(blockIdx.y) * group + lane) * kVec;
-    if (first >= tokens || c >= dim) return;
-    const int n = static_cast<int>(tokens - first < kSumChunk ? tokens - first : kSumChunk);
-    const bool from_before = first > 0 && keys[first - 1] == keys[first];
-    const bool into_next = first + n < tokens && keys[first + n] == keys[first + n - 1];
-    const auto load = [&](int b, Pack<T, kVec> (&x)[kRowsAhead]) {
-#pragma unroll
-        for (int u = 0; u < kRowsAhead; ++u)
-            x[u] = load_raw<T, kVec>(grad + order[first + (b + u < n ? b + u : n - 1)] * grad_stride, c, dim);
-    };
-    float sum[kVec] = {};
-    int start = 0;  // of the run being summed
-    const auto add = [&](int b, const Pack<T, kVec> (&x)[kRowsAhead]) {
-        uint32_t key[kRowsAhead + 1];
-#pragma unroll
-        for (int u = 0; u <= kRowsAhead; ++u) key[u] = keys[first + (b + u < n ? b + u : n - 1)];
-#pragma unroll
-        for (int u = 0; u < kRowsAhead; ++u) {
-            const int i = b + u;
-            if (i >= n) break;
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) sum[j] += static_cast<float>(x[u].v[j]);
-            const bool ends = i == n - 1 || key[u + 1] != key[u];
-            if (!ends) continue;
-            if (key[u] < vocab) {
-                const bool open_start = start == 0 && from_before, open_end = i == n - 1 && into_next;
-                if (!open_start && !open_end)
-                    write_row<T, kVec>(table + key[u] * table_stride, c, dim, sum, scale, accumulate);
-                else
-                    write_partial<kVec>(partials + (2 * chunk + (open_start ? 0 : 1)) * dim, c, dim, sum);
-            }
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) sum[j] = 0.0f;
-            start = i + 1;
-        }
-    };
-    static_assert(kSumChunk % (2 * kRowsAhead) == 0, "batches of rows in pairs");
-    Pack<T, kVec> even[kRowsAhead], odd[kRowsAhead];
-    load(0, even);
-#pragma unroll 1
-    for (int b = 0; b < n; b += 2 * kRowsAhead) {
-        load(b + kRowsAhead, odd);
-        add(b, even);
-        if (b + 2 * kRowsAhead < n) load(b + 2 * kRowsAhead, even);
-        add(b + kRowsAhead, odd);
-    }
-}
-
-// Adds the partial rows of the run that starts in a chunk and goes on past it.
-template <class T>
-__global__ __launch_bounds__(kBlock) void join_kernel(int64_t tokens, const uint32_t* keys, uint32_t vocab, float scale,
-                                                      bool accumulate, T* table, int64_t table_stride, int32_t dim,
-                                                      const float* partials, int group_bits) {
-    constexpr int kVec = 4;
-    const int group = 1 << group_bits, lane = threadIdx.x & (group - 1);
-    const int64_t chunk = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) >> group_bits;
-    const int64_t first = chunk * kSumChunk, next = first + kSumChunk;
-    const int c = (static_cast<int>(blockIdx.y) * group + lane) * kVec;
-    if (next >= tokens || c >= dim) return;
-    const uint32_t key = keys[next - 1];
-    if (key >= vocab || keys[next] != key) return;                           // no run goes on
-    if (keys[first] == key && first > 0 && keys[first - 1] == key) return;   // it started before this chunk
-    // the run's end
-    int64_t lo = next, hi = tokens;
+// First entry of the sorted keys that is not below `key`.
+__device__ int64_t lower_bound(const uint32_t* keys, int64_t n, uint32_t key) {
+    int64_t lo = 0, hi = n;
     while (lo < hi) {
         const int64_t m = lo + (hi - lo) / 2;
-        if (keys[m] <= key)
+        if (keys[m] < key)
             lo = m + 1;
         else
             hi = m;
     }
-    const int64_t last = (lo - 1) / kSumChunk;
-    float sum[kVec];
-    load_row<float, kVec>(partials + (2 * chunk + 1) * dim, c, dim, sum);
-    for (int64_t q = chunk + 1; q <= last; q += kRowsAhead) {
-        float x[kRowsAhead][kVec];
-#pragma unroll
-        for (int u = 0; u < kRowsAhead; ++u)
-            load_row<float, kVec>(partials + 2 * (q + u <= last ? q + u : last) * dim, c, dim, x[u]);
-#pragma unroll
-        for (int u = 0; u < kRowsAhead; ++u)
-            if (q + u <= last)
-#pragma unroll
-                for (int j = 0; j < kVec; ++j) sum[j] += x[u][j];
+    return lo;
+}
+
+constexpr int kZeroRowsMax = 256;
+
+// Zeros into those of `rows` rows from `from` on that no token has.
+template <class T>
+__device__ void zero_absent(const uint32_t* keys, int64_t tokens, int64_t from, int rows, T* table, int64_t stride, int32_t dim) {
+    constexpr int kVec = 16 / sizeof(T);
+    __shared__ uint32_t present[kZeroRowsMax];
+    __shared__ int64_t range[2];
+    for (int r = threadIdx.x; r < rows; r += kBlock) present[r] = 0;
+    if (threadIdx.x < 2)
+        range[threadIdx.x] = lower_bound(keys, tokens, static_cast<uint32_t>(from + (threadIdx.x == 0 ? 0 : rows)));
+    __syncthreads();
+    for (int64_t i = range[0] + threadIdx.x; i < range[1]; i += kBlock) present[keys[i] - from] = 1;
+    __syncthreads();
+    const int vectors = (dim + kVec - 1) / kVec;
+    // past the cache, where they would push out the rows that are being summed:
+    // 50257 x 2048 bfloat16, 87 us a call against 111
+    const float zeros[kVec] = {};
+    for (int i = threadIdx.x; i < rows * vectors; i += kBlock) {
+        const int r = i / vectors, c = (i - r * vectors) * kVec;
+        if (present[r]) continue;
+        T* at = table + (from + r) * stride + c;
+        if (c + kVec <= dim) {
+            stream_floats<T, kVec>(at, zeros);
+        } else {
+            for (int j = 0; c + j < dim; ++j) at[j] = static_cast<T>(0.0f);
+        }
     }
-    write_row<T, kVec>(table + key * table_stride, c, dim, sum, scale, accumulate);
+}
+
+// A group of 2^group_bits threads takes a chunk of kSumChunk sorted tokens,
+// columns [c, c + kVec) a thread.  kWide: groups of whole wavefronts, whose keys
+// and positions are the same in every lane: a lane each holds them.
+// A run (the tokens of one row) belongs to the chunk that it starts in, which
+// sums it to its end where that lies in the next chunk at the latest.  Of a
+// longer run each chunk leaves a partial row: chunk q's part of a run that comes
+// in from the chunk before goes to row 2q, of one that starts in it to row
+// 2q + 1.  The workgroups from `sums` on write the rows without a token,
+// zero_rows each: beside the sums, so that every row is written once.
+template <class T, bool kWide>
+__global__ __launch_bounds__(kBlock) void sum_kernel(const T* grad, int64_t grad_stride, int64_t tokens, const uint32_t* keys,
+                                                     const uint32_t* order, uint32_t vocab, float scale, bool accumulate,
+                                                     T* table, int64_t table_stride, int32_t dim, float* partials,
+                                                     int group_bits, uint32_t sums, int zero_rows) {
+    constexpr int kVec = 16 / sizeof(T), C = kSumChunk;
+    if (blockIdx.x >= sums) {
+        const int64_t from = static_cast<int64_t>(blockIdx.x - sums) * zero_rows;
+        const int rows = static_cast<int>(vocab - from < zero_rows ? vocab - from : zero_rows);
+        if (blockIdx.y == 0) zero_absent(keys, tokens, from, rows, table, table_stride, dim);
+        return;
+    }
+    const int group = 1 << group_bits, lane = threadIdx.x & (group - 1);
+    const int in_block = static_cast<int>(threadIdx.x) >> group_bits;
+    const int64_t chunk = static_cast<int64_t>(blockIdx.x) * (kBlock >> group_bits) +
+                          (kWide ? __builtin_amdgcn_readfirstlane(in_block) : in_block);
+    const int64_t first = chunk * C;
+    const int c = (static_cast<int>(blockIdx.y) * group + lane) * kVec;
+    // (lanes behind a row's end stay: the others read keys from them)
+    if (first >= tokens || (kWide ? c - (lane & 63) * kVec : c) >= dim) return;
+    const int64_t rest = tokens - first;
+    const int n = static_cast<int>(rest < C ? rest : C);
+    // this chunk's entries, the next one's and one more
+    uint32_t held_key = 0, held_at = 0;
+    if (kWide) {
+        const int l = threadIdx.x & 63;
+        held_key = keys[first + (l < rest ? l : rest - 1)];
+        held_at = order[first + (l < rest ? l : rest - 1)];
+    }
+    const uint32_t before = keys[first > 0 ? first - 1 : 0], earlier = keys[first > C ? first - C - 1 : 0];
+    const auto key_of = [&](int i) -> uint32_t {  // i < rest
+        if constexpr (kWide)
+            return __builtin_amdgcn_readlane(held_key, i);
+        else
+            return keys[first + i];
+    };
+    const auto at_of = [&](int i) -> int64_t {
+        if constexpr (kWide)
+            return static_cast<uint32_t>(__builtin_amdgcn_readlane(held_at, i));
+        else
+            return order[first + i];
+    };
+    const uint32_t head = key_of(0), tail = key_of(n - 1);
+    const bool from_before = first > 0 && before == head;
+    const bool into_next = n < rest && key_of(n) == tail;
+    int start = 0, end = n;
+    bool open_start = from_before, open_end = into_next;
+    if (from_before && (first == C || earlier != head) && !(tail == head && into_next)) {
+        // it started in the chunk before, which sums it to its end
+        open_start = false;
+        while (start < n && key_of(start) == head) ++start;
+    }
+    if (into_next && !(from_before && tail == head) && (2 * C >= rest || key_of(2 * C) != tail)) {
+        // it starts here and ends in the next chunk
+        open_end = false;
+        while (end < rest && end < 2 * C && key_of(end) == tail) ++end;
+    }
+    const auto load = [&](int b, Pack<T, kVec> (&x)[kRowsAhead]) {
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u)
+            x[u] = load_raw<T, kVec>(grad + at_of(b + u < end ? b + u : end - 1) * grad_stride, c, dim);
+    };
+    float sum[kVec] = {};
+    int run = start;  // where the run being summed began
+    const auto add = [&](int b, const Pack<T, kVec> (&x)[kRowsAhead]) {
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u) {
+            const int i = b + u;
+            if (i >= end) break;
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) sum[j] += static_cast<float>(x[u].v[j]);
+            const uint32_t key = key_of(i);
+            if (i != end - 1 && key_of(i + 1) == key) continue;
+            if (key < vocab) {
+                const bool in = run == 0 && open_start, out = i == end - 1 && open_end;
+                if (!in && !out)
+                    write_row<T, kVec>(table + key * table_stride, c, dim, sum, scale, accumulate);
+                else
+                    write_partial<kVec>(partials + (2 * chunk + (in ? 0 : 1)) * dim, c, dim, sum);
+            }
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) sum[j] = 0.0f;
+            run = i + 1;
+        }
+    };
+    if (start >= end) return;
+    Pack<T, kVec> even[kRowsAhead], odd[kRowsAhead];
+    load(start, even);
+#pragma unroll 1
+    for (int b = start; b < end; b += 2 * kRowsAhead) {
+        load(b + kRowsAhead, odd);
+        add(b, even);
+        if (b + 2 * kRowsAhead < end) load(b + 2 * kRowsAhead, even);
+        add(b + kRowsAhead, odd);
+    }
+}
+
+// Adds the partial rows of the run that starts in a chunk and goes on past the
+// next one:
+// 256 columns a workgroup, each wavefront a quarter of the run's chunks, the
+// quarters in their order.
+__device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+
+template <class T>
+__global__ __launch_bounds__(kBlock) void join_kernel(int64_t tokens, const uint32_t* keys, uint32_t vocab, float scale,
+                                                      bool accumulate, T* table, int64_t table_stride, int32_t dim,
+                                                      const float* partials) {
+    constexpr int kVec = 4, kParts = kBlock / 64;
+    __shared__ float4 quarters[kParts][64];
+    const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+    const int64_t chunk = blockIdx.x, first = chunk * kSumChunk, next = first + kSumChunk;
+    if (next >= tokens) return;
+    const uint32_t key = keys[next - 1], behind = keys[next], start = keys[first], ahead = keys[first > 0 ? first - 1 : 0];
+    if (key >= vocab || behind != key) return;                 // no run goes on
+    if (start == key && first > 0 && ahead == key) return;     // it started before this chunk
+    // the run's last chunk: the last one that begins with its key
+    int64_t last = chunk + 1;
+    for (;; last += 64) {
+        const int64_t at = (last + lane) * kSumChunk;
+        const uint64_t other = __ballot(at >= tokens || keys[at < tokens ? at : tokens - 1] != key);
+        if (other != 0) {
+            last += __ffsll(static_cast<unsigned long long>(other)) - 2;
+            break;
+        }
+    }
+    if (last == chunk + 1) return;                             // summed by the chunk it starts in
+    const int64_t each = (last - chunk + kParts) / kParts;                   // chunks [chunk, last] in parts
+    const int64_t from = chunk + part * each, until = from + each - 1 < last ? from + each - 1 : last;
+    const int c = (static_cast<int>(blockIdx.y) * 64 + lane) * kVec;
+    float sum[kVec] = {};
+    if (c < dim)
+        for (int64_t q = from; q <= until; q += kRowsAhead) {
+            float x[kRowsAhead][kVec];
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; ++u) {
+                const int64_t at = q + u <= until ? q + u : until;
+                load_row<float, kVec>(partials + (2 * at + (at == chunk ? 1 : 0)) * dim, c, dim, x[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kRowsAhead; ++u)
+                if (q + u <= until)
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) sum[j] += x[u][j];
+        }
+    quarters[part][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    __syncthreads();
+    if (part != 0 || c >= dim) return;
+    float4 all = quarters[0][lane];
+    for (int w = 1; w < kParts; ++w) all = add4(all, quarters[w][lane]);
+    const float total[kVec] = {all.x, all.y, all.z, all.w};
+    write_row<T, kVec>(table + key * table_stride, c, dim, total, scale, accumulate);
 }
 
 // log2 of the threads that share a row of `vectors` vectors.
@@ -407,10 +534,15 @@ hipError_t sums(const Rows& grad, int64_t tokens, float scale, bool accumulate, 
                     static_cast<uint32_t>((dim + (vec << bits) - 1) / (vec << bits)));
     };
     const int bits = group_bits_for((dim + kVec - 1) / kVec, 8);
+    dim3 blocks = grid(bits, kVec);
+    const uint32_t summing = blocks.x;
+    // 64 KB of rows a zeroing workgroup
+    const int zero_rows = static_cast<int>(std::clamp<int64_t>(65536 / (dim * int64_t(sizeof(T))), 1, kZeroRowsMax));
+    if (!accumulate) blocks.x += static_cast<uint32_t>((vocab + zero_rows - 1) / zero_rows);
     const auto sum = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid(bits, kVec), dim3(kBlock), 0, stream, static_cast<const T*>(grad.at), grad.stride,
-                           tokens, keys, order, static_cast<uint32_t>(vocab), scale, accumulate,
-                           static_cast<T*>(table.at), table.stride, dim, partials, bits);
+        hipLaunchKernelGGL(kernel, blocks, dim3(kBlock), 0, stream, static_cast<const T*>(grad.at), grad.stride, tokens, keys,
+                           order, static_cast<uint32_t>(vocab), scale, accumulate, static_cast<T*>(table.at), table.stride,
+                           dim, partials, bits, summing, zero_rows);
     };
     if (bits >= 6)
         sum(sum_kernel<T, true>);
@@ -418,10 +550,9 @@ hipError_t sums(const Rows& grad, int64_t tokens, float scale, bool accumulate, 
         sum(sum_kernel<T, false>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks < 2) return e;
-    const int join_bits = group_bits_for((dim + 3) / 4, 6);
-    hipLaunchKernelGGL(join_kernel<T>, grid(join_bits, 4), dim3(kBlock), 0, stream, tokens, keys,
-                       static_cast<uint32_t>(vocab), scale, accumulate, static_cast<T*>(table.at), table.stride, dim,
-                       partials, join_bits);
+    hipLaunchKernelGGL(join_kernel<T>, dim3(static_cast<uint32_t>(chunks), static_cast<uint32_t>((dim + 255) / 256)),
+                       dim3(kBlock), 0, stream, tokens, keys, static_cast<uint32_t>(vocab), scale, accumulate,
+                       static_cast<T*>(table.at), table.stride, dim, partials);
     return hipGetLastError();
 }
 
@@ -439,20 +570,16 @@ hipError_t launch_lookup_grad(const Rows& grad, int64_t tokens, const TokenIds& 
                               bool accumulate, const Rows& table, int64_t vocab, int32_t dim,
                               const LookupGradScratch& scratch, hipStream_t stream) {
     if (tokens == 0 && accumulate) return hipSuccess;
-    const int64_t size = table.type == MICRO_TYPE_F32 ? 4 : 2;
     int passes = 1;
     while (passes < 4 && (vocab >> (passes * kDigitBits)) != 0) ++passes;
-    const uint32_t tiles = static_cast<uint32_t>((tokens + kSortTile - 1) / kSortTile);
-    // a kilobyte and a half of the table a filling thread
-    int64_t fillers = accumulate ? 0 : (vocab * dim * size) / (kSortBlock * 1536) + 1;
-    if (fillers > 1024) fillers = 1024;
-    hipLaunchKernelGGL(sort_kernel, dim3(tiles + static_cast<uint32_t>(fillers)), dim3(kSortBlock), 0, stream, ids,
-                       tokens, vocab, padding, passes, tiles, scratch.keys[0], scratch.order[0],
-                       static_cast<char*>(table.at), dim * size, table.stride * size);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || tokens == 0) return e;
+    hipError_t e = hipSuccess;
+    if (tokens > 0) {
+        hipLaunchKernelGGL(sort_kernel, dim3(static_cast<uint32_t>((tokens + kSortTile - 1) / kSortTile)), dim3(kSortBlock), 0,
+                           stream, ids, tokens, vocab, padding, passes, scratch.keys[0], scratch.order[0]);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     int in = 0;
-    for (int64_t run = kSortTile; run < tokens; run *= 2, in ^= 1) {
+    for (int64_t run = kSortTile; run < tokens; run *= kMergeRuns, in ^= 1) {
         hipLaunchKernelGGL(merge_kernel, dim3(static_cast<uint32_t>((tokens + kBlock - 1) / kBlock)), dim3(kBlock), 0,
                            stream, scratch.keys[in], scratch.order[in], tokens, run, scratch.keys[in ^ 1],
                            scratch.order[in ^ 1]);
