@@ -14,9 +14,14 @@ namespace micro {
 constexpr int kProductDepth = 64;
 // binary32 operands enter the products as the sum of this many bfloat16 ones.
 constexpr int kSplitPlanes = 3;
-// Calls of up to so many tokens take narrow product tiles, and up to so many
-// middle ones.
-constexpr int kFewTokens = 64, kSomeTokens = 512;
+// Tiles of the products, by the call's tokens.  Middle ones (128 x 128, two
+// workgroups a compute unit) up to kSomeTokens: with gradients over 30522 x 1024
+// 100 tokens take 100 us and 300 take 135, in wide tiles (256 x 256, one
+// workgroup) 128 and 145; 512 tokens 162 and 161, over 50257 x 2048 470 and 416.
+// The loss alone of up to kFewTokens takes narrow ones (128 vocabulary rows x 32
+// tokens): it is bound by one read of the table (32 us over 50257 x 2048, 6.5
+// TB/s), which many small workgroups keep going.
+constexpr int kFewTokens = 32, kSomeTokens = 384;
 // Vocabulary rows that share one running maximum: what one wavefront of the
 // score product holds, in wide, middle and narrow tiles.
 constexpr int kGranule = 128, kGranuleSome = 64, kGranuleFew = 32;

@@ -76,7 +76,6 @@ struct Shape {
 using Wide = Shape<2, 4, 4, 2>;
 using Middle = Shape<2, 2, 2, 2>;
 using Narrow32 = Shape<4, 1, 1, 1>;
-using Narrow64 = Shape<4, 1, 1, 2>;
 
 // The tile of an operand in shared memory: kR values of the kept axis by
 // kDepth of k, filled by loads that go from global to shared memory without
@@ -156,7 +155,9 @@ __device__ __forceinline__ void interleave() {
     if constexpr (kAt < kProducts) {
         constexpr int kMma = 0x8, kVectorLoad = 0x20, kSharedRead = 0x100;
         __builtin_amdgcn_sched_group_barrier(kMma, 1, 0);
-        constexpr int reads = (kAt + 1) * kReads / kProducts - kAt * kReads / kProducts;
+        // the reads in the first half, so that the next products do not wait for them
+        constexpr int kHalf = kProducts < 8 ? kProducts : 4, each = (kReads + kHalf - 1) / kHalf;
+        constexpr int reads = kAt * each >= kReads ? 0 : kReads - kAt * each < each ? kReads - kAt * each : each;
         constexpr int loads = (kAt + 1) * kLoads / kProducts - kAt * kLoads / kProducts;
         if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(kVectorLoad, loads, 0);
         if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(kSharedRead, reads, 0);
@@ -1271,8 +1272,7 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
 
 template <class In, class T, class E, int kTerms>
 hipError_t pick(const LossCall& c, hipStream_t stream) {
-    if (c.tokens <= 32) return run<In, T, E, kTerms, Narrow32>(c, stream);
-    if (c.tokens <= kFewTokens) return run<In, T, E, kTerms, Narrow64>(c, stream);
+    if (c.tokens <= kFewTokens && !c.gradients) return run<In, T, E, kTerms, Narrow32>(c, stream);
     if (c.tokens <= kSomeTokens) return run<In, T, E, kTerms, Middle>(c, stream);
     return run<In, T, E, kTerms, Wide>(c, stream);
 }

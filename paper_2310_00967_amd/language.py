@@ -31,10 +31,12 @@ class _Enqueued:
         if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
         self._torch = torch
+        self._tensor = torch.Tensor
         self.device = dev
         self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
         self._raw_stream = self.stream.cuda_stream
         self._handle = None
+        self._index = dev.index
 
     def _open(self):
         if self._handle is None:
@@ -48,11 +50,11 @@ class _Enqueued:
             pass
 
     def _foreign(self):
-        return self._torch.cuda.current_stream(self.device).cuda_stream != self._raw_stream
+        return self._torch.cuda.current_stream(self._index).cuda_stream != self._raw_stream
 
-    def _empty(self, shape, dtype):
+    def _empty(self, shape, dtype, foreign):
         torch = self._torch
-        if self._foreign():
+        if foreign:
             with torch.cuda.stream(self.stream):
                 return torch.empty(shape, dtype=dtype, device=self.device)
         return torch.empty(shape, dtype=dtype, device=self.device)
@@ -60,10 +62,9 @@ class _Enqueued:
     def _used(self, *tensors):
         """Keeps the memory of tensors made on another stream until the
         enqueued work is done."""
-        if self._foreign():
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
 
     def _scalar(self, t, name, dtype):
         if not isinstance(t, self._torch.Tensor) or t.dtype != dtype or t.device != self.device or t.numel() != 1:
@@ -108,17 +109,21 @@ class GradientSet(_Enqueued):
         """The sum of the squares of all values (a float64 device scalar):
         what workers that hold parts of one model add up before clipping."""
         handle = self._open()
-        out = self._empty((), self._torch.float64)
+        foreign = self._foreign()
+        out = self._empty((), self._torch.float64, foreign)
         _lib.check(self._norm_fn(handle, out.data_ptr(), None))
-        self._used(*self.tensors)
+        if foreign:
+            self._used(*self.tensors)
         return out
 
     def norm(self):
         """The global L2 norm (a float32 device scalar)."""
         handle = self._open()
-        out = self._empty((), self._torch.float32)
+        foreign = self._foreign()
+        out = self._empty((), self._torch.float32, foreign)
         _lib.check(self._norm_fn(handle, None, out.data_ptr()))
-        self._used(*self.tensors)
+        if foreign:
+            self._used(*self.tensors)
         return out
 
     def clip_(self, max_norm, sumsq=None):
@@ -126,10 +131,12 @@ class GradientSet(_Enqueued):
         Returns the norm before clipping (a float32 device scalar).  sumsq: the
         squared norm to clip by, where other workers hold parts of the model."""
         handle = self._open()
+        foreign = self._foreign()
         other = None if sumsq is None else self._scalar(sumsq, "sumsq", self._torch.float64)
-        norm = self._empty((), self._torch.float32)
+        norm = self._empty((), self._torch.float32, foreign)
         _lib.check(self._clip_fn(handle, float(max_norm), other, norm.data_ptr()))
-        self._used(sumsq, *self.tensors)
+        if foreign:
+            self._used(sumsq, *self.tensors)
         return norm
 
     def flatten(self, flat, max_norm=None, sumsq=None):
@@ -138,6 +145,7 @@ class GradientSet(_Enqueued):
         device scalar); without max_norm the values are only converted, and None
         is returned."""
         handle = self._open()
+        foreign = self._foreign()
         if not isinstance(flat, self._torch.Tensor) or flat.dtype != self._torch.float32 \
                 or flat.device != self.device or not flat.is_contiguous():
             raise TypeError(f"flat must be a contiguous float32 tensor on {self.device}")
@@ -147,12 +155,14 @@ class GradientSet(_Enqueued):
             if sumsq is not None:
                 raise ValueError("sumsq without max_norm")
             _lib.check(self._flatten_fn(handle, math.inf, None, flat.data_ptr(), None))
-            self._used(flat, *self.tensors)
+            if foreign:
+                self._used(flat, *self.tensors)
             return None
         other = None if sumsq is None else self._scalar(sumsq, "sumsq", self._torch.float64)
-        norm = self._empty((), self._torch.float32)
+        norm = self._empty((), self._torch.float32, foreign)
         _lib.check(self._flatten_fn(handle, float(max_norm), other, flat.data_ptr(), norm.data_ptr()))
-        self._used(flat, sumsq, *self.tensors)
+        if foreign:
+            self._used(flat, sumsq, *self.tensors)
         return norm
 
 
@@ -197,14 +207,14 @@ class TokenTable(_Enqueued):
             self._handle = None
 
     def _ids(self, t, name):
-        if not isinstance(t, self._torch.Tensor) or t.dtype not in self._ids_types or t.device != self.device \
-                or not t.is_contiguous():
+        if not isinstance(t, self._tensor) or t.dtype not in self._ids_types or not t.is_cuda \
+                or t.get_device() != self._index or not t.is_contiguous():
             raise TypeError(f"{name} must be a contiguous int32 or int64 tensor on {self.device}")
         return t.data_ptr(), self._ids_types[t.dtype], t.numel()
 
     def _rows(self, t, name, rows):
         """(address, row stride) of `rows` rows of dim values."""
-        if not isinstance(t, self._torch.Tensor) or t.dtype != self.dtype or t.device != self.device:
+        if not isinstance(t, self._tensor) or t.dtype is not self.dtype or not t.is_cuda or t.get_device() != self._index:
             raise TypeError(f"{name} must be a {self.dtype} tensor on {self.device}")
         if t.dim() < 1 or t.shape[-1] != self.dim or t.numel() != rows * self.dim:
             raise ValueError(f"{name} must hold {rows} rows of {self.dim} values")
@@ -218,15 +228,17 @@ class TokenTable(_Enqueued):
         """scale * weight[ids], of the shape of ids with dim behind it.  An id
         outside the table gives a row of NaN."""
         handle = self._open()
+        foreign = self._foreign()
         at, kind, tokens = self._ids(ids, "ids")
         w, w_stride = self._rows(weight, "weight", self.vocab)
         if out is None:
-            out = self._empty((*ids.shape, self.dim), self.dtype)
+            out = self._empty((*ids.shape, self.dim), self.dtype, foreign)
         o, o_stride = self._rows(out, "out", tokens)
         st = self._lookup_fn(handle, w, w_stride, at, kind, tokens, float(scale), o, o_stride)
         if st:
             _lib.check(st)
-        self._used(weight, ids, out)
+        if foreign:
+            self._used(weight, ids, out)
         return out
 
     def lookup_grad(self, grad, ids, dweight, scale=1.0, accumulate=False):
@@ -235,6 +247,7 @@ class TokenTable(_Enqueued):
         to dweight (rows without a token stay as they are); otherwise every row
         is written.  Returns dweight."""
         handle = self._open()
+        foreign = self._foreign()
         at, kind, tokens = self._ids(ids, "ids")
         g, g_stride = self._rows(grad, "grad", tokens)
         d, d_stride = self._rows(dweight, "dweight", self.vocab)
@@ -242,7 +255,8 @@ class TokenTable(_Enqueued):
                                   d_stride)
         if st:
             _lib.check(st)
-        self._used(grad, ids, dweight)
+        if foreign:
+            self._used(grad, ids, dweight)
         return dweight
 
     @staticmethod
@@ -257,17 +271,19 @@ class TokenTable(_Enqueued):
         float32 device scalar) and every token's loss (float32, of the shape of
         targets; 0 where a token does not count)."""
         handle = self._open()
+        foreign = self._foreign()
         mean = self._mean(reduction)
         at, kind, tokens = self._ids(targets, "targets")
         h, h_stride = self._rows(hidden, "hidden", tokens)
         w, w_stride = self._rows(weight, "weight", self.vocab)
-        losses = self._empty(targets.shape, self._torch.float32)
-        loss = self._empty((), self._torch.float32)
+        losses = self._empty(targets.shape, self._torch.float32, foreign)
+        loss = self._empty((), self._torch.float32, foreign)
         st = self._loss_fn(handle, h, h_stride, w, w_stride, at, kind, tokens, mean, losses.data_ptr(),
                            loss.data_ptr())
         if st:
             _lib.check(st)
-        self._used(hidden, weight, targets)
+        if foreign:
+            self._used(hidden, weight, targets)
         return loss, losses
 
     def loss_grad(self, hidden, weight, targets, scale=1.0, reduction="mean", dhidden=None, dweight=None,
@@ -276,6 +292,7 @@ class TokenTable(_Enqueued):
         dhidden, dweight); given tensors are written, accumulate adds to the
         given dweight.  The losses are not scaled."""
         handle = self._open()
+        foreign = self._foreign()
         mean = self._mean(reduction)
         at, kind, tokens = self._ids(targets, "targets")
         h, h_stride = self._rows(hidden, "hidden", tokens)
@@ -283,17 +300,18 @@ class TokenTable(_Enqueued):
         if accumulate and dweight is None:
             raise ValueError("accumulate needs the dweight to add to")
         if dhidden is None:
-            dhidden = self._empty(hidden.shape, self.dtype)
+            dhidden = self._empty(hidden.shape, self.dtype, foreign)
         if dweight is None:
-            dweight = self._empty((self.vocab, self.dim), self.dtype)
+            dweight = self._empty((self.vocab, self.dim), self.dtype, foreign)
         dh, dh_stride = self._rows(dhidden, "dhidden", tokens)
         dw, dw_stride = self._rows(dweight, "dweight", self.vocab)
-        losses = self._empty(targets.shape, self._torch.float32)
-        loss = self._empty((), self._torch.float32)
+        losses = self._empty(targets.shape, self._torch.float32, foreign)
+        loss = self._empty((), self._torch.float32, foreign)
         st = self._loss_grad_fn(handle, h, h_stride, w, w_stride, at, kind, tokens, mean, float(scale),
                                 1 if accumulate else 0, losses.data_ptr(), loss.data_ptr(), dh, dh_stride, dw,
                                 dw_stride)
         if st:
             _lib.check(st)
-        self._used(hidden, weight, targets, dhidden, dweight)
+        if foreign:
+            self._used(hidden, weight, targets, dhidden, dweight)
         return loss, losses, dhidden, dweight
