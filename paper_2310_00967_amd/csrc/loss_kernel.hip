@@ -1241,7 +1241,8 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (!c.gradients) continue;
         const uint32_t turns = ceil_div(c.vocab_padded, kTurnBlock * (16 / int(sizeof(E))));
-        const uint32_t turn_rows = ceil_div((most + kDepth - 1) / kDepth * kDepth, kTurnRows);
+        // (a grid's second dimension ends at 65535; the kernel goes on by its size)
+        const uint32_t turn_rows = std::min<uint32_t>(ceil_div((most + kDepth - 1) / kDepth * kDepth, kTurnRows), 32768);
         hipLaunchKernelGGL((gradient_kernel<E, T>), dim3(turns, turn_rows), dim3(kTurnBlock), 0, stream, c.count, first,
                            block, static_cast<E*>(c.scores), c.vocab_padded, c.stats, granule, c.softmax, c.counted_losses,
                            c.labels, static_cast<T*>(c.split));

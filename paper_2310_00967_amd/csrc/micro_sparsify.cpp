@@ -156,7 +156,10 @@ void micro::set_thread_error(const char* fmt, ...) {
     va_start(ap, fmt);
     std::vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    g_init_error = buf;
+    try {
+        g_init_error = buf;
+    } catch (...) {  // no memory for the message: the last one stays
+    }
 }
 
 namespace {

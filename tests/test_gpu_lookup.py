@@ -78,7 +78,8 @@ def test_lookup_past_32_bit_offsets():
 GRAD_CASES = [(1, 1, 1, "uniform"), (5, 3, 2, "uniform"), (10, 64, 31, "one"), (10, 64, 32, "one"), (10, 64, 33, "one"),
               (300, 77, 1000, "skewed"), (257, 128, 4097, "skewed"), (70_000, 16, 5000, "uniform"), (3, 40, 20_000, "one"),
               (1000, 24, 16_384, "skewed"), (1000, 24, 16_385, "skewed"), (65_537, 8, 70_001, "skewed"),
-              (200, 2056, 300, "skewed")]
+              (200, 2056, 300, "skewed"), (5000, 4, 4096, "skewed"), (5000, 4, 4097, "uniform"), (900, 4, 32_769, "skewed"),
+              (70_000, 3, 300_001, "skewed"), (100, 64, 47, "one"), (100, 64, 48, "one"), (100, 64, 49, "one")]
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -100,6 +100,51 @@ def test_several_token_blocks(dtype, counted):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [257, 300, 384, 385])
+def test_short_calls_of_several_token_blocks(dtype, tokens):
+    """Blocks of 256 tokens at lengths on both sides of where the tiles change."""
+    table = micro.TokenTable(200, 72, tokens, dtype=dtype, score_bytes=1)
+    check(table, *make(200, 72, tokens, dtype, counted=0.95), scale=8.0)
+
+
+def chunked(hidden, weight, targets, rows):
+    """Losses of all tokens in 64 bits on the GPU, dhidden of the last tokens and
+    dweight of the given rows, in chunks of tokens (sum reduction)."""
+    h, w = hidden.double(), weight.double()
+    losses, dw = [], torch.zeros(len(rows), w.shape[1], dtype=torch.float64, device=DEV)
+    for a in range(0, h.shape[0], 4096):
+        y = targets[a:a + 4096]
+        logp = torch.log_softmax(h[a:a + 4096] @ w.t().contiguous(), 1)
+        losses.append(-logp.gather(1, y[:, None]).flatten())
+        g = logp[:, rows].exp() - (y[:, None] == rows[None, :]).double()
+        dw += g.t().contiguous() @ h[a:a + 4096]
+    g = logp.exp()
+    g[torch.arange(y.numel(), device=DEV), y] -= 1.0
+    return torch.cat(losses), g @ w, dw
+
+
+@pytest.mark.parametrize("vocab,dim,tokens,score_bytes", [(65_537, 64, 66_000, 9 << 30),  # 4.3e9 scores in one block
+                                                          (40, 8, 1_200_000, 2 << 30)])  # more rows than a grid's y
+def test_offsets_and_grids_past_their_limits(vocab, dim, tokens, score_bytes):
+    """Against 64 bits to 2% of the largest gradient (each value carries three
+    roundings of 2^-8; a wrong offset is off by all of it), losses to 1e-4."""
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    weight = torch.randn(vocab, dim, generator=gen, device=DEV).mul_(dim ** -0.5).bfloat16()
+    hidden = torch.randn(tokens, dim, generator=gen, device=DEV).bfloat16()
+    targets = torch.randint(0, vocab, (tokens,), generator=gen, device=DEV)
+    table = micro.TokenTable(vocab, dim, tokens, dtype=BF16, score_bytes=score_bytes)
+    loss, losses, dh, dw = table.loss_grad(hidden, weight, targets, reduction="sum")
+    rows = torch.tensor([0, 1, vocab // 2, vocab - 2, vocab - 1], device=DEV)
+    want, want_h, want_w = chunked(hidden, weight, targets, rows)
+    assert float((losses.double() - want).abs().max()) <= 1e-4
+    assert abs(float(loss) / float(want.sum()) - 1) <= 1e-6
+    last = want_h.shape[0]
+    assert float((dh[-last:].double() - want_h).abs().max()) <= 0.02 * float(want_h.abs().max())
+    assert float((dw[rows].double() - want_w).abs().max()) <= 0.02 * float(want_w.abs().max())
+    table.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_calls_of_different_lengths_on_one_handle(dtype):
     table = micro.TokenTable(400, 64, 900, dtype=dtype, score_bytes=400 * 2 * 512)
     for tokens in (900, 1, 33, 513, 64, 0, 256, 300, 20):
