@@ -429,7 +429,7 @@ MICRO_API void micro_sparsify_free(micro_ctx *ctx);
  * tensors stay where they are until micro_grads_free.  No two may share
  * memory.  `tensors`, `sizes` and `types` are host arrays of `count` entries,
  * read during the call, which waits for its upload.  Device scratch: 16 KB and
- * 32 bytes per 4,096 to 32,768 values.
+ * 24 bytes per 4,096 to 32,768 values.
  */
 typedef struct micro_grads micro_grads; /* opaque, owned by the library */
 MICRO_API micro_status micro_grads_init(micro_grads **grads, int32_t count, void *const *tensors,
@@ -497,7 +497,7 @@ MICRO_API void micro_table_config_default(micro_table_config *cfg);
  * (a lookup nothing; its gradient 16 bytes and dim/2 bytes a token; the loss a
  * padded copy of the hidden rows, and of the table where it cannot be read in
  * place: binary32, a dim that is no multiple of 64, or rows that are not
- * aligned to 16 bytes; its gradients the block's scores and 64 MB).
+ * aligned to 16 bytes; its gradients the block's scores and 128 MB).
  * MICRO_ERANGE for vocab above 2^31 - 2, dim above 65536 or max_tokens above
  * 2^22; MICRO_EINVAL for vocab < 1, dim < 1, max_tokens < 0 or an unknown
  * type.

