@@ -121,15 +121,15 @@ def load():
     return _lib
 
 
-def load_caller():
-    """The native marshalling's Caller type (never builds it)."""
+def load_caller(name="Caller"):
+    """A type of the native marshalling: Caller or TableCaller (never builds it)."""
     import torch  # noqa: F401  (its libraries before the module that links to them)
     try:
-        from ._caller import Caller
+        from . import _caller
     except ImportError as e:
         raise RuntimeError(f"the binding's native part is not built or not loadable ({e}); run "
                            "__graft_entry__.build() or python -m paper_2310_00967_amd.build") from e
-    return Caller
+    return getattr(_caller, name)
 
 
 def status_string(status):

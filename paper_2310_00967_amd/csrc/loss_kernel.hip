@@ -581,8 +581,13 @@ __global__ __launch_bounds__(kRowBlock) void gather_kernel(const In* hidden, int
         }
     } else if (t < end) {
         if (lane == 0) out.losses[t] = own == targets.ignored ? 0.0f : __builtin_nanf("");
-        if (dhidden)
-            for (int c = lane; c < dim; c += 64) dhidden[t * dstride + c] = static_cast<In>(0.0f);
+        if (dhidden) {
+            constexpr int kVec = 16 / sizeof(In);
+            In* row = dhidden + t * dstride;
+            int c = lane * kVec;
+            for (; c + kVec <= dim; c += 64 * kVec) *reinterpret_cast<Pack<In, kVec>*>(row + c) = Pack<In, kVec>{};
+            for (; c < dim && c + kVec > dim; ++c) row[c] = static_cast<In>(0.0f);
+        }
     }
     if (first + kGathered < targets.tokens) return;
     const int32_t n = before + __popc(mine);

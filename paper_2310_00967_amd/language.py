@@ -199,10 +199,15 @@ class TokenTable(_Enqueued):
         lib = _lib.load()
         self._lookup_fn, self._lookup_grad_fn = lib.micro_table_lookup, lib.micro_table_lookup_grad
         self._loss_fn, self._loss_grad_fn = lib.micro_table_loss, lib.micro_table_loss_grad
+        # the native marshalling of the lookup's plain case
+        self._caller = _lib.load_caller("TableCaller")(
+            ctypes.cast(self._lookup_fn, ctypes.c_void_p).value, self._handle.value, self.vocab, self.dim,
+            types[self.dtype], self._index, self.stream.stream_id)
         self._ids_types = {torch.int32: _lib.MICRO_IDS_I32, torch.int64: _lib.MICRO_IDS_I64}
 
     def close(self):
         if getattr(self, "_handle", None) is not None:
+            self._caller = None
             _lib.micro_table_free(self._handle)
             self._handle = None
 
@@ -228,6 +233,12 @@ class TokenTable(_Enqueued):
         """scale * weight[ids], of the shape of ids with dim behind it.  An id
         outside the table gives a row of NaN."""
         handle = self._open()
+        if out is None:
+            done = self._caller.lookup(weight, ids, scale)
+            if isinstance(done, self._tensor):
+                return done
+            if done is not None:
+                _lib.check(done)
         foreign = self._foreign()
         at, kind, tokens = self._ids(ids, "ids")
         w, w_stride = self._rows(weight, "weight", self.vocab)
