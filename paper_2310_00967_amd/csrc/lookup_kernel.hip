@@ -346,16 +346,18 @@ __device__ void zero_absent(const uint32_t* keys, int64_t tokens, int64_t from, 
     }
 }
 
-// A group of 2^group_bits threads takes a chunk of kSumChunk sorted tokens,
-// columns [c, c + kVec) a thread.  kWide: groups of whole wavefronts, whose keys
-// and positions are the same in every lane: a lane each holds them.
+// A group of 2^group_bits threads, whole wavefronts, takes a chunk of kSumChunk
+// sorted tokens, columns [c, c + kVec) a thread.  Keys and positions are the same
+// for a wavefront: a lane each holds them.  (Narrow rows leave lanes idle; groups
+// of fewer lanes, which had to load every key, took 40 us for a whole call of
+// 8190 tokens by 192 against 36.)
 // A run (the tokens of one row) belongs to the chunk that it starts in, which
 // sums it to its end where that lies in the next chunk at the latest.  Of a
 // longer run each chunk leaves a partial row: chunk q's part of a run that comes
 // in from the chunk before goes to row 2q, of one that starts in it to row
 // 2q + 1.  The workgroups from `sums` on write the rows without a token,
 // zero_rows each: beside the sums, so that every row is written once.
-template <class T, bool kWide>
+template <class T>
 __global__ __launch_bounds__(kBlock) void sum_kernel(const T* grad, int64_t grad_stride, int64_t tokens, const uint32_t* keys,
                                                      const uint32_t* order, uint32_t vocab, float scale, bool accumulate,
                                                      T* table, int64_t table_stride, int32_t dim, float* partials,
@@ -370,33 +372,21 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(const T* grad, int64_t grad
     const int group = 1 << group_bits, lane = threadIdx.x & (group - 1);
     const int in_block = static_cast<int>(threadIdx.x) >> group_bits;
     const int64_t chunk = static_cast<int64_t>(blockIdx.x) * (kBlock >> group_bits) +
-                          (kWide ? __builtin_amdgcn_readfirstlane(in_block) : in_block);
+                          __builtin_amdgcn_readfirstlane(in_block);
     const int64_t first = chunk * C;
     const int c = (static_cast<int>(blockIdx.y) * group + lane) * kVec;
     // (lanes behind a row's end stay: the others read keys from them)
-    if (first >= tokens || (kWide ? c - (lane & 63) * kVec : c) >= dim) return;
+    if (first >= tokens || c - (lane & 63) * kVec >= dim) return;
     const int64_t rest = tokens - first;
     const int n = static_cast<int>(rest < C ? rest : C);
     // this chunk's entries, the next one's and one more
-    uint32_t held_key = 0, held_at = 0;
-    if (kWide) {
-        const int l = threadIdx.x & 63;
-        held_key = keys[first + (l < rest ? l : rest - 1)];
-        held_at = order[first + (l < rest ? l : rest - 1)];
-    }
+    const int l = threadIdx.x & 63;
+    const uint32_t held_key = keys[first + (l < rest ? l : rest - 1)];
+    const uint32_t held_at = order[first + (l < rest ? l : rest - 1)];
     const uint32_t before = keys[first > 0 ? first - 1 : 0], earlier = keys[first > C ? first - C - 1 : 0];
-    const auto key_of = [&](int i) -> uint32_t {  // i < rest
-        if constexpr (kWide)
-            return __builtin_amdgcn_readlane(held_key, i);
-        else
-            return keys[first + i];
-    };
-    const auto at_of = [&](int i) -> int64_t {
-        if constexpr (kWide)
-            return static_cast<uint32_t>(__builtin_amdgcn_readlane(held_at, i));
-        else
-            return order[first + i];
-    };
+    static_assert(2 * C < 64, "a lane an entry");
+    const auto key_of = [&](int i) -> uint32_t { return __builtin_amdgcn_readlane(held_key, i); };  // i < rest
+    const auto at_of = [&](int i) -> int64_t { return static_cast<uint32_t>(__builtin_amdgcn_readlane(held_at, i)); };
     const uint32_t head = key_of(0), tail = key_of(n - 1);
     const bool from_before = first > 0 && before == head;
     const bool into_next = n < rest && key_of(n) == tail;
@@ -537,7 +527,7 @@ hipError_t sums(const Rows& grad, int64_t tokens, float scale, bool accumulate, 
         return dim3(static_cast<uint32_t>((chunks + per_block - 1) / per_block),
                     static_cast<uint32_t>((dim + (vec << bits) - 1) / (vec << bits)));
     };
-    const int bits = group_bits_for((dim + kVec - 1) / kVec, 8);
+    const int bits = std::max(group_bits_for((dim + kVec - 1) / kVec, 8), 6);
     dim3 blocks = grid(bits, kVec);
     const uint32_t summing = blocks.x;
     // 64 KB of rows a zeroing workgroup
@@ -548,10 +538,7 @@ hipError_t sums(const Rows& grad, int64_t tokens, float scale, bool accumulate, 
                            order, static_cast<uint32_t>(vocab), scale, accumulate, static_cast<T*>(table.at), table.stride,
                            dim, partials, bits, summing, zero_rows);
     };
-    if (bits >= 6)
-        sum(sum_kernel<T, true>);
-    else
-        sum(sum_kernel<T, false>);
+    sum(sum_kernel<T>);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks < 2) return e;
     hipLaunchKernelGGL(join_kernel<T>, dim3(static_cast<uint32_t>(chunks), static_cast<uint32_t>((dim + 255) / 256)),
