@@ -494,10 +494,10 @@ MICRO_API void micro_table_config_default(micro_table_config *cfg);
  * A handle for a table of vocab x dim values of `type` and calls of up to
  * max_tokens tokens, enqueuing on hip_stream; cfg NULL: the defaults.  Holds
  * no scratch yet: the first call of each kind allocates what its kind needs
- * (a lookup nothing; its gradient 16 bytes and dim/2 bytes a token; the loss a
- * padded copy of the hidden rows, and of the table where it cannot be read in
- * place: binary32, a dim that is no multiple of 64, or rows that are not
- * aligned to 16 bytes; its gradients the block's scores and 128 MB).
+ * (a lookup nothing; its gradient 16 bytes and dim/2 bytes a token; the loss
+ * 32 MB, a padded copy of the hidden rows, and one of the table where it cannot
+ * be read in place: binary32, a dim that is no multiple of 64, or rows that are
+ * not aligned to 16 bytes; its gradients the block's scores and 128 MB).
  * MICRO_ERANGE for vocab above 2^31 - 2, dim above 65536 or max_tokens above
  * 2^22; MICRO_EINVAL for vocab < 1, dim < 1, max_tokens < 0 or an unknown
  * type.

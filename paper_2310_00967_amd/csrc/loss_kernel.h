@@ -57,6 +57,7 @@ struct LossCall {
     float2* softmax;         // (maximum, 1 / sum of exponentials) of [B]
     void* scores;            // exponentials, then logit gradients, [B][Vp]; binary32: floats
     void* split;             // binary32: the logit gradients as [P][B][Vp] bfloat16
+    float* parts;            // parts of a short call's scores cut along the sum: two of its tiles per compute unit
     float* partials;         // parts of the two gradient products cut along the sum: a wide tile per compute unit each
     float* carried;          // wide tiles of dtable between token blocks; null with one block
     int compute_units;
@@ -67,7 +68,7 @@ bool table_in_place(const LossCall& c);
 
 hipError_t launch_loss(const LossCall& call, hipStream_t stream);
 
-// Floats of one wide product tile.
-constexpr int64_t kWideTile = 256 * 256;
+// Floats of one wide product tile, and of a short call's largest.
+constexpr int64_t kWideTile = 256 * 256, kPartTile = 128 * 128;
 
 }  // namespace micro

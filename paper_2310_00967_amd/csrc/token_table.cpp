@@ -148,6 +148,7 @@ micro_status loss_scratch(micro_table* t, bool copy_table, bool gradients) {
             p.take(c.softmax, c.block * 8);
             p.take(c.stats, granules * 8);
             p.take(c.h, planes * tokens * dim * 2);
+            p.take(c.parts, 2 * t->compute_units * kPartTile * 4);
         }))
         return st;
     if (copy_table)

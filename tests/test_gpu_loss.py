@@ -160,6 +160,16 @@ def test_a_product_of_few_tiles_is_split_along_the_sum(dtype, tokens):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,dim,tokens,counted", [(129, 1024, 1, 1.0), (1549, 2304, 7, 1.0), (700, 1100, 32, 0.1),
+                                                      (1000, 1500, 33, 1.0), (640, 2000, 200, 0.3), (300, 4096, 384, 1.0),
+                                                      (900, 1024, 90, 0.0)])
+def test_scores_of_few_tiles_are_split_along_the_width(dtype, vocab, dim, tokens, counted):
+    table = micro.TokenTable(vocab, dim, tokens, dtype=dtype)
+    check(table, *make(vocab, dim, tokens, dtype, counted=counted), scale=32.0)
+    table.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_strided_rows_and_shapes(dtype):
     hidden, weight, targets = make(90, 64, 60, dtype)
     table = micro.TokenTable(90, 64, 60, dtype=dtype)
