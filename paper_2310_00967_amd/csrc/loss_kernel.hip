@@ -783,7 +783,8 @@ __device__ __forceinline__ void finish_scores(const ScoreOut& out, int64_t n, MI
 // the table, 30 us for 206 MB (6.9 TB/s).  kCut: a short call over few tiles,
 // whose tiles are cut along the sum and left for the join, since a step of one
 // tile waits for its loads: whole calls of 7 tokens, 1549 x 2304, with gradients
-// in 127 us for 237 (binary32) and 58 for 66 (bfloat16).
+// in 127 us for 237 (binary32, 101 since the gradients' parts count its six
+// products' steps) and 58 for 66 (bfloat16).
 template <class S, class T, class E, int kTerms, bool kCut>
 __global__ __launch_bounds__(S::kThreads) void scores_kernel(Operand table, Operand h, int64_t blocks, ScoreOut out) {
     MICRO_STAGES(S);
@@ -1050,6 +1051,7 @@ struct GradientOut {
     bool accumulate;
     float* partials;           // one tile a workgroup of the grid
     float* carried;
+    int terms;                 // of the products
 };
 
 struct GradientPlan {
@@ -1070,7 +1072,7 @@ __device__ GradientPlan gradient_plan(const GradientOut& o) {
     p.tiles_a = (o.dim + S::kA - 1) / S::kA;
     p.tiles_b = (columns + S::kB - 1) / S::kB;
     p.blocks = ((o.table ? p.n : o.vocab) + kDepth - 1) / kDepth;
-    p.most_splits = p.blocks / 8;  // a part shorter than that is not worth its partial tile
+    p.most_splits = o.terms * p.blocks / 8;  // a part of fewer steps is not worth its partial tile
     return p;
 }
 
@@ -1356,7 +1358,7 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         // g as the operand of both products
         Operand g{kSplit ? c.split : c.scores, c.vocab_padded, 0, 0, block * c.vocab_padded};
         GradientOut o{c.count, first, block, false, c.vocab, c.dim, c.rows, c.scale, c.mean, kHeldUnit<T>,
-                      c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried};
+                      c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried, kTerms};
         Operand wide{table.at, table.stride, c.dim_padded, c.vocab, table.plane};
         hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o, o);
         const GradientOut of_hidden = o;  // its split tiles are joined by the next product's workgroups
