@@ -184,6 +184,65 @@ __global__ __launch_bounds__(kSortBlock) void sort_kernel(TokenIds ids, int64_t 
     }
 }
 
+// The same order for calls of up to kMostRanked tokens, by many workgroups: each
+// takes kRanked tokens of a tile and counts the keys of the tile that come before
+// each (smaller ones, and equal ones at earlier positions), kRankLanes lanes a
+// token and a sixteenth of the keys a wavefront.  More work than the sort, but
+// without its chain of passes: whole calls of 3851 tokens by 144 took 19.8 us for
+// 24.7, of 8190 by 192 32.6 for 36.2; at 16384 tokens it is 0.9 us slower.
+constexpr int kRanked = 16, kRankLanes = 64 / kRanked;
+constexpr int64_t kMostRanked = 8192;
+static_assert(kSortTile % (kSortWaves * kRankLanes * 4) == 0 && kSortTile % kRanked == 0, "four keys a lane a step");
+
+__global__ __launch_bounds__(kSortBlock) void rank_kernel(TokenIds ids, int64_t tokens, int64_t vocab, int64_t padding,
+                                                          uint32_t* keys, uint32_t* order) {
+    using Keys = uint32_t __attribute__((ext_vector_type(4)));
+    __shared__ __attribute__((aligned(16))) uint32_t tile[kSortTile];
+    __shared__ uint32_t counts[kSortWaves][64];
+    const int64_t of_block = static_cast<int64_t>(blockIdx.x) * kRanked, first = of_block / kSortTile * kSortTile;
+    const int n = static_cast<int>(tokens - first < kSortTile ? tokens - first : kSortTile);
+    constexpr int kStep = kSortWaves * kRankLanes * 4;  // keys
+    const int steps = (n + kStep - 1) / kStep;          // of every wavefront
+    int64_t id[kSortRounds];
+#pragma unroll
+    for (int u = 0; u < kSortRounds; ++u) {
+        const int i = threadIdx.x + u * kSortBlock;
+        id[u] = token_id(ids, first + (i < n ? i : n - 1));
+    }
+#pragma unroll
+    for (int u = 0; u < kSortRounds; ++u) {
+        const int i = threadIdx.x + u * kSortBlock;
+        // (places behind the last token come before no key)
+        tile[i] = i >= n ? 0xffffffffu : static_cast<uint32_t>(id[u] < 0 || id[u] >= vocab || id[u] == padding ? vocab : id[u]);
+    }
+    __syncthreads();
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int at = static_cast<int>(of_block - first) + lane % kRanked;
+    const uint32_t key = tile[at];
+    uint32_t before = 0;
+#pragma unroll 4
+    for (int s = 0; s < steps; ++s) {
+        const int j = ((wave * steps + s) * kRankLanes + lane / kRanked) * 4;
+        const Keys other = *reinterpret_cast<const Keys*>(tile + j);
+        const uint32_t bound = key + (j + 3 < at);  // (keys end below 2^31)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) before += other[u] < bound;
+        if (static_cast<uint32_t>(at - j) < 4)
+#pragma unroll
+            for (int u = 0; u < 3; ++u) before += j + u < at && other[u] == key;
+    }
+    counts[wave][lane] = before;
+    __syncthreads();
+    if (threadIdx.x >= kRanked || at >= n) return;
+    uint32_t rank = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w)
+#pragma unroll
+        for (int l = 0; l < kRankLanes; ++l) rank += counts[w][l * kRanked + lane];
+    keys[first + rank] = key;
+    order[first + rank] = static_cast<uint32_t>(first + at);
+}
+
 // Merges up to kMergeRuns neighbouring sorted runs of `run` entries: an entry's
 // place is its own rank plus the entries of each other run that come before it
 // (equal keys of an earlier run do, those of a later one do not).  Each run is
@@ -564,7 +623,11 @@ hipError_t launch_lookup_grad(const Rows& grad, int64_t tokens, const TokenIds& 
     int passes = 1;
     while (passes < 4 && (vocab >> (passes * kDigitBits)) != 0) ++passes;
     hipError_t e = hipSuccess;
-    if (tokens > 0) {
+    if (tokens > 0 && tokens <= kMostRanked) {
+        hipLaunchKernelGGL(rank_kernel, dim3(static_cast<uint32_t>((tokens + kRanked - 1) / kRanked)), dim3(kSortBlock), 0,
+                           stream, ids, tokens, vocab, padding, scratch.keys[0], scratch.order[0]);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else if (tokens > 0) {
         hipLaunchKernelGGL(sort_kernel, dim3(static_cast<uint32_t>((tokens + kSortTile - 1) / kSortTile)), dim3(kSortBlock), 0,
                            stream, ids, tokens, vocab, padding, passes, scratch.keys[0], scratch.order[0]);
         if ((e = hipGetLastError()) != hipSuccess) return e;

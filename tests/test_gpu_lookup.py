@@ -170,6 +170,26 @@ def test_a_calls_of_different_lengths_on_one_handle():
         assert ref.excess(out, want, bound) <= 1.0
 
 
+@pytest.mark.parametrize("tokens", [63, 64, 65, 1023, 4095, 8192, 8193, 65_536, 65_537, 66_600])
+@pytest.mark.parametrize("kind", ["uniform", "skewed", "one"])
+def test_order_of_tokens_around_the_sizes_of_its_steps(tokens, kind):
+    """Ids outside the vocabulary and the padding id among the others: each row's
+    terms are added once, the others nowhere."""
+    gen = torch.Generator().manual_seed(tokens)
+    ids = draw_ids(tokens, 700, kind, gen)
+    ids[torch.rand(tokens, generator=gen) < 0.1] = 5
+    outside = ids.clone()
+    out = torch.rand(tokens, generator=gen) < 0.1
+    outside[out] = torch.where(torch.rand(tokens, generator=gen) < 0.5, -1, 700)[out]
+    grad = torch.randn(tokens, 12, generator=gen)
+    table = micro.TokenTable(700, 12, tokens, padding_id=5)
+    got = table.lookup_grad(grad.to(DEV), outside.to(DEV), torch.full((700, 12), 3.0, device=DEV))
+    grad[out | (ids == 5)] = 0
+    want, bound = ref.lookup_grad(grad, ids, 700, 1.0, None)
+    assert ref.excess(got, want, bound) <= 1.0
+    assert bool((got[5] == 0).all())
+
+
 def test_refusals():
     weight = torch.ones(10, 8, device=DEV)
     table = micro.TokenTable(10, 8, 4)
