@@ -55,7 +55,7 @@ struct LossCall {
     float2* stats;           // (maximum, sum of exponentials) of [granule][B]
     float* label_logit;      // [B]
     float2* softmax;         // (maximum, 1 / sum of exponentials) of [B]
-    void* scores;            // exponentials, then logit gradients, [B][Vp]; binary32: floats
+    void* scores;            // exponentials (binary32: floats, else 16-bit codes), then logit gradients, [B][Vp]
     void* split;             // binary32: the logit gradients as [P][B][Vp] bfloat16
     float* parts;            // parts of a short call's scores cut along the sum: two of its tiles per compute unit
     float* partials;         // parts of the two gradient products cut along the sum: a wide tile per compute unit each
