@@ -553,8 +553,9 @@ MICRO_API micro_status micro_table_loss(micro_table *table, const void *hidden, 
  * Both are of the table's type, rounded once; between the products p - [..] is
  * rounded to the table's type once (binary32: to 24 bits; binary16 keeps it times
  * 2^14, so that it loses bits below 2^-28 and is 0 below 2^-39), sums in
- * binary32.  With 16-bit types that rounding adds to the gradients' error what
- * the output's own does not: where more matters, binary32 has it.
+ * binary32.  In dhidden the label's p - 1 counts unrounded.  In dweight of 16-bit
+ * types that rounding adds to the error what the output's own does not: where
+ * more matters, binary32 has it.
  * No output may share memory with another argument.
  */
 MICRO_API micro_status micro_table_loss_grad(micro_table *table, const void *hidden, int64_t hidden_stride,

@@ -54,6 +54,7 @@ struct LossCall {
     void* w;                 // table rows, [P][vocab][Dp], where the table itself cannot be read in place
     float2* stats;           // (maximum, sum of exponentials) of [granule][B]
     float* label_logit;      // [B]
+    float* label_rest;       // 16-bit types: the logit gradient at the label less its rounding, [B]
     float2* softmax;         // (maximum, 1 / sum of exponentials) of [B]
     void* scores;            // exponentials (binary32: floats, else 16-bit codes), then logit gradients, [B][Vp]
     void* split;             // binary32: the logit gradients as [P][B][Vp] bfloat16

@@ -657,10 +657,10 @@ constexpr float kHeldUnit<f16> = 16384.0f;
 // type's unit roundoff, so the rounding of p - [label] to the products' type is
 // the one that counts.  Exponentials rounded to that type, and p again
 // behind them, are 0.5 to 1.5% less time for a call with gradients (16384 x
-// 50257 x 2048 8.50 ms for 8.54); the gradients' error in root mean square is
-// then 5% larger (2.87e-5 for 3.02e-5, 700 x 1200 x 192 bfloat16; once rounded
-// in 64 bits 2.87e-5).  What lies below the range is zero in the type behind it,
-// times kHeldUnit or not.
+// 50257 x 2048 8.50 ms for 8.54), but the table gradient's rows without a label
+// are then off by 3.37e-4 of their size for 2.89e-4 (180 tokens x 30522 x 1024,
+// binary16; root mean square).  What lies below the range is zero in the type
+// behind it, times kHeldUnit or not.
 template <class E>
 constexpr float kCodeRange = 136.0f;
 template <>
@@ -1015,15 +1015,16 @@ constexpr int kTurnBlock = 256, kTurnRows = 16;
 
 // The exponentials of a block become the logit gradients, in place (binary32:
 // into three planes): times exp(granule's maximum - lse), less one at the
-// label, rounded to the products' type.  There p - 1 comes from the token's binary32 loss, so a token that is
-// nearly certain keeps its small gradient.  Zero rows up to a multiple
+// label, rounded to the products' type.  There p - 1 comes from the token's
+// binary32 loss, so a token that is nearly certain keeps its small gradient, and
+// what its rounding leaves goes into label_rest.  Zero rows up to a multiple
 // of kDepth.  A stream of one read and one write of the block's scores, bound by
 // HBM: 3.3 GB in 625 us (5.3 TB/s).
 template <class E, class T>
 __global__ __launch_bounds__(kTurnBlock) void gradient_kernel(const int32_t* count, int64_t first, int64_t block, E* scores,
                                                               int64_t padded, const float2* stats, int granule,
                                                               const float2* softmax, const float* counted_losses,
-                                                              const int32_t* labels, T* split) {
+                                                              const int32_t* labels, T* split, float* label_rest) {
     constexpr int kVec = 16 / sizeof(E);
     const int64_t counted = *count - first, n = counted < block ? counted : block;
     if (n <= 0) return;
@@ -1056,6 +1057,7 @@ __global__ __launch_bounds__(kTurnBlock) void gradient_kernel(const int32_t* cou
                 }
                 if (label >= 0 && label < kVec) {
                     const float p = kHeldUnit<E> * expm1f(-counted_losses[first + t]);
+                    if constexpr (sizeof(E) == 2) label_rest[t] = p - static_cast<float>(rounded<E>(p));
 #pragma unroll
                     for (int j = 0; j < kVec; ++j)
                         if (label == j) x[j] = p;
@@ -1094,6 +1096,12 @@ struct GradientOut {
     float* partials;           // one tile a workgroup of the grid
     float* carried;
     int terms;                 // of the products
+    // dhidden of 16-bit types: p - 1 at the label less its rounding, and the
+    // table's rows as the product reads them
+    const float* label_rest;
+    const int32_t* labels;
+    const void* table_rows;
+    int64_t table_stride;
 };
 
 struct GradientPlan {
@@ -1251,6 +1259,37 @@ __device__ __forceinline__ void join_parts(const GradientOut& o, int64_t grid, M
     }
 }
 
+// What dhidden's tile starts from: the label's term, by far the largest of a
+// token, gets back what the rounding of its operand took.  So dhidden is off by
+// what its own rounding takes alone (4915 x 30522 x 1024 bfloat16: 1.66e-3 of its
+// size in root mean square; 1.97e-3 without).  Here rather than when the tile is
+// finished: the first stage's loads are under way, and registers are free (there
+// they were not: 300 bytes a lane went to scratch, and the call took 5% longer).
+template <class S, class T>
+__device__ __forceinline__ void label_rests(const GradientOut& o, const GradientPlan& p, int64_t ta, int64_t tb,
+                                            Acc (&acc)[S::kTilesA][S::kTilesB]) {
+    const Place<S> place;
+    const int64_t a = ta * S::kA + place.row(0, 0);
+    const int left = static_cast<int>(o.dim - a);  // (rows are padded to whole runs of four)
+#pragma unroll
+    for (int j = 0; j < S::kTilesB; ++j) {
+        const int64_t token = tb * S::kB + place.column(j);
+        const float rest = token < p.n ? o.label_rest[token] : 0.0f;
+        const T* row = static_cast<const T*>(o.table_rows) + (token < p.n ? o.labels[o.first + token] : 0) * o.table_stride + a;
+#pragma unroll
+        for (int i = 0; i < S::kTilesA; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float w[4] = {};
+                if (rest != 0.0f && i * 32 + q * 8 < left) load_floats<T, 4>(row + (i * 32 + q * 8), w);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][4 * q + r] = rest * w[r];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
 // kTable: dtable^T = h^T g, else dhidden^T = W^T g^T.  a is always the width,
 // so a lane's values are adjacent in an output row.  Bound by the matrix cores:
 // 16384 x 50257 x 2048 in 2.6 and 2.55 ms (1.29 and 1.32 PFLOP/s).  dhidden's
@@ -1281,6 +1320,8 @@ __global__ __launch_bounds__(S::kThreads) void gradients_kernel(Operand wide, Op
     for (; more; tile = after) {
         Acc acc[S::kTilesA][S::kTilesB];
         clear<S>(acc);
+        if constexpr (!kTable && sizeof(Out) == 2)
+            if (tile.part <= 0) label_rests<S, T>(o, p, tile.a, tile.b, acc);
         product.run(acc, stage0, stage1);
         more = order.next(&after);
         if (more) start(after);
@@ -1397,11 +1438,12 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         const uint32_t turn_rows = std::min<uint32_t>(ceil_div((most + kDepth - 1) / kDepth * kDepth, kTurnRows), 32768);
         hipLaunchKernelGGL((gradient_kernel<E, T>), dim3(turns, turn_rows), dim3(kTurnBlock), 0, stream, c.count, first,
                            block, static_cast<E*>(c.scores), c.vocab_padded, c.stats, granule, c.softmax, c.counted_losses,
-                           c.labels, static_cast<T*>(c.split));
+                           c.labels, static_cast<T*>(c.split), c.label_rest);
         // g as the operand of both products
         Operand g{kSplit ? c.split : c.scores, c.vocab_padded, 0, 0, block * c.vocab_padded};
         GradientOut o{c.count, first, block, false, c.vocab, c.dim, c.rows, c.scale, c.mean, kHeldUnit<T>,
-                      c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried, kTerms};
+                      c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried, kTerms,
+                      c.label_rest, c.labels, table.at, table.stride};
         Operand wide{table.at, table.stride, c.dim_padded, c.vocab, table.plane};
         hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o, o);
         const GradientOut of_hidden = o;  // its split tiles are joined by the next product's workgroups

@@ -145,6 +145,7 @@ micro_status loss_scratch(micro_table* t, bool copy_table, bool gradients) {
             p.take(c.labels, tokens * 4);
             p.take(c.counted_losses, tokens * 4);
             p.take(c.label_logit, c.block * 4);
+            p.take(c.label_rest, c.block * 4);
             p.take(c.softmax, c.block * 8);
             p.take(c.stats, granules * 8);
             p.take(c.h, planes * tokens * dim * 2);

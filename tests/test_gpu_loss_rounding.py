@@ -47,3 +47,37 @@ def test_logit_gradients_are_rounded_once(dtype, vocab, dim, tokens, score_bytes
         error = [rms(product(g).to(dtype).double() - exact) for g in (held(p), twice)]
         assert error[1] > 1.02 * error[0]
         assert rms(got.cpu().double() - exact) <= error[0] + 0.5 * (error[1] - error[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("vocab,dim,tokens,score_bytes", [(600, 128, 200, None), (1200, 200, 700, None), (900, 72, 600, 1),
+                                                          (9001, 64, 60, None)])
+@pytest.mark.parametrize("counted", [1.0, 0.6])
+def test_the_labels_rounding_does_not_reach_dhidden(dtype, vocab, dim, tokens, score_bytes, counted):
+    """The label's p - 1 is most of a token's gradient.  dhidden is as near to 64
+    bits as where only p is rounded, and not where p - 1 is too: the bound is
+    half of what the latter adds."""
+    gen = torch.Generator().manual_seed(vocab)
+    weight = torch.randn(vocab, dim, generator=gen).mul_(dim ** -0.5).to(dtype)
+    targets = torch.randint(0, vocab, (tokens,), generator=gen)
+    row = weight[targets].float()
+    lean = torch.rand(tokens, 1, generator=gen) * 12.0  # the label's p from nearly 0 to nearly 1
+    hidden = (torch.randn(tokens, dim, generator=gen) + lean * row / row.square().sum(1, keepdim=True)).to(dtype)
+    targets[torch.rand(tokens, generator=gen) >= counted] = -100
+    table = micro.TokenTable(vocab, dim, tokens, dtype=dtype, score_bytes=score_bytes)
+    dh = table.loss_grad(hidden.to(DEV), weight.to(DEV), targets.to(DEV), reduction="sum")[2]
+    keep = (targets >= 0).nonzero().flatten()
+    h, w, y = hidden[keep].double(), weight.double(), targets[keep]
+    unit = 2.0 ** 14 if dtype is torch.float16 else 1.0
+    held = lambda x: (x * unit).to(dtype).double() / unit  # noqa: E731
+    logp = torch.log_softmax(h @ w.t(), 1)
+    g = logp.exp()
+    at = torch.arange(y.numel())
+    g[at, y] = torch.expm1(logp[at, y])
+    exact = g @ w
+    both = held(g)
+    only_p = both.clone()
+    only_p[at, y] = g[at, y]
+    error = [rms((x @ w).to(dtype).double() - exact) for x in (only_p, both)]
+    assert error[1] > 1.02 * error[0]
+    assert rms(dh.cpu()[keep].double() - exact) <= error[0] + 0.5 * (error[1] - error[0])
