@@ -54,6 +54,7 @@ micro_status build(micro_grads* g, int32_t count, void* const* tensors, const in
     const size_t head = kGradGridMax * sizeof(double);
     e = hipMalloc(&g->scratch, head + pieces.size() * sizeof(GradPiece));
     if (e != hipSuccess) {
+        forget_hip_error();
         g->scratch = nullptr;
         set_thread_error("device scratch of a set of %lld values: %s", static_cast<long long>(g->total),
                          hipGetErrorString(e));

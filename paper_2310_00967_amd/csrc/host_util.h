@@ -34,8 +34,13 @@ inline micro_status refuse(const char* what) {
     return MICRO_EINVAL;
 }
 
+// An error that is returned to the caller is taken from the runtime's record of
+// the thread, where the next call that looks there would report it again.
+inline void forget_hip_error() { (void)hipGetLastError(); }
+
 inline micro_status report_hip(hipError_t e, const char* what) {
     if (e == hipSuccess) return MICRO_OK;
+    forget_hip_error();
     set_thread_error("%s failed: %s", what, hipGetErrorString(e));
     return e == hipErrorOutOfMemory ? MICRO_ENOMEM : MICRO_EHIP;
 }

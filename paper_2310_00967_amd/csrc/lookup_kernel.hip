@@ -17,6 +17,7 @@
 
 #include <algorithm>
 
+#include "launch.h"
 #include "micro_sparsify.h"
 #include "value_types.h"
 
@@ -570,10 +571,9 @@ hipError_t lookup(const Rows& table, int64_t vocab, int32_t dim, const TokenIds&
     constexpr int kVec = 16 / sizeof(T);
     const int bits = group_bits_for((dim + kVec - 1) / kVec, 8);
     const int64_t per_block = kBlock >> bits;
-    hipLaunchKernelGGL(lookup_kernel<T>, dim3(static_cast<uint32_t>((tokens + per_block - 1) / per_block)), dim3(kBlock),
-                       0, stream, static_cast<const T*>(table.at), table.stride, vocab, dim, ids, tokens, scale,
-                       static_cast<T*>(out.at), out.stride, bits);
-    return hipGetLastError();
+    return launch(lookup_kernel<T>, dim3(static_cast<uint32_t>((tokens + per_block - 1) / per_block)), dim3(kBlock), stream,
+                  static_cast<const T*>(table.at), table.stride, vocab, dim, ids, tokens, scale, static_cast<T*>(out.at),
+                  out.stride, bits);
 }
 
 template <class T>
@@ -592,18 +592,13 @@ hipError_t sums(const Rows& grad, int64_t tokens, float scale, bool accumulate, 
     // 64 KB of rows a zeroing workgroup
     const int zero_rows = static_cast<int>(std::clamp<int64_t>(65536 / (dim * int64_t(sizeof(T))), 1, kZeroRowsMax));
     if (!accumulate) blocks.x += static_cast<uint32_t>((vocab + zero_rows - 1) / zero_rows);
-    const auto sum = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, blocks, dim3(kBlock), 0, stream, static_cast<const T*>(grad.at), grad.stride, tokens, keys,
-                           order, static_cast<uint32_t>(vocab), scale, accumulate, static_cast<T*>(table.at), table.stride,
-                           dim, partials, bits, summing, zero_rows);
-    };
-    sum(sum_kernel<T>);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = launch(sum_kernel<T>, blocks, dim3(kBlock), stream, static_cast<const T*>(grad.at), grad.stride, tokens,
+                                keys, order, static_cast<uint32_t>(vocab), scale, accumulate, static_cast<T*>(table.at),
+                                table.stride, dim, partials, bits, summing, zero_rows);
     if (e != hipSuccess || chunks < 2) return e;
-    hipLaunchKernelGGL(join_kernel<T>, dim3(static_cast<uint32_t>(chunks), static_cast<uint32_t>((dim + 255) / 256)),
-                       dim3(kBlock), 0, stream, tokens, keys, static_cast<uint32_t>(vocab), scale, accumulate,
-                       static_cast<T*>(table.at), table.stride, dim, partials);
-    return hipGetLastError();
+    return launch(join_kernel<T>, dim3(static_cast<uint32_t>(chunks), static_cast<uint32_t>((dim + 255) / 256)), dim3(kBlock),
+                  stream, tokens, keys, static_cast<uint32_t>(vocab), scale, accumulate, static_cast<T*>(table.at),
+                  table.stride, dim, partials);
 }
 
 }  // namespace
@@ -624,20 +619,18 @@ hipError_t launch_lookup_grad(const Rows& grad, int64_t tokens, const TokenIds& 
     while (passes < 4 && (vocab >> (passes * kDigitBits)) != 0) ++passes;
     hipError_t e = hipSuccess;
     if (tokens > 0 && tokens <= kMostRanked) {
-        hipLaunchKernelGGL(rank_kernel, dim3(static_cast<uint32_t>((tokens + kRanked - 1) / kRanked)), dim3(kSortBlock), 0,
-                           stream, ids, tokens, vocab, padding, scratch.keys[0], scratch.order[0]);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = launch(rank_kernel, dim3(static_cast<uint32_t>((tokens + kRanked - 1) / kRanked)), dim3(kSortBlock), stream, ids,
+                   tokens, vocab, padding, scratch.keys[0], scratch.order[0]);
     } else if (tokens > 0) {
-        hipLaunchKernelGGL(sort_kernel, dim3(static_cast<uint32_t>((tokens + kSortTile - 1) / kSortTile)), dim3(kSortBlock), 0,
-                           stream, ids, tokens, vocab, padding, passes, scratch.keys[0], scratch.order[0]);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = launch(sort_kernel, dim3(static_cast<uint32_t>((tokens + kSortTile - 1) / kSortTile)), dim3(kSortBlock), stream,
+                   ids, tokens, vocab, padding, passes, scratch.keys[0], scratch.order[0]);
     }
+    if (e != hipSuccess) return e;
     int in = 0;
     for (int64_t run = kSortTile; run < tokens; run *= kMergeRuns, in ^= 1) {
-        hipLaunchKernelGGL(merge_kernel, dim3(static_cast<uint32_t>((tokens + kBlock - 1) / kBlock)), dim3(kBlock), 0,
-                           stream, scratch.keys[in], scratch.order[in], tokens, run, scratch.keys[in ^ 1],
-                           scratch.order[in ^ 1]);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = launch(merge_kernel, dim3(static_cast<uint32_t>((tokens + kBlock - 1) / kBlock)), dim3(kBlock), stream,
+                   scratch.keys[in], scratch.order[in], tokens, run, scratch.keys[in ^ 1], scratch.order[in ^ 1]);
+        if (e != hipSuccess) return e;
     }
     if (table.type == MICRO_TYPE_F32)
         return sums<float>(grad, tokens, scale, accumulate, table, vocab, dim, scratch.keys[in], scratch.order[in],

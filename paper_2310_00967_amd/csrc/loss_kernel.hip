@@ -19,6 +19,7 @@
 
 #include <algorithm>
 
+#include "launch.h"
 #include "micro_sparsify.h"
 #include "value_types.h"
 
@@ -1376,22 +1377,22 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
     constexpr bool kSplit = sizeof(In) == 4;
     const int64_t rows_h = (std::max<int64_t>(c.tokens, 1) + kDepth - 1) / kDepth * kDepth;
     const Targets targets{c.targets, c.tokens, c.ignored, c.vocab};
+    hipError_t e = hipSuccess;
     if (c.tokens > kChunkTokens)
-        hipLaunchKernelGGL(count_kernel, dim3(ceil_div(c.tokens, kChunkTokens)), dim3(kChunkTokens), 0, stream, targets,
-                           c.chunks);
-    hipLaunchKernelGGL((gather_kernel<In, T>), dim3(ceil_div(std::max<int64_t>(c.tokens, 1), kGathered)), dim3(kRowBlock), 0,
-                       stream, static_cast<const In*>(c.hidden.at), c.hidden.stride, c.dim, targets,
-                       Selection{c.chunks, c.count, c.rows, c.labels, c.losses}, static_cast<T*>(c.h), c.dim_padded,
-                       rows_h * c.dim_padded, c.gradients ? static_cast<In*>(c.dhidden.at) : nullptr, c.dhidden.stride);
+        e = launch(count_kernel, dim3(ceil_div(c.tokens, kChunkTokens)), dim3(kChunkTokens), stream, targets, c.chunks);
+    if (e != hipSuccess) return e;
+    e = launch(gather_kernel<In, T>, dim3(ceil_div(std::max<int64_t>(c.tokens, 1), kGathered)), dim3(kRowBlock), stream,
+               static_cast<const In*>(c.hidden.at), c.hidden.stride, c.dim, targets,
+               Selection{c.chunks, c.count, c.rows, c.labels, c.losses}, static_cast<T*>(c.h), c.dim_padded,
+               rows_h * c.dim_padded, c.gradients ? static_cast<In*>(c.dhidden.at) : nullptr, c.dhidden.stride);
+    if (e != hipSuccess) return e;
     Operand table{c.table.at, c.table.stride, c.vocab, 0, 0};
     if (!table_in_place(c)) {
         table = {c.w, c.dim_padded, c.vocab, 0, c.vocab * c.dim_padded};
-        hipLaunchKernelGGL((table_kernel<In, T>), dim3(static_cast<uint32_t>(c.vocab)), dim3(kRowBlock), 0, stream,
-                           static_cast<const In*>(c.table.at), c.table.stride, c.dim, static_cast<T*>(c.w), c.dim_padded,
-                           table.plane);
+        e = launch(table_kernel<In, T>, dim3(static_cast<uint32_t>(c.vocab)), dim3(kRowBlock), stream,
+                   static_cast<const In*>(c.table.at), c.table.stride, c.dim, static_cast<T*>(c.w), c.dim_padded, table.plane);
+        if (e != hipSuccess) return e;
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     const int granule = S::kTilesA * 32;
     // a call of few tokens has more granules, and room for them in a shorter block
     const int64_t block = granule == kGranuleFew ? kFewTokens : granule == kGranuleSome ? std::min<int64_t>(kSomeTokens, c.block) : c.block;
@@ -1410,42 +1411,41 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
             static_assert(S::kPerUnit * S::kA * S::kB <= 2 * kPartTile, "a part for each workgroup");
             cut = scores.most_splits > 1 && tiles <= grid / kFewTiles;
             if (cut) {
-                hipLaunchKernelGGL((scores_kernel<S, T, E, kTerms, true>), dim3(grid), dim3(S::kThreads), 0, stream, table,
-                                   h, blocks, scores);
-                hipLaunchKernelGGL((join_scores_kernel<S, E>),
-                                   dim3(static_cast<uint32_t>(tiles * (S::kThreads / 64) * S::kTilesB)),
-                                   dim3(kJoinWaves * 64), 0, stream, scores, int64_t(grid));
+                e = launch(scores_kernel<S, T, E, kTerms, true>, dim3(grid), dim3(S::kThreads), stream, table, h, blocks,
+                           scores);
+                if (e != hipSuccess) return e;
+                e = launch(join_scores_kernel<S, E>, dim3(static_cast<uint32_t>(tiles * (S::kThreads / 64) * S::kTilesB)),
+                           dim3(kJoinWaves * 64), stream, scores, int64_t(grid));
             }
         }
         if (!cut)
-            hipLaunchKernelGGL((scores_kernel<S, T, E, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, table, h,
-                               blocks, scores);
+            e = launch(scores_kernel<S, T, E, kTerms, false>, dim3(grid), dim3(S::kThreads), stream, table, h, blocks, scores);
+        if (e != hipSuccess) return e;
         total_now = c.tokens <= std::min<int64_t>(block, kSomeTokens);
         const auto join = [&](auto kernel, int tokens, int slices) {
-            hipLaunchKernelGGL(kernel, dim3(ceil_div(most, tokens)), dim3(tokens * slices), 0, stream, c.count, first, block,
-                               c.stats, granules, c.label_logit, c.rows, c.softmax, c.counted_losses, c.losses, c.mean,
-                               total_now ? c.loss : nullptr);
+            return launch(kernel, dim3(ceil_div(most, tokens)), dim3(tokens * slices), stream, c.count, first, block, c.stats,
+                          granules, c.label_logit, c.rows, c.softmax, c.counted_losses, c.losses, c.mean,
+                          total_now ? c.loss : nullptr);
         };
         // few tokens: more threads for each, so that enough loads are under way
-        if (most <= kFewJoined)
-            join(softmax_kernel<8, 128>, 8, 128);
-        else
-            join(softmax_kernel<32, 16>, 32, 16);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = most <= kFewJoined ? join(softmax_kernel<8, 128>, 8, 128) : join(softmax_kernel<32, 16>, 32, 16);
+        if (e != hipSuccess) return e;
         if (!c.gradients) continue;
         const uint32_t turns = ceil_div(c.vocab_padded, kTurnBlock * (16 / int(sizeof(E))));
         // (a grid's second dimension ends at 65535; the kernel goes on by its size)
         const uint32_t turn_rows = std::min<uint32_t>(ceil_div((most + kDepth - 1) / kDepth * kDepth, kTurnRows), 32768);
-        hipLaunchKernelGGL((gradient_kernel<E, T>), dim3(turns, turn_rows), dim3(kTurnBlock), 0, stream, c.count, first,
-                           block, static_cast<E*>(c.scores), c.vocab_padded, c.stats, granule, c.softmax, c.counted_losses,
-                           c.labels, static_cast<T*>(c.split), c.label_rest);
+        e = launch(gradient_kernel<E, T>, dim3(turns, turn_rows), dim3(kTurnBlock), stream, c.count, first, block,
+                   static_cast<E*>(c.scores), c.vocab_padded, c.stats, granule, c.softmax, c.counted_losses, c.labels,
+                   static_cast<T*>(c.split), c.label_rest);
+        if (e != hipSuccess) return e;
         // g as the operand of both products
         Operand g{kSplit ? c.split : c.scores, c.vocab_padded, 0, 0, block * c.vocab_padded};
         GradientOut o{c.count, first, block, false, c.vocab, c.dim, c.rows, c.scale, c.mean, kHeldUnit<T>,
                       c.dhidden.at, c.dhidden.stride, false, c.partials, c.carried, kTerms,
                       c.label_rest, c.labels, table.at, table.stride};
         Operand wide{table.at, table.stride, c.dim_padded, c.vocab, table.plane};
-        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, false>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o, o);
+        e = launch(gradients_kernel<S, T, In, kTerms, false>, dim3(grid), dim3(S::kThreads), stream, wide, g, o, o);
+        if (e != hipSuccess) return e;
         const GradientOut of_hidden = o;  // its split tiles are joined by the next product's workgroups
         o.table = true;
         o.to = c.dtable.at;
@@ -1454,15 +1454,13 @@ hipError_t run(const LossCall& c, hipStream_t stream) {
         o.partials += c.compute_units * kWideTile;
         wide = {h.at, h.stride, c.dim_padded, 0, h.plane};
         g.kept = c.vocab_padded;
-        hipLaunchKernelGGL((gradients_kernel<S, T, In, kTerms, true>), dim3(grid), dim3(S::kThreads), 0, stream, wide, g, o,
-                           of_hidden);
-        hipLaunchKernelGGL((join_parts_kernel<S, In>), dim3(grid), dim3(S::kThreads), 0, stream, o, grid);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        e = launch(gradients_kernel<S, T, In, kTerms, true>, dim3(grid), dim3(S::kThreads), stream, wide, g, o, of_hidden);
+        if (e != hipSuccess) return e;
+        e = launch(join_parts_kernel<S, In>, dim3(grid), dim3(S::kThreads), stream, o, grid);
+        if (e != hipSuccess) return e;
     }
-    if (!total_now)
-        hipLaunchKernelGGL(total_kernel, dim3(1), dim3(kTotalBlock), 0, stream, c.count, c.counted_losses, c.mean,
-                           c.loss);
-    return hipGetLastError();
+    if (total_now) return hipSuccess;
+    return launch(total_kernel, dim3(1), dim3(kTotalBlock), stream, c.count, c.counted_losses, c.mean, c.loss);
 }
 
 template <class In, class T, class E, int kTerms>

@@ -62,6 +62,7 @@ micro_status ensure(void** memory, const char* what, LayOut lay_out) {
     void* p = nullptr;
     const hipError_t e = hipMalloc(&p, static_cast<size_t>(std::max<int64_t>(parts.used, 256)));
     if (e != hipSuccess) {
+        forget_hip_error();
         lay_out(parts = Parts{});  // no part points anywhere
         set_thread_error("%s: %lld bytes of device scratch: %s", what, static_cast<long long>(parts.used),
                          hipGetErrorString(e));
