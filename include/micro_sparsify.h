@@ -474,6 +474,9 @@ MICRO_API void micro_grads_free(micro_grads *grads);
  * device addresses with a row stride in values (>= dim; the values of a row
  * are adjacent, the address aligned to the type); tokens' ids and targets are
  * int32 or int64 (MICRO_IDS_*), one after the other, aligned to their size.
+ * No output may share a value with another argument (columns of one buffer, of
+ * the same row stride, may be different arguments; rows of different strides may
+ * not lie among each other): MICRO_EINVAL.
  */
 #define MICRO_IDS_I32 0
 #define MICRO_IDS_I64 1
@@ -556,7 +559,6 @@ MICRO_API micro_status micro_table_loss(micro_table *table, const void *hidden, 
  * binary32.  In dhidden the label's p - 1 counts unrounded.  In dweight of 16-bit
  * types that rounding adds to the error what the output's own does not: where
  * more matters, binary32 has it.
- * No output may share memory with another argument.
  */
 MICRO_API micro_status micro_table_loss_grad(micro_table *table, const void *hidden, int64_t hidden_stride,
                                              const void *weight, int64_t weight_stride, const void *targets,

@@ -7,6 +7,7 @@
 #include "lookup_kernel.h"
 #include "loss_kernel.h"
 #include "micro_sparsify.h"
+#include "strided_rows.h"
 
 namespace {
 
@@ -84,8 +85,7 @@ void release(micro_table* t) {
 }
 
 struct Region {
-    const void* at;
-    int64_t bytes;
+    RowSpan rows;
     bool written;
 };
 
@@ -93,18 +93,21 @@ template <int N>
 micro_status check_apart(const Region (&r)[N]) {
     for (int i = 0; i < N; ++i)
         for (int j = i + 1; j < N; ++j)
-            if ((r[i].written || r[j].written) && share_bytes(r[i].at, r[i].bytes, r[j].at, r[j].bytes))
+            if ((r[i].written || r[j].written) && rows_share_bytes(r[i].rows, r[j].rows))
                 return refuse("an output shares memory with another argument");
     return MICRO_OK;
 }
 
-int64_t rows_bytes(int64_t rows, int64_t stride, int64_t dim, int64_t size) {
-    return rows > 0 ? ((rows - 1) * stride + dim) * size : 0;
+// An argument's rows, and `values` values one after the other, in bytes.
+RowSpan rows_of(const micro_table* t, const void* at, int64_t rows, int64_t stride) {
+    return {at, rows, stride * t->size(), t->dim * t->size()};
 }
+RowSpan run_of(const void* at, int64_t values, int64_t size) { return {at, 1, values * size, values * size}; }
 
 micro_status check_rows(const micro_table* t, const void* at, int64_t stride, int64_t rows) {
     if (stride < t->dim) return refuse("a row stride is below the table's dim");
-    if (stride > (int64_t(1) << 32)) return refuse("a row stride is above 2^32");
+    if (stride > (int64_t(1) << 32) || rows > (int64_t(1) << 56) / stride)
+        return refuse("a row stride is above 2^32, or the rows end past 2^56 values");
     if (rows > 0 && (!at || !aligned_to(at, t->size()))) return refuse("rows are NULL or not aligned to their type");
     return MICRO_OK;
 }
@@ -122,7 +125,9 @@ micro_status check_tokens(const micro_table* t, const void* ids, int32_t ids_typ
     return MICRO_OK;
 }
 
-int64_t ids_bytes(int32_t ids_type, int64_t tokens) { return tokens * (ids_type == MICRO_IDS_I64 ? 8 : 4); }
+RowSpan ids_of(const void* ids, int32_t ids_type, int64_t tokens) {
+    return run_of(ids, tokens, ids_type == MICRO_IDS_I64 ? 8 : 4);
+}
 
 // The loss's scratch for the handle's largest call.
 micro_status loss_scratch(micro_table* t, bool copy_table, bool gradients) {
@@ -186,15 +191,14 @@ micro_status run_loss(micro_table* t, const void* hidden, int64_t hidden_stride,
         set_thread_error("a loss over %lld rows: at most 2^22", static_cast<long long>(t->vocab));
         return MICRO_ERANGE;
     }
-    const int64_t size = t->size();
     const Region regions[] = {
-        {hidden, rows_bytes(tokens, hidden_stride, t->dim, size), false},
-        {weight, rows_bytes(t->vocab, weight_stride, t->dim, size), false},
-        {targets, ids_bytes(targets_type, tokens), false},
-        {losses, tokens * 4, true},
-        {loss, 4, true},
-        {dhidden, gradients ? rows_bytes(tokens, dhidden_stride, t->dim, size) : 0, true},
-        {dweight, gradients ? rows_bytes(t->vocab, dweight_stride, t->dim, size) : 0, true},
+        {rows_of(t, hidden, tokens, hidden_stride), false},
+        {rows_of(t, weight, t->vocab, weight_stride), false},
+        {ids_of(targets, targets_type, tokens), false},
+        {run_of(losses, tokens, 4), true},
+        {run_of(loss, 1, 4), true},
+        {rows_of(t, dhidden, gradients ? tokens : 0, dhidden_stride), true},
+        {rows_of(t, dweight, gradients ? t->vocab : 0, dweight_stride), true},
     };
     if (micro_status st = check_apart(regions)) return st;
     CallDevice scope(t->device);
@@ -272,9 +276,9 @@ micro_status micro_table_lookup(micro_table* t, const void* weight, int64_t weig
     if (micro_status st = check_tokens(t, ids, ids_type, tokens)) return st;
     if (micro_status st = check_rows(t, weight, weight_stride, t->vocab)) return st;
     if (micro_status st = check_rows(t, out, out_stride, tokens)) return st;
-    const Region regions[] = {{weight, rows_bytes(t->vocab, weight_stride, t->dim, t->size()), false},
-                              {ids, ids_bytes(ids_type, tokens), false},
-                              {out, rows_bytes(tokens, out_stride, t->dim, t->size()), true}};
+    const Region regions[] = {{rows_of(t, weight, t->vocab, weight_stride), false},
+                              {ids_of(ids, ids_type, tokens), false},
+                              {rows_of(t, out, tokens, out_stride), true}};
     if (micro_status st = check_apart(regions)) return st;
     CallDevice scope(t->device);
     return report_hip(launch_lookup({const_cast<void*>(weight), weight_stride, t->type}, t->vocab, t->dim,
@@ -290,9 +294,9 @@ micro_status micro_table_lookup_grad(micro_table* t, const void* grad, int64_t g
     if (micro_status st = check_tokens(t, ids, ids_type, tokens)) return st;
     if (micro_status st = check_rows(t, grad, grad_stride, tokens)) return st;
     if (micro_status st = check_rows(t, dweight, dweight_stride, t->vocab)) return st;
-    const Region regions[] = {{grad, rows_bytes(tokens, grad_stride, t->dim, t->size()), false},
-                              {ids, ids_bytes(ids_type, tokens), false},
-                              {dweight, rows_bytes(t->vocab, dweight_stride, t->dim, t->size()), true}};
+    const Region regions[] = {{rows_of(t, grad, tokens, grad_stride), false},
+                              {ids_of(ids, ids_type, tokens), false},
+                              {rows_of(t, dweight, t->vocab, dweight_stride), true}};
     if (micro_status st = check_apart(regions)) return st;
     CallDevice scope(t->device);
     LookupGradScratch& s = t->lookup;
