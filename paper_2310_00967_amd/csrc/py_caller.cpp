@@ -247,7 +247,7 @@ PyObject* table_lookup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor& ids = THPVariable_Unpack(args[1]);
     const auto plain = [&](const at::Tensor& t) {
         return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == c->device && t.is_contiguous() &&
-               !t.requires_grad();
+               !t.requires_grad() && !t._fw_grad(/*level=*/0).defined();
     };
     const bool wide = ids.scalar_type() == at::kLong;
     if (!plain(weight) || !plain(ids) || weight.scalar_type() != c->type || weight.dim() != 2 ||

@@ -32,6 +32,7 @@ class _Enqueued:
             dev = torch.device("cuda", torch.cuda.current_device())
         self._torch = torch
         self._tensor = torch.Tensor
+        self._forward_ad = torch.autograd.forward_ad
         self.device = dev
         self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
         self._raw_stream = self.stream.cuda_stream
@@ -173,9 +174,11 @@ class TokenTable(_Enqueued):
     The handle holds sizes and scratch, not the table: `weight` is an argument
     of every call.  Calls take up to max_tokens tokens.  Rows may be strided
     (the last dimension adjacent); ids and targets are int32 or int64, of any
-    contiguous shape.  padding_id: an id whose row gets no gradient from
-    lookups; ignore_id: the target of a token that does not count; score_bytes:
-    scratch for one token block's scores at most."""
+    contiguous shape.  Calls are outside autograd: a tensor that requires its
+    gradient is refused unless under torch.no_grad(), one with a tangent always.
+    padding_id: an id whose row gets no gradient from lookups; ignore_id: the
+    target of a token that does not count; score_bytes: scratch for one token
+    block's scores at most."""
 
     def __init__(self, vocab, dim, max_tokens, dtype=None, padding_id=None, ignore_id=-100, score_bytes=None,
                  device=None, stream=None):
@@ -221,6 +224,11 @@ class TokenTable(_Enqueued):
         """(address, row stride) of `rows` rows of dim values."""
         if not isinstance(t, self._tensor) or t.dtype is not self.dtype or not t.is_cuda or t.get_device() != self._index:
             raise TypeError(f"{name} must be a {self.dtype} tensor on {self.device}")
+        if t.requires_grad and self._torch.is_grad_enabled():
+            raise RuntimeError(f"{name} requires its gradient, which this call does not record: call under "
+                               "torch.no_grad() or pass its detach()")
+        if self._forward_ad._current_level >= 0 and self._forward_ad.unpack_dual(t).tangent is not None:
+            raise RuntimeError(f"{name} has a tangent, which this call does not carry on")
         if t.dim() < 1 or t.shape[-1] != self.dim or t.numel() != rows * self.dim:
             raise ValueError(f"{name} must hold {rows} rows of {self.dim} values")
         if t.is_contiguous():
