@@ -79,7 +79,11 @@ class GradientSet(_Enqueued):
 
     Contiguous float32, float16 or bfloat16 tensors on one device; no two may
     share memory.  The set holds them, and uses the memory they had when it was
-    made: make a new set when a gradient is replaced by another tensor."""
+    made, which it keeps allocated.  So it must be made anew when a gradient is
+    another tensor or has other memory, as every step's is after torch's
+    zero_grad() (set_to_none=True, its default): an old set reads the old values
+    without an error.  Making one allocates, uploads and waits for its stream;
+    gradients that are zeroed or written in place keep theirs."""
 
     def __init__(self, tensors, device=None, stream=None):
         tensors = list(tensors)
@@ -93,6 +97,7 @@ class GradientSet(_Enqueued):
                 raise TypeError(f"tensor {i} must be a contiguous float32, float16 or bfloat16 tensor on "
                                 f"{self.device}")
         self.tensors = tensors
+        self._memory = [t.detach() for t in tensors]  # whatever becomes of the tensors' data
         self.n_total = sum(t.numel() for t in tensors)
         with self._torch.cuda.device(self.device):
             self._handle = _lib.micro_grads_init([t.data_ptr() for t in tensors], [t.numel() for t in tensors],
@@ -105,6 +110,7 @@ class GradientSet(_Enqueued):
         if getattr(self, "_handle", None) is not None:
             _lib.micro_grads_free(self._handle)
             self._handle = None
+            self._memory = []
 
     def sumsq(self):
         """The sum of the squares of all values (a float64 device scalar):
@@ -114,7 +120,7 @@ class GradientSet(_Enqueued):
         out = self._empty((), self._torch.float64, foreign)
         _lib.check(self._norm_fn(handle, out.data_ptr(), None))
         if foreign:
-            self._used(*self.tensors)
+            self._used(*self._memory)
         return out
 
     def norm(self):
@@ -124,7 +130,7 @@ class GradientSet(_Enqueued):
         out = self._empty((), self._torch.float32, foreign)
         _lib.check(self._norm_fn(handle, None, out.data_ptr()))
         if foreign:
-            self._used(*self.tensors)
+            self._used(*self._memory)
         return out
 
     def clip_(self, max_norm, sumsq=None):
@@ -137,7 +143,7 @@ class GradientSet(_Enqueued):
         norm = self._empty((), self._torch.float32, foreign)
         _lib.check(self._clip_fn(handle, float(max_norm), other, norm.data_ptr()))
         if foreign:
-            self._used(sumsq, *self.tensors)
+            self._used(sumsq, *self._memory)
         return norm
 
     def flatten(self, flat, max_norm=None, sumsq=None):
@@ -157,13 +163,13 @@ class GradientSet(_Enqueued):
                 raise ValueError("sumsq without max_norm")
             _lib.check(self._flatten_fn(handle, math.inf, None, flat.data_ptr(), None))
             if foreign:
-                self._used(flat, *self.tensors)
+                self._used(flat, *self._memory)
             return None
         other = None if sumsq is None else self._scalar(sumsq, "sumsq", self._torch.float64)
         norm = self._empty((), self._torch.float32, foreign)
         _lib.check(self._flatten_fn(handle, float(max_norm), other, flat.data_ptr(), norm.data_ptr()))
         if foreign:
-            self._used(flat, sumsq, *self.tensors)
+            self._used(flat, sumsq, *self._memory)
         return norm
 
 
