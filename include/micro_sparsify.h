@@ -497,10 +497,16 @@ MICRO_API void micro_table_config_default(micro_table_config *cfg);
  * A handle for a table of vocab x dim values of `type` and calls of up to
  * max_tokens tokens, enqueuing on hip_stream; cfg NULL: the defaults.  Holds
  * no scratch yet: the first call of each kind allocates what its kind needs
- * (a lookup nothing; its gradient 16 bytes and dim/2 bytes a token; the loss
- * 32 MB, a padded copy of the hidden rows, and one of the table where it cannot
- * be read in place: binary32, a dim that is no multiple of 64, or rows that are
- * not aligned to 16 bytes; its gradients the block's scores and 128 MB).
+ * (of max_tokens, whatever the call's own: a lookup nothing; its gradient 16
+ * bytes and dim/2 bytes a token; the loss 32 MB, a padded copy of the hidden
+ * rows, 8 bytes a block's token for every 128 rows of the table (at least what
+ * 768 tokens take), and a padded copy of the table where it cannot be read in
+ * place: binary32, a dim that is no multiple of 64, or rows that are not aligned
+ * to 16 bytes; its gradients the block's scores, 128 MB, and where max_tokens
+ * exceeds a block 4 bytes for every value of the table, both sides rounded up to
+ * multiples of 256).  A block is as many tokens as score_bytes holds at 2 bytes
+ * a score (binary32: 10), in multiples of 256.  A call that is captured into a
+ * graph must have its scratch: make one like it before.
  * MICRO_ERANGE for vocab above 2^31 - 2, dim above 65536 or max_tokens above
  * 2^22; MICRO_EINVAL for vocab < 1, dim < 1, max_tokens < 0 or an unknown
  * type.
@@ -519,8 +525,9 @@ MICRO_API micro_status micro_table_lookup(micro_table *table, const void *weight
 
 /*
  * The lookup's gradient: dweight[v] = scale * the sum of grad[t] over the
- * tokens t with ids[t] == v, in ascending t and in binary32 (chunks of 16
- * sorted tokens, then the chunks' sums), rounded to the type once.
+ * tokens t with ids[t] == v, in binary32 and an order that the ids alone
+ * determine (ascending t, for more than 16 to 31 tokens in runs of 16 whose sums
+ * are added), rounded to the type once.
  * accumulate != 0 adds that to dweight[v] before rounding and leaves rows
  * without a token untouched; else every row is written.  Tokens whose id is
  * padding_id or outside [0, vocab) have no part.

@@ -23,7 +23,7 @@ namespace {
 using namespace micro;
 
 // Values of a piece: a multiple of what a workgroup loads in one round.  Long
-// sets take kPieceMax, whose 32-byte record is nothing beside its values;
+// sets take kPieceMax, whose 24-byte record is nothing beside its values;
 // shorter ones as much less as gives every workgroup of a full grid a piece.
 constexpr int64_t kPieceMax = 32768, kPieceMin = 4096;
 

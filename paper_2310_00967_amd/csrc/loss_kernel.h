@@ -18,6 +18,8 @@ constexpr int kSplitPlanes = 3;
 // workgroups a compute unit) up to kSomeTokens: with gradients over 30522 x 1024
 // 100 tokens take 100 us and 300 take 135, in wide tiles (256 x 256, one
 // workgroup) 128 and 145; 512 tokens 162 and 161, over 50257 x 2048 470 and 416.
+// (Settled on these two tables.  Over a few thousand rows the wide tiles of more
+// tokens than that do not fill the card, and middle ones might be faster.)
 // The loss alone of up to kFewTokens takes narrow ones (128 vocabulary rows x 32
 // tokens): it is bound by one read of the table (32 us over 50257 x 2048, 6.5
 // TB/s), which many small workgroups keep going.
@@ -58,7 +60,7 @@ struct LossCall {
     float2* softmax;         // (maximum, 1 / sum of exponentials) of [B]
     void* scores;            // exponentials (binary32: floats, else 16-bit codes), then logit gradients, [B][Vp]
     void* split;             // binary32: the logit gradients as [P][B][Vp] bfloat16
-    float* parts;            // parts of a short call's scores cut along the sum: two of its tiles per compute unit
+    float* parts;            // parts of a short call's scores cut along the sum: two middle tiles or four narrow ones per compute unit
     float* partials;         // parts of the two gradient products cut along the sum: a wide tile per compute unit each
     float* carried;          // wide tiles of dtable between token blocks; null with one block
     int compute_units;

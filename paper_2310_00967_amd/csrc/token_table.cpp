@@ -67,7 +67,7 @@ micro_status ensure(void** memory, const char* what, LayOut lay_out) {
         lay_out(parts = Parts{});  // no part points anywhere
         set_thread_error("%s: %lld bytes of device scratch: %s", what, static_cast<long long>(parts.used),
                          hipGetErrorString(e));
-        return MICRO_ENOMEM;
+        return e == hipErrorOutOfMemory ? MICRO_ENOMEM : MICRO_EHIP;
     }
     *memory = p;
     parts = Parts{static_cast<char*>(p), 0};

@@ -4,9 +4,11 @@ with their gradients.
 
 Calls are enqueued on the handle's stream (by default the current one when the
 handle was made) and return after the launches, without waiting.  Inputs must
-be ready on that stream.  Outputs that a call allocates belong to that stream;
-tensors of another stream are kept from reuse until the handle's stream is done
-with them.
+be ready on that stream.  Outputs that a call allocates belong to that stream.
+Where another stream is current during a call, its tensors are kept from reuse
+until the handle's stream is done with them; where the handle's own is current,
+as with torch's operators, a tensor that another stream allocated needs the
+caller's record_stream.
 """
 import ctypes
 import math
