@@ -812,9 +812,9 @@ __device__ __forceinline__ void finish_scores(const ScoreOut& out, int64_t n, MI
 
 // a: vocabulary, b: tokens, so a lane holds one token's logits and reduces
 // them without shuffles but the one between its two halves.  Bound by the matrix
-// cores: 16384 x 50257 x 2048 in 2.75 to 2.8 ms (1.2 PFLOP/s), of which the
-// exponentials, maxima and stores of a finished tile are a tenth; alone, without
-// scores to store, 8192 tokens in 1.31 ms (1.29).  Few tokens: by the one read of
+// cores: 16384 x 50257 x 2048 in 2.85 ms (1.18 PFLOP/s), of which the exponentials,
+// their codes, maxima and stores of a finished tile are an eighth; alone, without
+// scores to store, 8192 tokens in 1.27 to 1.39 ms (1.21 to 1.32).  Few tokens: by the one read of
 // the table, 30 us for 206 MB (6.9 TB/s).  kCut: a short call over few tiles,
 // whose tiles are cut along the sum and left for the join, since a step of one
 // tile waits for its loads: whole calls of 7 tokens, 1549 x 2304, with gradients
