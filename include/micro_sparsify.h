@@ -573,8 +573,113 @@ MICRO_API micro_status micro_table_loss_grad(micro_table *table, const void *hid
                                              int32_t accumulate, float *losses, float *loss, void *dhidden,
                                              int64_t dhidden_stride, void *dweight, int64_t dweight_stride);
 
+/*
+ * Draws a token for each row of logits over the table's vocabulary.  With m the
+ * row's largest logit and T its temperature a token's weight is w = exp((l - m) /
+ * T); tokens are ordered by logit, the largest first, equal ones by index.
+ *   top_k   the first top_k tokens of that order are kept (<= 0: all);
+ *   top_p   of those the shortest prefix whose weights reach top_p of theirs (at
+ *           least one token; >= 1: all);
+ *   min_p   of those the ones with w >= min_p.
+ * ids[t] is the first token, by index, at which the running sum of the kept
+ * weights exceeds uniforms[t] times their sum, logprobs[t] the logarithm of its
+ * share.  T == 0 takes the first largest logit.  Logits of -inf or NaN have no
+ * part, and equal +inf ones share the row; where none is left ids[t] is -1 and
+ * logprobs[t] NaN.  Weights are whole multiples of 2^-f in 64 bits, where the
+ * vocabulary has at most 2^(62 - f) tokens and f is at most 50, and their sums are
+ * exact: a token of less than that share of the largest is never drawn.
+ *   logits    device, `rows` rows of `vocab` values of logits_type, any row stride
+ *             >= vocab.
+ *   uniforms  device float[rows] in [0, 1); below (or NaN) counts as 0, above as
+ *             the largest below 1.
+ *   sampling  host: the settings of all rows, or for any of the four a device
+ *             array of one value a row in its place (float, top_k int32), where a
+ *             temperature that is not above 0 counts as 0 and a NaN top_p or min_p
+ *             as one that keeps all.
+ *   ids       device, of ids_type;  logprobs  device float[rows]; may be NULL.
+ * MICRO_ERANGE for a vocab above 2^22, MICRO_EINVAL for a setting out of range
+ * (temperature < 0 or NaN, top_p outside (0, 1], min_p outside [0, 1]).
+ */
+typedef struct micro_sampling {
+    double temperature, top_p, min_p;
+    int64_t top_k;
+    const float *temperatures, *top_ps, *min_ps; /* device, one a row; NULL: the value above */
+    const int32_t *top_ks;
+} micro_sampling;
+
+MICRO_API micro_status micro_table_sample(micro_table *table, const void *logits, int32_t logits_type,
+                                          int64_t logits_stride, int64_t rows, const float *uniforms,
+                                          const micro_sampling *sampling, void *ids, int32_t ids_type,
+                                          float *logprobs);
+
 /* Releases the handle's scratch after waiting for its stream; NULL is a no-op. */
 MICRO_API void micro_table_free(micro_table *table);
+
+/*
+ * Microscaled 4-bit matrices (OCP MX v1.0, MXFP4) and their products.  A matrix
+ * of rows x cols values is held in blocks of 32 values along a row: a scale 2^e,
+ * one byte e + 127, and a 4-bit code a value, sign and one of 0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6.  With a the block's largest magnitude e = floor(log2 a) - 2, at least
+ * -127, and the code is that of value / 2^e, to nearest, ties to the even code,
+ * at most 6.  A block that holds a NaN or an infinity is NaN (byte 255, codes 0).
+ * A block of zeros has byte 0.
+ *   codes   rows of pitch / 2 bytes, where pitch is cols rounded up to a multiple
+ *           of 256: value c in byte c / 2, an even c in the lower half; 0 behind
+ *           cols.  Aligned to 16 bytes.
+ *   scales  the byte of block b of row r at ((b / 8) * rows + r) * 8 + b % 8, for
+ *           the pitch / 32 blocks of a row.  Aligned to 8 bytes.
+ * Sides are at most 2^24 (MICRO_ERANGE).
+ */
+typedef struct micro_mx4_matrix {
+    void *codes, *scales; /* device */
+    int64_t rows, cols;
+} micro_mx4_matrix;
+
+/* Bytes of a matrix's codes and scales (host arithmetic).  MICRO_EINVAL for a
+ * negative side or NULL outputs, MICRO_ERANGE for one above 2^24. */
+MICRO_API micro_status micro_mx4_bytes(int64_t rows, int64_t cols, int64_t *codes, int64_t *scales);
+
+/* A handle for calls on hip_stream and the current device.  Holds no scratch; the
+ * first product whose sum is cut into parts allocates 64 MB (make such a call
+ * before capturing one into a graph). */
+typedef struct micro_mx4 micro_mx4; /* opaque, owned by the library */
+MICRO_API micro_status micro_mx4_init(micro_mx4 **mx, void *hip_stream);
+
+/*
+ * Packs `rows` rows of `cols` values of `type` (row stride in values, >= cols)
+ * into *packed (rows x cols), *turned (cols x rows, the transposed matrix, whose
+ * blocks run along the rows of x), or both from one read; either may be NULL.
+ * MICRO_EINVAL for sides that do not fit x or an output that shares memory.
+ */
+MICRO_API micro_status micro_mx4_pack(micro_mx4 *mx, const void *x, int32_t type, int64_t stride, int64_t rows,
+                                      int64_t cols, const micro_mx4_matrix *packed, const micro_mx4_matrix *turned);
+
+/* The values that a packed matrix stands for, rounded to `type` once (binary32 and
+ * bfloat16 hold them exactly). */
+MICRO_API micro_status micro_mx4_unpack(micro_mx4 *mx, const micro_mx4_matrix *packed, void *out, int32_t type,
+                                        int64_t stride);
+
+/*
+ * out[i][j] = sum over k of a[i][k] b[j][k] (a: m x k, b: n x k, out: m rows of n
+ * values of `type`): products of values are exact, sums in binary32 and an order
+ * that only the sizes determine, rounded to the type once.  accumulate != 0 adds to
+ * out before rounding.  A value of 0 times a NaN block is NaN.  With cols == 0 the
+ * sum is 0.
+ */
+MICRO_API micro_status micro_mx4_product(micro_mx4 *mx, const micro_mx4_matrix *a, const micro_mx4_matrix *b,
+                                         int32_t accumulate, void *out, int32_t type, int64_t stride);
+
+/*
+ * The product with an a that is packed on the way: x has a->rows rows of a->cols
+ * values of x_type; *a is scratch for their packed form, whose contents are
+ * undefined afterwards.
+ */
+MICRO_API micro_status micro_mx4_linear(micro_mx4 *mx, const void *x, int32_t x_type, int64_t x_stride,
+                                        const micro_mx4_matrix *a, const micro_mx4_matrix *b, int32_t accumulate,
+                                        void *out, int32_t type, int64_t stride);
+
+/* Releases the handle's scratch after waiting for its stream; NULL is a no-op. */
+MICRO_API void micro_mx4_free(micro_mx4 *mx);
 
 #ifdef __cplusplus
 }

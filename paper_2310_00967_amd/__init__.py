@@ -21,6 +21,14 @@ Around the step on a language model (language.py):
     x = table.lookup(weight, ids)
     loss, losses, dhidden, dweight = table.loss_grad(hidden, weight, targets)
     table.lookup_grad(dx, ids, dweight, accumulate=True)
+    ids, logprobs = table.sample(logits, uniforms, temperature=0.8, top_k=50, top_p=0.95)
+
+Microscaled 4-bit matrices and their products (microscaled.py):
+
+    mx = Microscaled()
+    w, wt = mx.pack_both(weight)                   # along the rows, and of the transpose
+    y = mx.linear(x, w)                            # x packed on the way
+    dx = mx.product(mx.pack(dy), wt, dtype=x.dtype)
 """
 import ctypes
 
@@ -31,6 +39,7 @@ from ._lib import (MICRO_FLAG_SEPARATE_SCAN, MICRO_FLAG_TIME_KERNEL, MICRO_RULE_
                    MICRO_TOPK_ROUTE_LIST, MICRO_VARIANT_STAGED, MICRO_VARIANT_TICKET, MicroError, default_config, micro_cycle, micro_estimate_threshold,
                    micro_partition, micro_threshold_f32)
 from .language import GradientSet, TokenTable
+from .microscaled import Microscaled, PackedMatrix
 
 __all__ = ["Sparsifier", "MicroError", "default_config", "micro_partition", "micro_cycle",
            "micro_estimate_threshold", "micro_threshold_f32", "MICRO_RULE_PROPORTIONAL",
@@ -38,7 +47,8 @@ __all__ = ["Sparsifier", "MicroError", "default_config", "micro_partition", "mic
            "MICRO_VARIANT_TICKET",
            "MICRO_VARIANT_STAGED",
            "MICRO_FLAG_TIME_KERNEL", "MICRO_FLAG_SEPARATE_SCAN", "MICRO_TOPK_ROUTE_FULL", "MICRO_TOPK_ROUTE_LIST",
-           "MICRO_TOPK_ROUTE_HINT_LIST", "MICRO_TOPK_ROUTE_HINT_PICK", "GradientSet", "TokenTable"]
+           "MICRO_TOPK_ROUTE_HINT_LIST", "MICRO_TOPK_ROUTE_HINT_PICK", "GradientSet", "TokenTable",
+           "Microscaled", "PackedMatrix"]
 
 
 class Sparsifier:

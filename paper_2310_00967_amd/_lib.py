@@ -41,8 +41,21 @@ class micro_table_config(ctypes.Structure):
     _fields_ = [("padding_id", ctypes.c_int64), ("ignored", ctypes.c_int64), ("score_bytes", ctypes.c_int64)]
 
 
+class micro_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_double), ("top_p", ctypes.c_double), ("min_p", ctypes.c_double),
+                ("top_k", ctypes.c_int64), ("temperatures", ctypes.c_void_p), ("top_ps", ctypes.c_void_p),
+                ("min_ps", ctypes.c_void_p), ("top_ks", ctypes.c_void_p)]
+
+
+class micro_mx4_matrix(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
+
+
 _cfgp = ctypes.POINTER(micro_config)
 _tcfgp = ctypes.POINTER(micro_table_config)
+_samplingp = ctypes.POINTER(micro_sampling)
+_mx4p = ctypes.POINTER(micro_mx4_matrix)
 _ptr, _i64, _i32, _dbl = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_double
 
 SIGNATURES = {
@@ -88,7 +101,15 @@ SIGNATURES = {
     "micro_table_loss": (ctypes.c_int, [_ptr, _ptr, _i64, _ptr, _i64, _ptr, _i32, _i64, _i32, _ptr, _ptr]),
     "micro_table_loss_grad": (ctypes.c_int, [_ptr, _ptr, _i64, _ptr, _i64, _ptr, _i32, _i64, _i32, _dbl, _i32, _ptr,
                                              _ptr, _ptr, _i64, _ptr, _i64]),
+    "micro_table_sample": (ctypes.c_int, [_ptr, _ptr, _i32, _i64, _i64, _ptr, _samplingp, _ptr, _i32, _ptr]),
     "micro_table_free": (None, [_ptr]),
+    "micro_mx4_bytes": (ctypes.c_int, [_i64, _i64, _i64p, _i64p]),
+    "micro_mx4_init": (ctypes.c_int, [ctypes.POINTER(_ptr), _ptr]),
+    "micro_mx4_pack": (ctypes.c_int, [_ptr, _ptr, _i32, _i64, _i64, _i64, _mx4p, _mx4p]),
+    "micro_mx4_unpack": (ctypes.c_int, [_ptr, _mx4p, _ptr, _i32, _i64]),
+    "micro_mx4_product": (ctypes.c_int, [_ptr, _mx4p, _mx4p, _i32, _ptr, _i32, _i64]),
+    "micro_mx4_linear": (ctypes.c_int, [_ptr, _ptr, _i32, _i64, _mx4p, _mx4p, _i32, _ptr, _i32, _i64]),
+    "micro_mx4_free": (None, [_ptr]),
 }
 
 _lib = None
@@ -306,3 +327,20 @@ def micro_table_init(vocab, dim, max_tokens, value_type, stream_handle=None, cfg
 
 def micro_table_free(table):
     load().micro_table_free(table)
+
+
+def micro_mx4_bytes(rows, cols):
+    """(bytes of the codes, bytes of the scales) of a packed matrix."""
+    codes, scales = ctypes.c_int64(), ctypes.c_int64()
+    check(load().micro_mx4_bytes(int(rows), int(cols), ctypes.byref(codes), ctypes.byref(scales)))
+    return codes.value, scales.value
+
+
+def micro_mx4_init(stream_handle=None):
+    mx = ctypes.c_void_p()
+    check(load().micro_mx4_init(ctypes.byref(mx), ctypes.c_void_p(stream_handle or 0)))
+    return mx
+
+
+def micro_mx4_free(mx):
+    load().micro_mx4_free(mx)

@@ -39,8 +39,9 @@ DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-p
 TAKEOVER_LIB = os.path.join(ROOT, "tests", "libmicro_takeover.so")
 TAKEOVER = ["-DMICRO_PASS_PATIENCE=1", "-DMICRO_PASS_ABSENT"]
 KERNEL_SOURCES = ["sparsify_kernel.hip", "union_kernel.hip", "static_scratch.hip", "topk_kernel.hip",
-                  "gradients_kernel.hip", "lookup_kernel.hip", "loss_kernel.hip"]
-HOST_SOURCES = ["micro_sparsify.cpp", "gradients.cpp", "token_table.cpp"]
+                  "gradients_kernel.hip", "lookup_kernel.hip", "loss_kernel.hip",
+                  "sample_kernel.hip", "mx4_kernel.hip"]
+HOST_SOURCES = ["micro_sparsify.cpp", "gradients.cpp", "token_table.cpp", "mx4.cpp"]
 
 
 def _run(cmd, verbose):

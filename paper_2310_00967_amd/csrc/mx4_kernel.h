@@ -1,0 +1,35 @@
+// Launches of the microscaled 4-bit calls (mx4_kernel.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "lookup_kernel.h"
+
+namespace micro {
+
+// Values of a block, which share a scale, and of a group: a row's codes lie in
+// 128-byte lines of one group each.
+constexpr int kMxBlock = 32, kMxGroup = 256, kMxLine = kMxGroup / 2;
+
+struct Mx4 {
+    char* codes;      // [rows][groups][kMxLine]
+    uint8_t* scales;  // [groups][rows][8]
+    int64_t rows, cols, groups;
+};
+
+// packed, turned: codes NULL where not wanted.
+hipError_t launch_mx4_pack(const Rows& x, int64_t rows, int64_t cols, const Mx4& packed, const Mx4& turned,
+                           hipStream_t stream);
+hipError_t launch_mx4_unpack(const Mx4& packed, const Rows& out, hipStream_t stream);
+
+// out[i][j] (+)= sum over k of a[i][k] b[j][k].
+struct Mx4Product {
+    Mx4 a, b;
+    Rows out;
+    bool accumulate;
+};
+hipError_t launch_mx4_product(const Mx4Product& call, hipStream_t stream);
+
+}  // namespace micro

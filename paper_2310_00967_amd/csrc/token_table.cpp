@@ -3,11 +3,11 @@
 #include <cmath>
 #include <new>
 
-#include "host_util.h"
+#include "handle_util.h"
 #include "lookup_kernel.h"
 #include "loss_kernel.h"
 #include "micro_sparsify.h"
-#include "strided_rows.h"
+#include "sample_kernel.h"
 
 namespace {
 
@@ -17,20 +17,6 @@ constexpr int64_t kMostTokens = int64_t(1) << 22;
 // Of the loss: 32-bit offsets within a product tile.
 constexpr int64_t kMostLossVocab = int64_t(1) << 22;
 constexpr int64_t kMostDim = 65536;
-
-int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-
-// Device memory cut into parts, each aligned to 256 bytes: first the sizes are
-// added up, then one allocation is handed out in the same order.
-struct Parts {
-    char* base = nullptr;
-    int64_t used = 0;
-    template <class T>
-    void take(T*& p, int64_t bytes) {
-        p = base ? reinterpret_cast<T*>(base + used) : nullptr;
-        used += round_up(bytes, 256);
-    }
-};
 
 }  // namespace
 
@@ -54,27 +40,6 @@ struct micro_table {
 
 namespace {
 
-// Allocates what `lay_out` takes, once.
-template <class LayOut>
-micro_status ensure(void** memory, const char* what, LayOut lay_out) {
-    if (*memory) return MICRO_OK;
-    Parts parts;
-    lay_out(parts);
-    void* p = nullptr;
-    const hipError_t e = hipMalloc(&p, static_cast<size_t>(std::max<int64_t>(parts.used, 256)));
-    if (e != hipSuccess) {
-        forget_hip_error();
-        lay_out(parts = Parts{});  // no part points anywhere
-        set_thread_error("%s: %lld bytes of device scratch: %s", what, static_cast<long long>(parts.used),
-                         hipGetErrorString(e));
-        return e == hipErrorOutOfMemory ? MICRO_ENOMEM : MICRO_EHIP;
-    }
-    *memory = p;
-    parts = Parts{static_cast<char*>(p), 0};
-    lay_out(parts);
-    return MICRO_OK;
-}
-
 void release(micro_table* t) {
     if (!t) return;
     CallDevice scope(t->device);
@@ -84,25 +49,10 @@ void release(micro_table* t) {
     delete t;
 }
 
-struct Region {
-    RowSpan rows;
-    bool written;
-};
-
-template <int N>
-micro_status check_apart(const Region (&r)[N]) {
-    for (int i = 0; i < N; ++i)
-        for (int j = i + 1; j < N; ++j)
-            if ((r[i].written || r[j].written) && rows_share_bytes(r[i].rows, r[j].rows))
-                return refuse("an output shares memory with another argument");
-    return MICRO_OK;
-}
-
-// An argument's rows, and `values` values one after the other, in bytes.
+// An argument's rows.
 RowSpan rows_of(const micro_table* t, const void* at, int64_t rows, int64_t stride) {
     return {at, rows, stride * t->size(), t->dim * t->size()};
 }
-RowSpan run_of(const void* at, int64_t values, int64_t size) { return {at, 1, values * size, values * size}; }
 
 micro_status check_rows(const micro_table* t, const void* at, int64_t stride, int64_t rows) {
     if (stride < t->dim) return refuse("a row stride is below the table's dim");
@@ -329,6 +279,49 @@ micro_status micro_table_loss_grad(micro_table* t, const void* hidden, int64_t h
                                    void* dhidden, int64_t dhidden_stride, void* dweight, int64_t dweight_stride) {
     return run_loss(t, hidden, hidden_stride, weight, weight_stride, targets, targets_type, tokens, mean != 0, losses,
                     loss, true, scale, accumulate != 0, dhidden, dhidden_stride, dweight, dweight_stride);
+}
+
+micro_status micro_table_sample(micro_table* t, const void* logits, int32_t logits_type, int64_t logits_stride,
+                                int64_t rows, const float* uniforms, const micro_sampling* sampling, void* ids,
+                                int32_t ids_type, float* logprobs) {
+    if (!t) return refuse("table is NULL");
+    if (!type_valid(logits_type)) return refuse("unknown type of logits");
+    if (micro_status st = check_tokens(t, ids, ids_type, rows)) return st;
+    if (t->vocab > kMostLossVocab) {
+        set_thread_error("a draw from %lld tokens: at most 2^22", static_cast<long long>(t->vocab));
+        return MICRO_ERANGE;
+    }
+    const int64_t size = type_bytes(logits_type);
+    if (micro_status st = check_strided(logits, logits_stride, rows, t->vocab, size)) return st;
+    if ((rows > 0 && !uniforms) || !aligned_to(uniforms, 4) || !aligned_to(logprobs, 4))
+        return refuse("uniforms are NULL or not 4-byte aligned, or logprobs are not");
+    if (!sampling) return refuse("sampling is NULL");
+    const micro_sampling& s = *sampling;
+    if (!s.temperatures && !(s.temperature >= 0.0)) return refuse("temperature is negative or NaN");
+    if (!s.top_ps && !(s.top_p > 0.0 && s.top_p <= 1.0)) return refuse("top_p is outside (0, 1]");
+    if (!s.min_ps && !(s.min_p >= 0.0 && s.min_p <= 1.0)) return refuse("min_p is outside [0, 1]");
+    for (const void* p : {static_cast<const void*>(s.temperatures), static_cast<const void*>(s.top_ps),
+                          static_cast<const void*>(s.min_ps), static_cast<const void*>(s.top_ks)})
+        if (!aligned_to(p, 4)) return refuse("an array of settings is not 4-byte aligned");
+    const Region regions[] = {{{logits, rows, logits_stride * size, t->vocab * size}, false},
+                              {run_of(uniforms, rows, 4), false},
+                              {run_of(s.temperatures, s.temperatures ? rows : 0, 4), false},
+                              {run_of(s.top_ps, s.top_ps ? rows : 0, 4), false},
+                              {run_of(s.min_ps, s.min_ps ? rows : 0, 4), false},
+                              {run_of(s.top_ks, s.top_ks ? rows : 0, 4), false},
+                              {ids_of(ids, ids_type, rows), true},
+                              {run_of(logprobs, logprobs ? rows : 0, 4), true}};
+    if (micro_status st = check_apart(regions)) return st;
+    CallDevice scope(t->device);
+    SampleCall c{};
+    c.logits = {const_cast<void*>(logits), logits_stride, logits_type};
+    c.rows = rows;
+    c.vocab = t->vocab;
+    c.uniforms = uniforms;
+    c.sampling = s;
+    c.ids = {ids, ids_type == MICRO_IDS_I64};
+    c.logprobs = logprobs;
+    return report_hip(launch_sample(c, t->stream), "token draw launch");
 }
 
 void micro_table_free(micro_table* t) { release(t); }

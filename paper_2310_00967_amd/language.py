@@ -69,6 +69,13 @@ class _Enqueued:
             if t is not None:
                 t.record_stream(self.stream)
 
+    def _outside_autograd(self, t, name):
+        if t.requires_grad and self._torch.is_grad_enabled():
+            raise RuntimeError(f"{name} requires its gradient, which this call does not record: call under "
+                               "torch.no_grad() or pass its detach()")
+        if self._forward_ad._current_level >= 0 and self._forward_ad.unpack_dual(t).tangent is not None:
+            raise RuntimeError(f"{name} has a tangent, which this call does not carry on")
+
     def _scalar(self, t, name, dtype):
         if not isinstance(t, self._torch.Tensor) or t.dtype != dtype or t.device != self.device or t.numel() != 1:
             raise TypeError(f"{name} must be one {dtype} on {self.device}")
@@ -210,6 +217,8 @@ class TokenTable(_Enqueued):
         lib = _lib.load()
         self._lookup_fn, self._lookup_grad_fn = lib.micro_table_lookup, lib.micro_table_lookup_grad
         self._loss_fn, self._loss_grad_fn = lib.micro_table_loss, lib.micro_table_loss_grad
+        self._sample_fn = lib.micro_table_sample
+        self._value_types = types
         # the native marshalling of the lookup's plain case
         self._caller = _lib.load_caller("TableCaller")(
             ctypes.cast(self._lookup_fn, ctypes.c_void_p).value, self._handle.value, self.vocab, self.dim,
@@ -232,11 +241,7 @@ class TokenTable(_Enqueued):
         """(address, row stride) of `rows` rows of dim values."""
         if not isinstance(t, self._tensor) or t.dtype is not self.dtype or not t.is_cuda or t.get_device() != self._index:
             raise TypeError(f"{name} must be a {self.dtype} tensor on {self.device}")
-        if t.requires_grad and self._torch.is_grad_enabled():
-            raise RuntimeError(f"{name} requires its gradient, which this call does not record: call under "
-                               "torch.no_grad() or pass its detach()")
-        if self._forward_ad._current_level >= 0 and self._forward_ad.unpack_dual(t).tangent is not None:
-            raise RuntimeError(f"{name} has a tangent, which this call does not carry on")
+        self._outside_autograd(t, name)
         if t.dim() < 1 or t.shape[-1] != self.dim or t.numel() != rows * self.dim:
             raise ValueError(f"{name} must hold {rows} rows of {self.dim} values")
         if t.is_contiguous():
@@ -342,3 +347,66 @@ class TokenTable(_Enqueued):
         if foreign:
             self._used(hidden, weight, targets, dhidden, dweight)
         return loss, losses, dhidden, dweight
+
+    def _setting(self, sampling, name, value, dtype, rows):
+        """Enters one of sample's settings: a number, or a tensor of one a row,
+        which is returned."""
+        if not isinstance(value, self._tensor):
+            setattr(sampling, name, value)
+            return None
+        if value.dtype != dtype or not value.is_cuda or value.get_device() != self._index or not value.is_contiguous():
+            raise TypeError(f"{name} must be a number or a contiguous {dtype} tensor on {self.device}")
+        if value.numel() != rows:
+            raise ValueError(f"{name} must hold {rows} values")
+        setattr(sampling, name + "s", value.data_ptr())
+        return value
+
+    def sample(self, logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None):
+        """Draws a token from each of the logits' rows by the given random numbers.
+        Returns (ids, logprobs) of the shape of uniforms: int64 (or the given int32
+        or int64 out) and float32, the logarithm of the drawn token's share of what
+        is kept.
+
+        logits: float32, float16 or bfloat16 rows of vocab values, strided or of any
+        contiguous shape; uniforms: float32 in [0, 1).  top_k keeps the k largest
+        (0: all), top_p of those the fewest that reach that share, min_p of those the
+        ones with at least that share of the largest's; equal logits go by their
+        index.  Each may be a tensor of one value a row (float32, top_k int32).
+        temperature 0 takes the first largest logit.  Logits of -inf or NaN have no
+        part; a row without any other gives -1 and NaN."""
+        handle = self._open()
+        foreign = self._foreign()
+        torch = self._torch
+        if not isinstance(uniforms, self._tensor) or uniforms.dtype is not torch.float32 or not uniforms.is_cuda \
+                or uniforms.get_device() != self._index or not uniforms.is_contiguous():
+            raise TypeError(f"uniforms must be a contiguous float32 tensor on {self.device}")
+        rows = uniforms.numel()
+        if not isinstance(logits, self._tensor) or logits.dtype not in self._value_types or not logits.is_cuda \
+                or logits.get_device() != self._index:
+            raise TypeError(f"logits must be a float32, float16 or bfloat16 tensor on {self.device}")
+        if logits.dim() < 1 or logits.shape[-1] != self.vocab or logits.numel() != rows * self.vocab:
+            raise ValueError(f"logits must hold {rows} rows of {self.vocab} values")
+        self._outside_autograd(logits, "logits")
+        stride = self.vocab
+        if not logits.is_contiguous():
+            if logits.dim() != 2 or (self.vocab > 1 and logits.stride(1) != 1) or \
+                    (rows > 1 and logits.stride(0) < self.vocab):
+                raise TypeError("logits must be contiguous, or two-dimensional with adjacent values in a row")
+            stride = logits.stride(0) if rows > 1 else self.vocab
+        sampling = _lib.micro_sampling()
+        arrays = [self._setting(sampling, "temperature", temperature, torch.float32, rows),
+                  self._setting(sampling, "top_k", top_k, torch.int32, rows),
+                  self._setting(sampling, "top_p", top_p, torch.float32, rows),
+                  self._setting(sampling, "min_p", min_p, torch.float32, rows)]
+        ids = self._empty(uniforms.shape, torch.int64, foreign) if out is None else out
+        at, kind, count = self._ids(ids, "out")
+        if count != rows:
+            raise ValueError(f"out must hold {rows} ids")
+        logprobs = self._empty(uniforms.shape, torch.float32, foreign)
+        st = self._sample_fn(handle, logits.data_ptr(), self._value_types[logits.dtype], stride, rows, uniforms.data_ptr(),
+                             ctypes.byref(sampling), at, kind, logprobs.data_ptr())
+        if st:
+            _lib.check(st)
+        if foreign:
+            self._used(logits, uniforms, *arrays, out)
+        return ids, logprobs

@@ -1,0 +1,238 @@
+"""Drawing tokens from logits on the GPU, against its definition: the token has to
+be the one that is drawn there, its probability within derived bounds."""
+import math
+
+import pytest
+import torch
+
+import paper_2310_00967_amd as micro
+
+import sample_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+def check(table, logits, uniforms, out=None, **settings):
+    """settings: numbers or CPU tensors of one a row."""
+    given = {k: v.to(DEV) if isinstance(v, torch.Tensor) else v for k, v in settings.items()}
+    ids, logprobs = table.sample(logits.to(DEV), uniforms.to(DEV), out=out, **given)
+    assert ids.shape == uniforms.shape and logprobs.dtype == torch.float32
+    rows = uniforms.numel()
+    flat = logits.reshape(rows, -1).double()
+    for r in range(rows):
+        own = {k: v[r].item() if isinstance(v, torch.Tensor) else v for k, v in settings.items()}
+        tokens, share = ref.draw(flat[r].numpy(), float(uniforms.flatten()[r]), **own)
+        got, logprob = int(ids.flatten()[r]), float(logprobs.flatten()[r])
+        assert got in tokens, (r, got, tokens, own)
+        if got == -1:
+            assert math.isnan(logprob)
+        else:
+            # one rounding to binary32; before it two logarithms' few 2^-53 of their size, and the
+            # sum's own roundings, 2^-40 of it at the least
+            assert abs(logprob - share[got]) <= 2.0 ** -24 * abs(share[got]) + 2.0 ** -40 * (1 + abs(share[got])), (r, own)
+    return ids, logprobs
+
+
+def rows_of(rows, vocab, dtype, seed, spread=2.5):
+    gen = torch.Generator().manual_seed(seed)
+    return (torch.randn(rows, vocab, generator=gen) * spread).to(dtype), torch.rand(rows, generator=gen)
+
+
+SETTINGS = [{}, {"temperature": 0.0}, {"temperature": 0.7}, {"temperature": 1.6}, {"top_k": 1}, {"top_k": 40},
+            {"top_k": 1000}, {"top_p": 0.9}, {"top_p": 0.3}, {"top_p": 1e-9}, {"min_p": 0.05}, {"min_p": 1.0},
+            {"temperature": 0.8, "top_k": 50, "top_p": 0.95}, {"temperature": 1.3, "top_k": 500, "top_p": 0.8, "min_p": 0.01},
+            {"temperature": 3.0, "top_p": 0.999}, {"temperature": 1e-3, "top_p": 0.9}, {"temperature": 1e6}]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("settings", SETTINGS, ids=lambda s: "-".join(f"{k}{v}" for k, v in s.items()) or "plain")
+@pytest.mark.parametrize("rows,vocab", [(3, 1), (5, 2), (6, 63), (4, 1000), (3, 8193), (2, 30522)])
+def test_sample(dtype, settings, rows, vocab):
+    logits, uniforms = rows_of(rows, vocab, dtype, vocab)
+    check(micro.TokenTable(vocab, 1, rows), logits, uniforms, **settings)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_settings_of_every_row(dtype):
+    rows, vocab = 48, 4099
+    logits, uniforms = rows_of(rows, vocab, dtype, 5)
+    gen = torch.Generator().manual_seed(8)
+    pick = lambda v, t: torch.tensor(v, dtype=t)[torch.randint(len(v), (rows,), generator=gen)]  # noqa: E731
+    check(micro.TokenTable(vocab, 1, rows), logits, uniforms, temperature=pick([0.0, 0.5, 1.0, 2.0], torch.float32),
+          top_k=pick([0, 1, 7, 300, 4098, 4099, 5000], torch.int32), top_p=pick([1.0, 0.5, 0.97], torch.float32),
+          min_p=pick([0.0, 0.02, 0.5], torch.float32))
+
+
+def test_settings_of_a_row_that_are_out_of_range():
+    """Arrays cannot be looked at: what is not above 0 is a temperature of 0, a NaN
+    top_p or min_p keeps all, a top_p of 0 keeps one."""
+    vocab = 300
+    logits, uniforms = rows_of(6, vocab, torch.float32, 3)
+    nan = math.nan
+    f = lambda *v: torch.tensor(v, device=DEV)  # noqa: E731
+    table = micro.TokenTable(vocab, 1, 6)
+    got = table.sample(logits.to(DEV), uniforms.to(DEV), temperature=f(-1.0, nan, 1.0, 1.0, 1.0, 1.0),
+                       top_p=f(1.0, 1.0, nan, 0.0, -3.0, 7.0), min_p=f(0.0, 0.0, nan, 0.0, 0.0, -1.0),
+                       top_k=torch.tensor([0, 0, -5, 0, 0, 0], dtype=torch.int32, device=DEV))
+    want = check(table, logits, uniforms, temperature=torch.tensor([0.0, 0.0, 1.0, 1.0, 1.0, 1.0]),
+                 top_p=torch.tensor([1.0, 1.0, 1.0, 1e-9, 1e-9, 1.0]))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("settings", [{}, {"top_k": 20}, {"top_p": 0.5}, {"top_k": 30, "top_p": 0.5}, {"min_p": 0.9},
+                                      {"temperature": 0.0}, {"top_k": 700, "top_p": 0.9}])
+def test_many_equal_logits(dtype, settings):
+    """Cuts that fall among equal logits take them by their index."""
+    gen = torch.Generator().manual_seed(6)
+    vocab, rows = 5001, 12
+    logits = torch.randint(0, 4, (rows, vocab), generator=gen).float().sub(2.0)
+    logits[0] = 0.0
+    logits[1] = -0.0
+    logits[1, ::3] = 0.0
+    logits[2, 4000:] = 9.0
+    logits[3, 17] = 9.0
+    check(micro.TokenTable(vocab, 1, rows), logits.to(dtype), torch.rand(rows, generator=gen), **settings)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("settings", [{}, {"top_k": 5}, {"top_p": 0.8}, {"temperature": 0.0}, {"min_p": 0.1},
+                                      {"temperature": math.inf}])
+def test_masked_rows_and_values_that_are_not_finite(dtype, settings):
+    logits, uniforms = rows_of(10, 777, dtype, 2)
+    inf = math.inf
+    logits[0] = -inf
+    logits[1] = math.nan
+    logits[2] = -inf
+    logits[2, 776] = -5.0
+    logits[3, ::2] = -inf
+    logits[4, 1::2] = math.nan
+    logits[5, [3, 70, 500]] = inf
+    logits[6, 0] = inf
+    logits[7, 100:] = torch.finfo(dtype).min  # a mask of the type's lowest value
+    logits[8] = torch.finfo(dtype).min
+    logits[9, 5] = torch.finfo(dtype).max
+    ids, _ = check(micro.TokenTable(777, 1, 10), logits, uniforms, **settings)
+    assert ids[:3].tolist() == [-1, -1, 776] and int(ids[6]) == 0
+    if settings.get("temperature") != inf:  # at which every finite logit weighs exp(0)
+        assert int(ids[9]) == 5
+
+
+def test_uniforms_at_the_ends():
+    vocab = 1000
+    logits, _ = rows_of(1, vocab, torch.float32, 4)
+    logits[0, :10] = -math.inf
+    logits[0, 990:] = -math.inf
+    u = torch.tensor([0.0, -1.0, math.nan, 1.0, 2.0, math.inf, 1.0 - 2.0 ** -24, 2.0 ** -149])
+    table = micro.TokenTable(vocab, 1, u.numel())
+    ids, _ = check(table, logits.expand(u.numel(), vocab).contiguous(), u)
+    assert ids[:3].tolist() == [10, 10, 10] and ids[3:6].tolist() == [989, 989, 989]
+    same = torch.zeros(4, 8)  # borders that are exact: u on one belongs to the token behind it
+    ids, logprobs = check(micro.TokenTable(8, 1, 4), same, torch.tensor([0.125, 0.5, 0.4999, 0.875]))
+    assert ids.tolist() == [1, 4, 3, 7] and torch.equal(logprobs.cpu(), torch.full((4,), 0.125).log())
+
+
+def test_frequencies():
+    """10^5 draws of one row: counts within five standard deviations."""
+    vocab, draws = 50, 100_000
+    logits, _ = rows_of(1, vocab, torch.float32, 11, spread=1.5)
+    uniforms = torch.rand(draws, generator=torch.Generator().manual_seed(12))
+    table = micro.TokenTable(vocab, 1, draws)
+    ids, logprobs = table.sample(logits.to(DEV).expand(draws, vocab).contiguous(), uniforms.to(DEV), top_k=30)
+    kept = torch.topk(logits[0].double(), 30)
+    p = torch.zeros(vocab, dtype=torch.float64).scatter(0, kept.indices, torch.softmax(kept.values, 0))
+    count = torch.bincount(ids.cpu(), minlength=vocab).double()
+    assert bool(((count - draws * p).abs() <= 5 * (draws * p * (1 - p)).sqrt() + 1e-9).all())
+    assert torch.allclose(logprobs.cpu().exp().double(), p[ids.cpu()], rtol=1e-6, atol=0)
+
+
+def test_layouts_types_of_ids_and_repeats():
+    vocab, rows = 1031, 6
+    logits, uniforms = rows_of(rows, vocab, torch.bfloat16, 9)
+    table = micro.TokenTable(vocab, 1, rows)
+    want = check(table, logits, uniforms, top_p=0.9)
+    base = torch.zeros(rows, vocab + 100, dtype=torch.bfloat16, device=DEV)
+    base[:, 33:33 + vocab] = logits.to(DEV)
+    got = table.sample(base[:, 33:33 + vocab], uniforms.to(DEV), top_p=0.9)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    out = torch.full((rows,), 7, dtype=torch.int32, device=DEV)
+    got = table.sample(logits.to(DEV), uniforms.to(DEV), top_p=0.9, out=out)
+    assert got[0] is out and torch.equal(out.long(), want[0])
+    got = table.sample(logits.to(DEV).view(2, 3, vocab), uniforms.to(DEV).view(2, 3), top_p=0.9)
+    assert got[0].shape == (2, 3) and torch.equal(got[0].flatten(), want[0])
+    assert table.sample(torch.empty(0, vocab, device=DEV), torch.empty(0, device=DEV))[0].shape == (0,)
+
+
+def test_large_vocabulary_and_offsets_past_32_bits():
+    vocab = 2 ** 22
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    table = micro.TokenTable(vocab, 1, 600)
+    logits = torch.full((600, vocab), -20.0, dtype=torch.bfloat16, device=DEV)  # 2.5e9 values
+    logits[:, ::1 << 14] = 3.0
+    logits[-1, -1] = 30.0
+    u = torch.rand(600, generator=gen, device=DEV)
+    for settings in ({}, {"top_k": 200}, {"top_p": 0.9}):
+        ids, _ = table.sample(logits, u, **settings)
+        assert int(ids[-1]) == vocab - 1
+        few = [0, 299, 598]
+        for r in few:
+            tokens, _ = ref.draw(logits[r].double().cpu().numpy(), float(u[r]), **settings)
+            assert int(ids[r]) in tokens
+
+
+def test_another_stream_and_a_captured_graph():
+    vocab, rows = 3001, 40
+    logits, uniforms = rows_of(rows, vocab, torch.float32, 21)
+    logits, uniforms = logits.to(DEV), uniforms.to(DEV)
+    table = micro.TokenTable(vocab, 1, rows)
+    want = table.sample(logits, uniforms, top_p=0.9, top_k=100)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    other = micro.TokenTable(vocab, 1, rows, stream=stream)
+    got = other.sample(logits, uniforms, top_p=0.9, top_k=100)
+    torch.cuda.current_stream().wait_stream(stream)
+    assert torch.equal(got[0], want[0])
+    with torch.cuda.stream(stream):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            ids, logprobs = other.sample(logits, uniforms, top_p=0.9, top_k=100)
+    for _ in range(4):
+        uniforms.uniform_()
+        logits.mul_(0.9)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = table.sample(logits, uniforms, top_p=0.9, top_k=100)
+        assert torch.equal(ids, want[0]) and torch.equal(logprobs, want[1])
+
+
+def test_refusals():
+    vocab = 100
+    logits, uniforms = rows_of(4, vocab, torch.float32, 1)
+    logits, uniforms = logits.to(DEV), uniforms.to(DEV)
+    table = micro.TokenTable(vocab, 1, 4)
+    out = torch.full((4,), 7, dtype=torch.int64, device=DEV)
+    for settings, error in [({"temperature": -1.0}, micro.MicroError), ({"temperature": math.nan}, micro.MicroError),
+                            ({"top_p": 0.0}, micro.MicroError), ({"top_p": 1.5}, micro.MicroError),
+                            ({"top_p": math.nan}, micro.MicroError), ({"min_p": -0.1}, micro.MicroError),
+                            ({"min_p": 1.1}, micro.MicroError), ({"top_k": 2.5}, TypeError), ({"top_p": "x"}, TypeError),
+                            ({"temperature": torch.ones(4)}, TypeError), ({"temperature": torch.ones(3, device=DEV)}, ValueError),
+                            ({"top_k": torch.ones(4, dtype=torch.int64, device=DEV)}, TypeError),
+                            ({"out": out[:3]}, ValueError), ({"out": out.float()}, TypeError)]:
+        with pytest.raises(error):
+            table.sample(logits, uniforms, **({"out": out} | settings))
+    for a, b, error in [(logits.double(), uniforms, TypeError), (logits, uniforms.double(), TypeError),
+                        (logits[:, :50], uniforms, ValueError), (logits[:3], uniforms, ValueError),
+                        (logits.cpu(), uniforms, TypeError), (logits.t().contiguous().t(), uniforms, TypeError),
+                        (torch.nn.Parameter(logits), uniforms, RuntimeError)]:
+        with pytest.raises(error):
+            table.sample(a, b, out=out)
+    with pytest.raises(micro.MicroError):  # more rows than the handle holds
+        table.sample(logits.repeat(2, 1), uniforms.repeat(2))
+    with pytest.raises(micro.MicroError):  # an output that is also an input
+        table.sample(logits, uniforms, out=logits.view(-1)[:8].view(torch.int64))
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())
