@@ -623,11 +623,12 @@ MICRO_API void micro_table_free(micro_table *table);
  * -127, and the code is that of value / 2^e, to nearest, ties to the even code,
  * at most 6.  A block that holds a NaN or an infinity is NaN (byte 255, codes 0).
  * A block of zeros has byte 0.
- *   codes   rows of pitch / 2 bytes, where pitch is cols rounded up to a multiple
- *           of 256: value c in byte c / 2, an even c in the lower half; 0 behind
- *           cols.  Aligned to 16 bytes.
- *   scales  the byte of block b of row r at ((b / 8) * rows + r) * 8 + b % 8, for
- *           the pitch / 32 blocks of a row.  Aligned to 8 bytes.
+ * A row is divided into groups of 128 values, the last one filled up with zeros.
+ *   codes   64 bytes for each group and row, the rows of a group one after the
+ *           other: value c of row r in byte ((c / 128) * rows + r) * 64 + c % 128 /
+ *           2, an even c in the lower half.  Aligned to 16 bytes.
+ *   scales  the byte of block b of row r at ((b / 4) * rows + r) * 4 + b % 4.
+ *           Aligned to 4 bytes.
  * Sides are at most 2^24 (MICRO_ERANGE).
  */
 typedef struct micro_mx4_matrix {
@@ -639,9 +640,9 @@ typedef struct micro_mx4_matrix {
  * negative side or NULL outputs, MICRO_ERANGE for one above 2^24. */
 MICRO_API micro_status micro_mx4_bytes(int64_t rows, int64_t cols, int64_t *codes, int64_t *scales);
 
-/* A handle for calls on hip_stream and the current device.  Holds no scratch; the
- * first product whose sum is cut into parts allocates 64 MB (make such a call
- * before capturing one into a graph). */
+/* A handle for calls on hip_stream and the current device, with scratch of 256 KB for
+ * each compute unit (64 MB), which its products share: two of one handle, captured into
+ * graphs too, must not run at once. */
 typedef struct micro_mx4 micro_mx4; /* opaque, owned by the library */
 MICRO_API micro_status micro_mx4_init(micro_mx4 **mx, void *hip_stream);
 

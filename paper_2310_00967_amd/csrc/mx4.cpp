@@ -6,8 +6,10 @@
 #include "mx4_kernel.h"
 
 struct micro_mx4 {
-    int device = -1;
+    int device = -1, compute_units = 256;
     hipStream_t stream = nullptr;
+    void* memory = nullptr;  // the parts of products
+    float* parts = nullptr;
 };
 
 namespace {
@@ -32,16 +34,16 @@ micro_status check_matrix(const micro_mx4_matrix* m) {
     if (!m) return refuse("a packed matrix is NULL");
     if (micro_status st = check_sides(m->rows, m->cols)) return st;
     if (m->rows > 0 && m->cols > 0 && (!m->codes || !m->scales)) return refuse("a packed matrix has NULL codes or scales");
-    if (!aligned_to(m->codes, 16) || !aligned_to(m->scales, 8))
-        return refuse("codes are not aligned to 16 bytes, or scales to 8");
+    if (!aligned_to(m->codes, 16) || !aligned_to(m->scales, 4))
+        return refuse("codes are not aligned to 16 bytes, or scales to 4");
     return MICRO_OK;
 }
 
 Mx4 matrix_of(const micro_mx4_matrix& m) {
     return {static_cast<char*>(m.codes), static_cast<uint8_t*>(m.scales), m.rows, m.cols, groups_of(m.cols)};
 }
-RowSpan codes_of(const micro_mx4_matrix* m) { return m ? run_of(m->codes, m->rows * groups_of(m->cols), kMxLine) : RowSpan{}; }
-RowSpan scales_of(const micro_mx4_matrix* m) { return m ? run_of(m->scales, m->rows * groups_of(m->cols), 8) : RowSpan{}; }
+RowSpan codes_of(const micro_mx4_matrix* m) { return m ? run_of(m->codes, m->rows * groups_of(m->cols), kMxBytes) : RowSpan{}; }
+RowSpan scales_of(const micro_mx4_matrix* m) { return m ? run_of(m->scales, m->rows * groups_of(m->cols), kMxBlocks) : RowSpan{}; }
 
 micro_status check_values(const void* at, int32_t type, int64_t stride, int64_t rows, int64_t cols) {
     if (!type_valid(type)) return refuse("unknown type");
@@ -62,7 +64,9 @@ micro_status check_product(const micro_mx4_matrix* a, const micro_mx4_matrix* b,
 
 micro_status run_product(micro_mx4* mx, const micro_mx4_matrix* a, const micro_mx4_matrix* b, int32_t accumulate,
                          void* out, int32_t type, int64_t stride) {
-    return report_hip(launch_mx4_product({matrix_of(*a), matrix_of(*b), {out, stride, type}, accumulate != 0}, mx->stream),
+    return report_hip(launch_mx4_product({matrix_of(*a), matrix_of(*b), {out, stride, type}, accumulate != 0,
+                                          mx->compute_units, mx->parts},
+                                         mx->stream),
                       "4-bit product launch");
 }
 
@@ -73,20 +77,29 @@ extern "C" {
 micro_status micro_mx4_bytes(int64_t rows, int64_t cols, int64_t* codes, int64_t* scales) {
     if (!codes || !scales) return refuse("an output is NULL");
     if (micro_status st = check_sides(rows, cols)) return st;
-    *codes = rows * groups_of(cols) * kMxLine;
-    *scales = rows * groups_of(cols) * 8;
+    *codes = rows * groups_of(cols) * kMxBytes;
+    *scales = rows * groups_of(cols) * kMxBlocks;
     return MICRO_OK;
 }
 
 micro_status micro_mx4_init(micro_mx4** out, void* hip_stream) {
     if (!out) return refuse("mx is NULL");
     *out = nullptr;
-    int device = -1;
-    if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return report_hip(e, "device of the 4-bit calls");
+    int device = -1, units = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, device);
+    if (e != hipSuccess) return report_hip(e, "device of the 4-bit calls");
     micro_mx4* mx = new (std::nothrow) micro_mx4;
     if (!mx) return MICRO_ENOMEM;
     mx->device = device;
+    mx->compute_units = std::max(units, 8);
     mx->stream = static_cast<hipStream_t>(hip_stream);
+    // with the handle, so that any of its calls may be captured into a graph
+    if (micro_status st = ensure(&mx->memory, "4-bit products",
+                                 [&](Parts& p) { p.take(mx->parts, mx->compute_units * kMxParts * 4); })) {
+        delete mx;
+        return st;
+    }
     *out = mx;
     return MICRO_OK;
 }
@@ -155,6 +168,7 @@ void micro_mx4_free(micro_mx4* mx) {
     if (!mx) return;
     CallDevice scope(mx->device);
     (void)hipStreamSynchronize(mx->stream);
+    if (mx->memory) (void)hipFree(mx->memory);
     delete mx;
 }
 

@@ -9,13 +9,14 @@
 
 namespace micro {
 
-// Values of a block, which share a scale, and of a group: a row's codes lie in
-// 128-byte lines of one group each.
-constexpr int kMxBlock = 32, kMxGroup = 256, kMxLine = kMxGroup / 2;
+// Values of a block, which share a scale, and of a group, whose codes and scales
+// lie beside those of the next row: a step of the products reads whole lines of a
+// tile's rows, whatever the rows' length.
+constexpr int kMxBlock = 32, kMxGroup = 128, kMxBlocks = kMxGroup / kMxBlock, kMxBytes = kMxGroup / 2;
 
 struct Mx4 {
-    char* codes;      // [rows][groups][kMxLine]
-    uint8_t* scales;  // [groups][rows][8]
+    char* codes;      // [groups][rows][kMxBytes]
+    uint8_t* scales;  // [groups][rows][kMxBlocks]
     int64_t rows, cols, groups;
 };
 
@@ -29,7 +30,10 @@ struct Mx4Product {
     Mx4 a, b;
     Rows out;
     bool accumulate;
+    int compute_units;
+    float* parts;  // scratch: the parts of tiles whose sums are cut, kMxParts floats a compute unit
 };
+constexpr int64_t kMxParts = 256 * 256;
 hipError_t launch_mx4_product(const Mx4Product& call, hipStream_t stream);
 
 }  // namespace micro

@@ -10,6 +10,7 @@
 
 #include "launch.h"
 #include "micro_sparsify.h"
+#include "product_tiles.h"
 #include "value_types.h"
 
 namespace micro {
@@ -17,7 +18,6 @@ namespace {
 
 using Words4 = int __attribute__((ext_vector_type(4)));
 using Words8 = int __attribute__((ext_vector_type(8)));
-using Acc = float __attribute__((ext_vector_type(16)));
 
 // What the two scales of a 32 x 32 x 64 product come from: the bytes of a word
 // for each lane's row, one of which (step) it takes.
@@ -73,18 +73,19 @@ __device__ __forceinline__ void load_some(const T* p, int64_t valid, float (&v)[
     }
 }
 
-// Rows: a workgroup takes kPackRows rows of kPackGroups groups, half a wavefront
-// a row's group, eight values a lane.
-constexpr int kPackThreads = 256, kPackRows = 16, kPackGroups = 4;
+// Rows: a workgroup takes kPackRows rows of kPackGroups groups, sixteen lanes a row's
+// group, eight values a lane, so that neighbouring lanes read one row and the
+// workgroup's stores fill whole lines of a group's rows.
+constexpr int kPackThreads = 256, kPackRows = 16, kPackGroups = 8, kPackLanes = kMxGroup / 8;
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* x, int64_t stride, Mx4 to) {
     const int64_t wide = (to.groups + kPackGroups - 1) / kPackGroups;
     const int64_t tiles = (to.rows + kPackRows - 1) / kPackRows * wide;
-    const int lane = threadIdx.x & 31, half = threadIdx.x >> 5;
-    constexpr int kRowsAtOnce = kPackThreads / 32 / kPackGroups;
+    const int lane = threadIdx.x % kPackLanes, part = threadIdx.x / kPackLanes;
+    constexpr int kRowsAtOnce = kPackThreads / kPackLanes / kPackGroups;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t g = tile % wide * kPackGroups + half % kPackGroups;
-        const int64_t r0 = tile / wide * kPackRows + half / kPackGroups;
+        const int64_t g = tile % wide * kPackGroups + part % kPackGroups;
+        const int64_t r0 = tile / wide * kPackRows + part / kPackGroups;
         if (g >= to.groups) continue;
         const int64_t c = g * kMxGroup + lane * 8;
 #pragma unroll
@@ -99,23 +100,28 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* x, int64_t 
             most = max(most, __shfl_xor(most, 1));
             most = max(most, __shfl_xor(most, 2));
             const uint32_t scale = scale_of(most);
-            *reinterpret_cast<uint32_t*>(to.codes + (r * to.groups + g) * kMxLine + lane * 4) = codes_of(v, scale);
-            if ((lane & 3) == 0) to.scales[(g * to.rows + r) * 8 + lane / 4] = static_cast<uint8_t>(scale);
+            *reinterpret_cast<uint32_t*>(to.codes + (g * to.rows + r) * kMxBytes + lane * 4) = codes_of(v, scale);
+            if ((lane & 3) == 0) to.scales[(g * to.rows + r) * kMxBlocks + lane / 4] = static_cast<uint8_t>(scale);
         }
     }
 }
 
 // Columns: a thread takes kVec adjacent columns of one block of 32 rows, the
-// eight blocks of a group beside each other, so a column's line of codes is
-// written by eight lanes.
+// four blocks of a group beside each other, so that the codes of neighbouring columns
+// are written as whole lines.
+template <class T>
+struct Turn {
+    static constexpr int kVec = 16 / sizeof(T), kAcross = 64 / kMxBlocks;  // threads of a wavefront along a row
+    static constexpr int kColumns = kAcross * kVec * kPackThreads / 64;
+};
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void pack_turned_kernel(const T* x, int64_t stride, Mx4 to) {
-    constexpr int kVec = 16 / sizeof(T), kColumns = 8 * kVec * kPackThreads / 64;
+    constexpr int kVec = Turn<T>::kVec, kAcross = Turn<T>::kAcross, kColumns = Turn<T>::kColumns;
     const int64_t across = (to.rows + kColumns - 1) / kColumns, tiles = across * to.groups;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, block = lane >> 3;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, block = lane / kAcross;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t g = tile / across;
-        const int64_t c = tile % across * kColumns + (wave * 8 + (lane & 7)) * kVec;
+        const int64_t c = tile % across * kColumns + (wave * kAcross + lane % kAcross) * kVec;
         const int64_t k = g * kMxGroup + block * kMxBlock;
         if (c >= to.rows) continue;
         float v[kMxBlock][kVec];
@@ -136,22 +142,23 @@ __global__ __launch_bounds__(kPackThreads) void pack_turned_kernel(const T* x, i
                 for (int i = 0; i < 8; ++i) w[i] = v[q * 8 + i][j];
                 codes[q] = static_cast<int>(codes_of(w, scale));
             }
-            *reinterpret_cast<Words4*>(to.codes + ((c + j) * to.groups + g) * kMxLine + block * 16) = codes;
-            to.scales[(g * to.rows + c + j) * 8 + block] = static_cast<uint8_t>(scale);
+            *reinterpret_cast<Words4*>(to.codes + (g * to.rows + c + j) * kMxBytes + block * 16) = codes;
+            to.scales[(g * to.rows + c + j) * kMxBlocks + block] = static_cast<uint8_t>(scale);
         }
     }
 }
 
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void unpack_kernel(Mx4 from, T* out, int64_t stride) {
+    constexpr int kLines = kPackThreads / kPackLanes;
     const int64_t lines = from.rows * from.groups;
-    const int lane = threadIdx.x & 31;
-    for (int64_t line = static_cast<int64_t>(blockIdx.x) * (kPackThreads / 32) + (threadIdx.x >> 5); line < lines;
-         line += static_cast<int64_t>(gridDim.x) * (kPackThreads / 32)) {
+    const int lane = threadIdx.x % kPackLanes;
+    for (int64_t line = static_cast<int64_t>(blockIdx.x) * kLines + threadIdx.x / kPackLanes; line < lines;
+         line += static_cast<int64_t>(gridDim.x) * kLines) {
         const int64_t r = line / from.groups, g = line - r * from.groups, c = g * kMxGroup + lane * 8;
         if (c >= from.cols) continue;
-        const uint32_t codes = *reinterpret_cast<const uint32_t*>(from.codes + line * kMxLine + lane * 4);
-        const float by = power_of(from.scales[(g * from.rows + r) * 8 + lane / 4]);
+        const uint32_t codes = *reinterpret_cast<const uint32_t*>(from.codes + (g * from.rows + r) * kMxBytes + lane * 4);
+        const float by = power_of(from.scales[(g * from.rows + r) * kMxBlocks + lane / 4]);
         float v[8];
         const auto two = [&](auto pair, int i) {
             v[i] = pair[0] * by;
@@ -177,22 +184,21 @@ __global__ __launch_bounds__(kPackThreads) void unpack_kernel(Mx4 from, T* out, 
 // ---------------------------------------------------------------------------
 
 // Where a lane's operand comes from: row `row` of a matrix, clamped to its last;
-// half 0 of a wavefront takes the first four blocks of a group, half 1 the others
+// half 0 of a wavefront takes the first two blocks of a group, half 1 the others
 // (a sum's order is free, and both operands agree).
 struct Side {
     const char* codes;
     const uint8_t* scales;
-    int64_t scale_step;
-    __device__ Side(const Mx4& m, int64_t row, int half) {
+    int64_t rows;
+    __device__ Side(const Mx4& m, int64_t row, int half) : rows(m.rows) {
         const int64_t r = row < m.rows ? row : m.rows - 1;
-        codes = m.codes + r * m.groups * kMxLine + half * 64;
-        scales = m.scales + r * 8 + half * 4;
-        scale_step = m.rows * 8;
+        codes = m.codes + r * kMxBytes + half * 32;
+        scales = m.scales + r * kMxBlocks + half * 2;
     }
-    __device__ __forceinline__ void load(int64_t g, Words4 (&c)[4], uint32_t& s) const {
+    __device__ __forceinline__ void load(int64_t g, Words4 (&c)[2], uint32_t& s) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const Words4*>(codes + g * kMxLine + i * 16);
-        s = *reinterpret_cast<const uint32_t*>(scales + g * scale_step);
+        for (int i = 0; i < 2; ++i) c[i] = *reinterpret_cast<const Words4*>(codes + g * rows * kMxBytes + i * 16);
+        s = *reinterpret_cast<const uint16_t*>(scales + g * rows * kMxBlocks);
     }
 };
 
@@ -211,14 +217,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(Mx4 a, Mx4 b, T* ou
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
         for (int64_t g = wave; g < a.groups; g += kFewWaves) {
-            Words4 ca[4], cb[4];
+            Words4 ca[2], cb[2];
             uint32_t xa, xb;
             sb.load(g, cb, xb);
             sa.load(g, ca, xa);
             acc = mma<0>(cb[0], xb, ca[0], xa, acc);
             acc = mma<1>(cb[1], xb, ca[1], xa, acc);
-            acc = mma<2>(cb[2], xb, ca[2], xa, acc);
-            acc = mma<3>(cb[3], xb, ca[3], xa, acc);
         }
         __syncthreads();
 #pragma unroll
@@ -249,6 +253,395 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(Mx4 a, Mx4 b, T* ou
     }
 }
 
+// Larger tiles: the operands in shared memory, two groups of k a step, in two stages
+// that take turns.  First operand: b, whose rows are out's columns, so that a lane
+// holds runs of a row of out.
+constexpr int kMxStages = 2, kMxStep = 2;  // groups of a step
+
+// kR rows of a group in shared memory.  The four 16-byte units of a row are permuted
+// by the row where they come from, so that the eight lanes that read at once meet
+// different banks.
+template <class S, int kR>
+struct MxStage {
+    static constexpr int kLoads = kR * kMxBytes / 16 / S::kThreads;
+    static constexpr int kBytes = kR * (kMxBytes + kMxBlocks);
+    static_assert(kLoads * S::kThreads * 16 == kR * kMxBytes && kR <= S::kThreads && kR % 64 == 0, "whole loads");
+
+    const Mx4& m;
+    const char* codes;      // of the tile's first row
+    const uint8_t* scales;
+    uint32_t rows;          // from there on
+    uint32_t unit;          // where this thread's first unit comes from
+
+    __device__ __forceinline__ explicit MxStage(const Mx4& matrix) : m(matrix) {
+        const uint32_t row = threadIdx.x / 4;
+        unit = row * kMxBytes + ((threadIdx.x ^ row / 4) & 3) * 16;
+    }
+    __device__ __forceinline__ void place(int64_t first) {
+        codes = m.codes + first * kMxBytes;
+        scales = m.scales + first * kMxBlocks;
+        rows = static_cast<uint32_t>(m.rows - first);
+    }
+    // Rows behind the last read as 0: their sums are not used.  So do all where there is
+    // no such group (wanted false), without a read.
+    __device__ __forceinline__ void load(int64_t g, bool wanted, MICRO_SHARED char* to) const {
+        const uint32_t some = wanted ? rows : 0;
+        const __amdgpu_buffer_rsrc_t from =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(codes + g * m.rows * kMxBytes), 0, some * kMxBytes, kRawBuffer);
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to + (i * S::kThreads + wave * 64) * 16, 16,
+                                                     unit + i * S::kThreads * 16, 0, 0, 0);
+        const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t*>(scales + g * m.rows * kMxBlocks), 0, some * kMxBlocks, kRawBuffer);
+        // (a tile of fewer rows than threads: the same ones again)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(words, to + kR * kMxBytes + wave * 64 % kR * 4, 4,
+                                                 threadIdx.x % kR * kMxBlocks, 0, 0, 0);
+    }
+    // Half h of a wavefront takes the blocks 2 h and 2 h + 1 of its rows.
+    static __device__ __forceinline__ Words4 codes_at(MICRO_SHARED char* tile, int row, int kk) {
+        const int half = threadIdx.x >> 5 & 1;
+        return *(MICRO_SHARED Words4*)(tile + row * kMxBytes + ((half * 2 + kk) ^ (row / 4 & 3)) * 16);
+    }
+    static __device__ __forceinline__ uint32_t scales_at(MICRO_SHARED char* tile, int row) {
+        return *(MICRO_SHARED uint16_t*)(tile + kR * kMxBytes + row * kMxBlocks + (threadIdx.x >> 5 & 1) * 2);
+    }
+};
+
+template <class S>
+struct MxTiles {
+    using StageA = MxStage<S, S::kA>;
+    using StageB = MxStage<S, S::kB>;
+    // The tiles of a step's groups.
+    struct Part {
+        MICRO_SHARED char *a, *b;
+    };
+    struct Shared {
+        Part stage[kMxStages][kMxStep];
+    };
+    struct Fragments {
+        Words4 a[S::kTilesA], b[S::kTilesB];
+    };
+    struct Scales {
+        uint32_t a[S::kTilesA], b[S::kTilesB];
+        // Where there is no such group the least scales, 2^-254 together: whatever
+        // codes they meet add less than half of binary32's least number.
+        __device__ __forceinline__ void keep(bool there) {
+            const uint32_t mask = there ? 0xffffffffu : 0;
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i) a[i] &= mask;
+#pragma unroll
+            for (int j = 0; j < S::kTilesB; ++j) b[j] &= mask;
+        }
+    };
+    static constexpr int kReads = S::kTilesA + S::kTilesB, kProducts = S::kTilesA * S::kTilesB;
+    static constexpr int kLoads = kMxStep * (StageA::kLoads + StageB::kLoads + 2);
+
+    StageA sa;
+    StageB sb;
+    int64_t step, end;  // groups
+    int row_a, row_b;   // the lane's first rows in the tiles
+
+    __device__ __forceinline__ MxTiles(const Mx4& a, const Mx4& b) : sa(a), sb(b) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        row_a = wave / S::kWavesB * (S::kTilesA * 32) + (lane & 31);
+        row_b = wave % S::kWavesB * (S::kTilesB * 32) + (lane & 31);
+    }
+
+    __device__ __forceinline__ void load(int64_t g, const Part (&to)[kMxStep]) const {
+#pragma unroll
+        for (int i = 0; i < kMxStep; ++i) {
+            sa.load(g + i, g + i < end, to[i].a);
+            sb.load(g + i, g + i < end, to[i].b);
+        }
+    }
+    // Until all but the last kPending of each wavefront's loads and stores are done (they
+    // end in their order), where `more`, or else all; until what it has read from shared
+    // memory is in registers; and until the others are here too.
+    template <int kPending>
+    static __device__ __forceinline__ void meet(bool more) {
+        static_assert(kPending < 64, "the counter's bits");
+        if (more)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPending) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    static __device__ __forceinline__ void meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+    __device__ __forceinline__ void read(const Part& p, int kk, Fragments& f) const {
+#pragma unroll
+        for (int j = 0; j < S::kTilesB; ++j) f.b[j] = StageB::codes_at(p.b, row_b + j * 32, kk);
+#pragma unroll
+        for (int i = 0; i < S::kTilesA; ++i) f.a[i] = StageA::codes_at(p.a, row_a + i * 32, kk);
+    }
+    __device__ __forceinline__ void read(const Part& p, Scales& s) const {
+#pragma unroll
+        for (int j = 0; j < S::kTilesB; ++j) s.b[j] = StageB::scales_at(p.b, row_b + j * 32);
+#pragma unroll
+        for (int i = 0; i < S::kTilesA; ++i) s.a[i] = StageA::scales_at(p.a, row_a + i * 32);
+    }
+    template <int kk>
+    static __device__ __forceinline__ void multiply(const Fragments& f, const Scales& s, Acc (&acc)[S::kTilesA][S::kTilesB]) {
+#pragma unroll
+        for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+            for (int j = 0; j < S::kTilesB; ++j) acc[i][j] = mma<kk>(f.a[i], s.a[i], f.b[j], s.b[j], acc[i][j]);
+    }
+
+    // The tile at (a, b), groups [first, until), of which the first step begins to
+    // load.  All stages are free.
+    __device__ __forceinline__ void start(int64_t a, int64_t b, int64_t first, int64_t until, const Shared& at) {
+        step = first;
+        end = until;
+        sa.place(a);
+        sb.place(b);
+        load(step, at.stage[0]);
+    }
+
+    // acc += the sum.  Fragments are read while the matrix cores work on the ones
+    // before.  stored: kStores stores at least lie behind start(); they need not be
+    // done before the loads that follow them are waited for.
+    template <int kStores>
+    __device__ __forceinline__ void run(Acc (&acc)[S::kTilesA][S::kTilesB], const Shared& at, bool stored) {
+        Fragments even, odd;
+        Scales first, second;
+        // All of a step but its last quarter.
+        const auto work = [&](const Part (&p)[kMxStep]) {
+            read(p[0], 1, odd);
+            multiply<0>(even, first, acc);
+            interleave<kProducts, kReads, 0>();
+            read(p[1], second);
+            read(p[1], 0, even);
+            multiply<1>(odd, first, acc);
+            interleave<kProducts, 2 * kReads, 0>();
+            second.keep(step + 1 < end);
+            read(p[1], 1, odd);
+            multiply<0>(even, second, acc);
+            interleave<kProducts, kReads, 0>();
+        };
+        // A step's last fragments are in registers before the barrier, so behind it
+        // the loads of the step after next may overwrite its stage, and the next
+        // step's first fragments are read, both under the step's last products.
+        const auto turn = [&](const Part (&p)[kMxStep], const Part (&next)[kMxStep]) {
+            meet();
+            __builtin_amdgcn_sched_barrier(0);
+            load(step + 2 * kMxStep, p);
+            read(next[0], first);
+            read(next[0], 0, even);
+            multiply<1>(odd, second, acc);
+            interleave<kProducts, 2 * kReads, kLoads>();
+            step += kMxStep;
+        };
+        meet<kStores>(stored);
+        load(step + kMxStep, at.stage[1]);
+        read(at.stage[0][0], first);
+        read(at.stage[0][0], 0, even);
+        __builtin_amdgcn_sched_barrier(0);
+        int64_t left = (end - step + 1) / kMxStep;
+        for (; left > 2; left -= 2) {
+            work(at.stage[0]);
+            turn(at.stage[0], at.stage[1]);
+            work(at.stage[1]);
+            turn(at.stage[1], at.stage[0]);
+        }
+        work(at.stage[0]);
+        if (left == 2) {
+            meet();
+            read(at.stage[1][0], first);
+            read(at.stage[1][0], 0, even);
+            multiply<1>(odd, second, acc);
+            step += kMxStep;
+            work(at.stage[1]);
+        }
+        multiply<1>(odd, second, acc);
+        meet();  // the stages are free
+    }
+};
+
+// One 16-byte chunk of a row of out, its values in [j, columns).
+template <class T>
+__device__ __forceinline__ void store_chunk(T* row, int64_t j, int64_t columns, Chunk x) {
+    constexpr int kVec = 16 / sizeof(T);
+    const Pack<T, kVec> v = __builtin_bit_cast(Pack<T, kVec>, x);
+    if (j + kVec <= columns) {
+        *reinterpret_cast<Pack<T, kVec>*>(row + j) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (j + i < columns) row[j + i] = v.v[i];
+    }
+}
+
+struct MxOut {
+    void* at;
+    int64_t stride, rows, columns;
+    bool accumulate;
+    float* parts;
+    int64_t most_splits;
+};
+
+// The 16-byte stores of a wavefront's whole tile, its least (binary32 and sums added
+// to out take more).
+template <class S>
+constexpr int kLeastStores = S::kTilesB * S::kTilesA / 2 * 4;
+
+// A finished tile's columns of matrix tiles from the j0-th on into out.
+template <class S, class T, int kColumns>
+__device__ __forceinline__ void finish_tile(const MxOut& out, MICRO_SHARED char* area, const Place<S>& place, int64_t ta,
+                                            int64_t tb, int j0, Acc (&acc)[S::kTilesA][kColumns]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < kColumns; ++j) {
+        const int64_t row0 = tb * S::kB + place.wave_b + (j0 + j) * 32 + (lane >> 3);
+        if (sizeof(T) == 4 || out.accumulate) {
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i) {
+                Chunk in[4], to[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const Vec4<float> x = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    in[q] = __builtin_bit_cast(Chunk, x);
+                }
+                exchange(area, in, to);
+                const int64_t column = ta * S::kA + place.wave_a + i * 32 + (lane & 7) * 4;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t r = row0 + 8 * k;
+                    if (r >= out.rows || column >= out.columns) continue;
+                    T* row = static_cast<T*>(out.at) + r * out.stride;
+                    const Vec4<float> v = __builtin_bit_cast(Vec4<float>, to[k]);
+                    if (column + 4 <= out.columns) {
+                        float x[4] = {v[0], v[1], v[2], v[3]};
+                        if (out.accumulate) {
+                            float old[4];
+                            load_floats(row + column, old);
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) x[m] += old[m];
+                        }
+                        store_floats(row + column, x);
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < 4; ++m)
+                            if (column + m < out.columns)
+                                row[column + m] =
+                                    rounded<T>(out.accumulate ? v[m] + static_cast<float>(row[column + m]) : v[m]);
+                    }
+                }
+            }
+        } else if constexpr (sizeof(T) == 2) {
+            constexpr int kRun = 2;  // matrix tiles whose 16-bit values fill 128 bytes of a row
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; i += kRun) {
+                Chunk in[4], to[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (i + m / 2 >= S::kTilesA) {
+                        in[m] = Chunk{0, 0, 0, 0};
+                        continue;
+                    }
+                    Vec4<T> lo, hi;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        lo[r] = rounded<T>(acc[i + m / 2][j][m % 2 * 8 + r]);
+                        hi[r] = rounded<T>(acc[i + m / 2][j][m % 2 * 8 + 4 + r]);
+                    }
+                    swap_halves(lo, hi);
+                    in[m] = __builtin_bit_cast(Chunk, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+                exchange(area, in, to);
+                const int64_t column = ta * S::kA + place.wave_a + i * 32 + (lane & 7) * 8;
+                const bool in_tile = (lane & 7) * 8 < (S::kTilesA - i) * 32;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int64_t r = row0 + 8 * k;
+                    if (r < out.rows && column < out.columns && in_tile)
+                        store_chunk(static_cast<T*>(out.at) + r * out.stride, column, out.columns, to[k]);
+                }
+            }
+        }
+    }
+}
+
+// Workgroups of a compute unit: what its shared memory holds.
+template <class S>
+constexpr int kMxPerUnit = 160 * 1024 / (kMxStages * kMxStep * (S::kA + S::kB) * (kMxBytes + kMxBlocks));
+
+template <class S, class T>
+__global__ __launch_bounds__(S::kThreads) void product_kernel(Mx4 a, Mx4 b, MxOut out) {
+    using Tiles = MxTiles<S>;
+    // (each stage a variable of its own: that is how the compiler knows that reads of
+    // one need not wait for the loads into another)
+#define MICRO_MX_PART(name)                                                         \
+    __shared__ __attribute__((aligned(1024))) char name##_a[Tiles::StageA::kBytes]; \
+    __shared__ __attribute__((aligned(1024))) char name##_b[Tiles::StageB::kBytes]; \
+    const typename Tiles::Part name{(MICRO_SHARED char*)name##_a, (MICRO_SHARED char*)name##_b}
+    MICRO_MX_PART(part0);
+    MICRO_MX_PART(part1);
+    MICRO_MX_PART(part2);
+    MICRO_MX_PART(part3);
+    const typename Tiles::Shared at{{{part0, part1}, {part2, part3}}};
+    TileOrder order((a.rows + S::kA - 1) / S::kA, (b.rows + S::kB - 1) / S::kB, out.most_splits);
+    Tiles product(a, b);
+    const Place<S> place;
+    // the exchange of finished tiles, in the stage that start() leaves
+    constexpr int kHalf = S::kThreads / 128;
+    static_assert(kHalf * kExchange <= Tiles::StageA::kBytes && kHalf * kExchange <= Tiles::StageB::kBytes, "the exchange fits");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    MICRO_SHARED char* const area = (wave < kHalf ? part2.a : part2.b) + wave % kHalf * kExchange;
+    const auto start = [&](const Tile& t) {
+        const int64_t steps = (a.groups + kMxStep - 1) / kMxStep, parts = t.part < 0 ? 1 : order.splits;
+        const int64_t part = t.part < 0 ? 0 : t.part, until = steps * (part + 1) / parts * kMxStep;
+        product.start(t.a * S::kA, t.b * S::kB, steps * part / parts * kMxStep, until < a.groups ? until : a.groups, at);
+    };
+    Tile tile, after;
+    bool more = order.next(&tile), full = false;
+    if (more) start(tile);
+    for (; more; tile = after) {
+        Acc acc[S::kTilesA][S::kTilesB];
+        clear<S>(acc);
+        product.template run<kLeastStores<S>>(acc, at, full);
+        more = order.next(&after);
+        if (more) start(after);
+        if (tile.part >= 0) {
+#pragma unroll
+            for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+                for (int j = 0; j < S::kTilesB; ++j) store_part<S>(tile_at<S>(out.parts, tile.index), i, j, acc[i][j]);
+            full = false;
+        } else {
+            finish_tile<S, T, S::kTilesB>(out, area, place, tile.a, tile.b, 0, acc);
+            full = (tile.a + 1) * S::kA <= out.columns && (tile.b + 1) * S::kB <= out.rows;
+        }
+    }
+}
+
+// Adds the parts of tiles whose sums were cut, in their order, a workgroup a column
+// of matrix tiles of one wavefront.
+template <class S, class T>
+__global__ __launch_bounds__(64) void join_kernel(int64_t tiles_a, int64_t tiles_b, MxOut out, int64_t grid) {
+    __shared__ __attribute__((aligned(1024))) char shared[kExchange];
+    const TileOrder order(tiles_a, tiles_b, out.most_splits, grid);
+    constexpr int kWaves = S::kThreads / 64;
+    const int64_t t = blockIdx.x / (kWaves * S::kTilesB);
+    if (t >= order.tail) return;
+    const int of = blockIdx.x % (kWaves * S::kTilesB) / S::kTilesB, j = blockIdx.x % S::kTilesB;
+    int64_t ta, tb;
+    order.place(order.full + t, &ta, &tb);
+    const Place<S> place(of);
+    if (tb * S::kB + place.wave_b + j * 32 >= out.rows) return;
+    Acc acc[S::kTilesA][1];
+#pragma unroll
+    for (int i = 0; i < S::kTilesA; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][0][r] = 0.0f;
+    for (int64_t s = 0; s < order.splits; ++s)
+#pragma unroll
+        for (int i = 0; i < S::kTilesA; ++i)
+            add_part<S>(tile_at<S>(out.parts, s * order.tail + t, of * 64 + threadIdx.x), i, j, acc[i][0]);
+    finish_tile<S, T, 1>(out, (MICRO_SHARED char*)shared, place, ta, tb, j, acc);
+}
+
 constexpr int64_t kMostGroups = int64_t(1) << 20;
 dim3 grid_of(int64_t n) { return dim3(static_cast<uint32_t>(std::min(n, kMostGroups))); }
 
@@ -262,8 +655,8 @@ hipError_t pack(const Rows& x, const Mx4& packed, const Mx4& turned, hipStream_t
                                         kPackThreads, stream, at, x.stride, packed))
             return e;
     if (!turned.codes) return hipSuccess;
-    constexpr int kColumns = 8 * (16 / sizeof(T)) * kPackThreads / 64;
-    return launch(pack_turned_kernel<T>, grid_of((turned.rows + kColumns - 1) / kColumns * turned.groups), kPackThreads,
+    return launch(pack_turned_kernel<T>,
+                  grid_of((turned.rows + Turn<T>::kColumns - 1) / Turn<T>::kColumns * turned.groups), kPackThreads,
                   stream, at, x.stride, turned);
 }
 
@@ -281,7 +674,7 @@ hipError_t launch_mx4_pack(const Rows& x, int64_t rows, int64_t cols, const Mx4&
 
 hipError_t launch_mx4_unpack(const Mx4& from, const Rows& out, hipStream_t stream) {
     if (from.rows == 0 || from.cols == 0) return hipSuccess;
-    const dim3 grid = grid_of((from.rows * from.groups + kPackThreads / 32 - 1) / (kPackThreads / 32));
+    const dim3 grid = grid_of((from.rows * from.groups + kPackThreads / kPackLanes - 1) / (kPackThreads / kPackLanes));
     switch (out.type) {
         case MICRO_TYPE_F32:
             return launch(unpack_kernel<float>, grid, kPackThreads, stream, from, static_cast<float*>(out.at), out.stride);
@@ -294,11 +687,52 @@ hipError_t launch_mx4_unpack(const Mx4& from, const Rows& out, hipStream_t strea
 
 namespace {
 
+constexpr int64_t kPartGroups = 32;
+
+// The product in tiles of shape S by a grid that fills the card.
+template <class S, class T>
+hipError_t tiles(const Mx4Product& c, hipStream_t stream) {
+    const int64_t ta = (c.b.rows + S::kA - 1) / S::kA, tb = (c.a.rows + S::kB - 1) / S::kB;
+    const int64_t grid = c.compute_units / TileOrder::kDies * TileOrder::kDies * kMxPerUnit<S>;
+    static_assert(S::kA * S::kB * kMxPerUnit<S> <= kMxParts, "the parts of a grid fit");
+    MxOut out{c.out.at, c.out.stride, c.a.rows, c.b.rows, c.accumulate, c.parts, 1};
+    // The tiles behind the last full round are cut along the sum where they are a quarter
+    // of the grid at most and a part keeps kPartGroups: writing and adding the parts costs
+    // more than it saves else (1024 x 1024 x 16384 in 23.6 us for 41.5, but 1024 x 4096 x
+    // 8192 in 34.2 for 26.7).
+    const int64_t tail = ta * tb % grid;
+    if (tail > 0 && tail * 4 <= grid) out.most_splits = std::min(grid / tail, std::max<int64_t>(c.a.groups / kPartGroups, 1));
+    if (const hipError_t e = launch(product_kernel<S, T>, dim3(static_cast<uint32_t>(grid)), S::kThreads, stream, c.b, c.a, out))
+        return e;
+    if (out.most_splits <= 1) return hipSuccess;
+    return launch(join_kernel<S, T>, dim3(static_cast<uint32_t>(tail * (S::kThreads / 64) * S::kTilesB)), 64, stream, ta, tb,
+                  out, grid);
+}
+
+// How long `tiles` tiles take: rounds of a full grid, and the less that the last one
+// takes when it is not full, in microseconds for each step of long sums (16384 x 4096 x
+// 16384: 8 rounds of middle tiles in 571 us, 4 of wide ones in 452; one round that is
+// not full 0.6 to 0.7 and 1.2).
+double rounds(int64_t tiles, int64_t grid, double full, double rest) {
+    return tiles / grid * full + (tiles % grid ? rest : 0.0);
+}
+
+// Tiles of 32 x 32 that are better off one a workgroup, whose wavefronts share the sum,
+// while they and their groups are few: 256 x 1024 x 2048 takes 4.7 us for 9.5 in middle
+// tiles, 256 x 4096 x 2048 9.3 for 9.7, 512 x 4096 x 2048 14.9 for 10.2; with short sums
+// 512 x 4096 x 256 6.0 for 6.5, 1024 x 4096 x 256 9.0 for 7.3.
+constexpr int64_t kFewTiles = 4096, kFewGroups = 32768;
+
 template <class T>
 hipError_t product(const Mx4Product& c, hipStream_t stream) {
-    const int64_t tiles = (c.a.rows + kTile - 1) / kTile * ((c.b.rows + kTile - 1) / kTile);
-    return launch(few_kernel<T>, grid_of(tiles), 64 * kFewWaves, stream, c.a, c.b, static_cast<T*>(c.out.at), c.out.stride,
-                  c.accumulate);
+    const int64_t few = (c.a.rows + kTile - 1) / kTile * ((c.b.rows + kTile - 1) / kTile);
+    if ((few <= kFewTiles && few * c.a.groups <= kFewGroups) || c.a.groups == 0)
+        return launch(few_kernel<T>, grid_of(few), 64 * kFewWaves, stream, c.a, c.b, static_cast<T*>(c.out.at), c.out.stride,
+                      c.accumulate);
+    const auto count = [&](int64_t a, int64_t b) { return (c.b.rows + a - 1) / a * ((c.a.rows + b - 1) / b); };
+    const double middle = rounds(count(Middle::kA, Middle::kB), c.compute_units * kMxPerUnit<Middle>, 1.1, 0.7);
+    const double wide = rounds(count(Wide::kA, Wide::kB), c.compute_units * kMxPerUnit<Wide>, 1.77, 1.25);
+    return wide < middle ? tiles<Wide, T>(c, stream) : tiles<Middle, T>(c, stream);
 }
 
 }  // namespace

@@ -9,16 +9,15 @@ import ctypes
 from . import _lib
 from .language import _Enqueued, _value_types
 
-GROUP = 256  # values of a line of codes; a row is whole lines
+GROUP, BLOCKS = 128, 4  # values and blocks of a group; a row is whole groups
 
 
 class PackedMatrix:
     """A rows x cols matrix in blocks of 32 values along its rows.
 
-    codes: uint8, (rows, groups * 128), two values a byte; scales: uint8, (groups,
-    rows, 8), the exponents of 2 plus 127; groups = cols / 256, rounded up.  Values
-    behind cols are 0.  Both are contiguous and may be saved and loaded as they
-    are."""
+    codes: uint8, (groups, rows, 64), two values a byte; scales: uint8, (groups, rows,
+    4), the exponents of 2 plus 127; groups = cols / 128, rounded up.  Values behind
+    cols are 0.  Both are contiguous and may be saved and loaded as they are."""
 
     __slots__ = ("codes", "scales", "rows", "cols", "_c")
 
@@ -28,7 +27,8 @@ class PackedMatrix:
         if self.rows < 0 or self.cols < 0:
             raise ValueError("a side is negative")
         groups = -(-self.cols // GROUP)
-        for t, name, shape in ((codes, "codes", (self.rows, groups * GROUP // 2)), (scales, "scales", (groups, self.rows, 8))):
+        for t, name, shape in ((codes, "codes", (groups, self.rows, GROUP // 2)),
+                               (scales, "scales", (groups, self.rows, BLOCKS))):
             if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous():
                 raise TypeError(f"{name} must be a contiguous uint8 tensor")
             if tuple(t.shape) != shape:
@@ -100,8 +100,8 @@ class Microscaled(_Enqueued):
     def _new(self, rows, cols, foreign):
         groups = -(-cols // GROUP)
         u8 = self._torch.uint8
-        return PackedMatrix(self._empty((rows, groups * GROUP // 2), u8, foreign), self._empty((groups, rows, 8), u8, foreign),
-                            rows, cols)
+        return PackedMatrix(self._empty((groups, rows, GROUP // 2), u8, foreign),
+                            self._empty((groups, rows, BLOCKS), u8, foreign), rows, cols)
 
     def _kept(self, *what):
         for m in what:

@@ -9,12 +9,12 @@ EPS = 2.0 ** -24
 
 def quantise(x):
     """(codes 0 to 15 of every value, scale bytes of every block) of x's rows, both
-    over whole groups of 256 columns."""
+    over whole groups of 128 columns."""
     rows, cols = x.shape
-    groups = -(-cols // 256)
-    v = torch.zeros(rows, groups * 256, dtype=torch.float64)
+    groups = -(-cols // 128)
+    v = torch.zeros(rows, groups * 128, dtype=torch.float64)
     v[:, :cols] = x.double()
-    v = v.view(rows, groups * 8, 32)
+    v = v.view(rows, groups * 4, 32)
     top = v.abs().amax(2)
     bad = ~v.isfinite().all(2)
     exponent = torch.frexp(torch.where(bad | (top == 0), torch.ones_like(top), top)).exponent.double() - 3  # floor(log2) - 2
@@ -33,8 +33,9 @@ def quantise(x):
 def layout(code, scale):
     """The bytes of PackedMatrix.codes and .scales."""
     rows = code.shape[0]
-    c = code.view(rows, -1, 2)
-    return (c[..., 0] | c[..., 1] << 4).to(torch.uint8), scale.view(rows, -1, 8).transpose(0, 1).to(torch.uint8).contiguous()
+    c = code.view(rows, -1, 64, 2).transpose(0, 1)
+    return ((c[..., 0] | c[..., 1] << 4).to(torch.uint8).contiguous(),
+            scale.view(rows, -1, 4).transpose(0, 1).to(torch.uint8).contiguous())
 
 
 def values(code, scale, cols):

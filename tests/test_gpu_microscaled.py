@@ -143,20 +143,62 @@ def test_product(dtype, m, n, k):
     assert bool((whole[:, :5] == 3).all()) and bool((whole[:, 5 + n:] == 3).all())
 
 
-@pytest.mark.parametrize("m,n", [(3, 40), (100, 300), (300, 300)])
+# (rows, columns, length): middle tiles in one round and in several, wide ones in one and
+# in two, each with an odd number of groups, edges on both sides and a tail cut along the sum
+LARGE_PRODUCTS = [(2000, 2300, 130), (1500, 3001, 300), (2000, 9000, 40), (2050, 9000, 257), (500, 1000, 9000),
+                  (130, 5000, 8200), (250, 65500, 300), (256, 65536, 512), (500, 50000, 130), (4100, 4096, 640),
+                  (256, 65600, 8300)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", LARGE_PRODUCTS)
+def test_large_product(dtype, m, n, k):
+    gen = torch.Generator(device=DEV).manual_seed(m + n + k)
+    draw_on = lambda rows: torch.randn(rows, k, generator=gen, device=DEV) * torch.exp2(  # noqa: E731
+        torch.randint(-3, 3, (rows, 1), generator=gen, device=DEV).float())
+    mx = micro.Microscaled()
+    qa, qb = mx.pack(draw_on(m)), mx.pack(draw_on(n))
+    got = mx.product(qa, qb, dtype=dtype)
+    rows = torch.unique(torch.cat([torch.arange(0, m, max(1, m // 60)), torch.tensor([0, m // 2, m - 1])])).to(DEV)
+    va, vb = mx.unpack(qa).double()[rows], mx.unpack(qb).double()
+    want, bound = ref.product(va, vb, dtype)
+    assert float(((got[rows].double() - want).abs() / bound).max()) <= 1.0
+    assert torch.equal(got, mx.product(qa, qb, dtype=dtype))
+    # the other way around, every row against what was checked above
+    assert float(((mx.product(qb, qa, dtype=dtype)[:, rows].t().double() - want).abs() / bound).max()) <= 1.0
+    # into strided rows, added to what is there
+    whole = torch.full((m, n + 9), 3.0, dtype=dtype, device=DEV)
+    old = torch.randn(rows.numel(), n, generator=gen, device=DEV).to(dtype)
+    whole[rows, 5:5 + n] = old
+    out = whole[:, 5:5 + n]
+    mx.product(qa, qb, out=out, accumulate=True)
+    want, bound = ref.product(va, vb, dtype, old)
+    assert float(((out[rows].double() - want).abs() / bound).max()) <= 1.0
+    assert bool((whole[:, :5] == 3).all()) and bool((whole[:, 5 + n:] == 3).all())
+    # rows that were not looked at are what the sum of one more row would be
+    plain = mx.product(qa, qb, dtype=dtype)
+    rest = torch.ones(m, dtype=torch.bool, device=DEV)
+    rest[rows] = False
+    want = plain[rest].double() + 3.0
+    # one sum in binary32 and its rounding against two roundings to the type
+    slack = (2 * ref.U[dtype] + 4 * ref.EPS) * (plain[rest].double().abs() + 3.0) * (1 + ref.U[dtype])
+    assert bool(((out[rest].double() - want).abs() <= slack).all())
+
+
+@pytest.mark.parametrize("m,n", [(3, 40), (100, 300), (2100, 2300), (250, 65540)])
 def test_product_of_blocks_that_are_not_numbers(m, n):
     """A NaN block reaches its own row's and column's sums, whatever it meets."""
-    a, b = draw(m, 300, torch.float32, 1), draw(n, 300, torch.float32, 2)
+    a, b = torch.ones(m, 300), torch.ones(n, 300)
     a[1, 100], b[5, 299] = float("nan"), float("inf")
     b[:, 96:128] = 0.0
     mx = micro.Microscaled()
-    got = mx.product(mx.pack(a.to(DEV)), mx.pack(b.to(DEV))).cpu()
-    nan = torch.zeros(m, n, dtype=torch.bool)
+    got = mx.product(mx.pack(a.to(DEV)), mx.pack(b.to(DEV)))
+    nan = torch.zeros(m, n, dtype=torch.bool, device=DEV)
     nan[1], nan[:, 5] = True, True
     assert torch.equal(got.isnan(), nan)
 
 
-@pytest.mark.parametrize("m,n", [(2, 40), (60, 70), (300, 300)])
+@pytest.mark.parametrize("m,n", [(2, 40), (60, 70), (2100, 2300), (250, 65540)])
 def test_product_at_the_ends_of_the_range(m, n):
     """Blocks of the largest and the smallest scales: sums past binary32 are
     infinite, products below its least are lost, and nothing else is."""
@@ -179,7 +221,7 @@ def test_empty_sides():
     some = mx.pack(torch.ones(7, 40, device=DEV))
     assert mx.product(none, some).shape == (0, 7) and mx.product(some, none).shape == (7, 0)
     flat = mx.pack(torch.empty(7, 0, device=DEV))
-    assert flat.codes.shape == (7, 0) and torch.equal(mx.product(flat, flat), torch.zeros(7, 7, device=DEV))
+    assert flat.codes.shape == (0, 7, 64) and torch.equal(mx.product(flat, flat), torch.zeros(7, 7, device=DEV))
     assert torch.equal(mx.product(flat, flat, out=torch.ones(7, 7, device=DEV), accumulate=True), torch.ones(7, 7, device=DEV))
     assert mx.unpack(flat).shape == (7, 0)
     assert mx.pack(torch.empty(7, 0, device=DEV), transposed=True).shape == (0, 7)
@@ -187,18 +229,18 @@ def test_empty_sides():
 
 def test_offsets_past_32_bits():
     mx = micro.Microscaled()
-    # 9 GB of codes: rows 512 bytes apart, 2^24 of them
+    # 9 GB of codes
     rows, cols = 2 ** 24, 1024
-    codes = torch.zeros(rows, 512, dtype=torch.uint8, device=DEV)
-    scales = torch.full((4, rows, 8), 127, dtype=torch.uint8, device=DEV)
-    codes[-1, -1] = 0x20  # 1 in the last value
-    scales[3, -1, 7] = 130
+    codes = torch.zeros(8, rows, 64, dtype=torch.uint8, device=DEV)
+    scales = torch.full((8, rows, 4), 127, dtype=torch.uint8, device=DEV)
+    codes[-1, -1, -1] = 0x20  # 1 in the last value
+    scales[-1, -1, -1] = 130
     big = micro.PackedMatrix(codes, scales, rows, cols)
     one = torch.zeros(1, cols, device=DEV)
     one[0, -1] = 3.0
     got = mx.linear(one, big, dtype=torch.float32)
     assert float(got[0, -1]) == 24.0 and float(got.abs().sum()) == 24.0
-    last = mx.unpack(micro.PackedMatrix(codes[-5:], scales[:, -5:].contiguous(), 5, cols))
+    last = mx.unpack(micro.PackedMatrix(codes[:, -5:].contiguous(), scales[:, -5:].contiguous(), 5, cols))
     assert float(last[-1, -1]) == 8.0 and float(last.sum()) == 8.0
     del codes, scales, big, got
     # an output of 2.4e9 values
@@ -286,7 +328,7 @@ def test_refusals():
                         (lambda: mx.product(q, q, accumulate=True), ValueError),
                         (lambda: mx.linear(x[:, :32], q), ValueError),
                         (lambda: mx.unpack(q, out=out), ValueError),
-                        (lambda: mx.product(q, q, out=q.codes.view(torch.float32)[:8, :8]), (micro.MicroError, ValueError)),
+                        (lambda: mx.product(q, q, out=q.codes.view(torch.float32).view(8, 16)[:, :8]), (micro.MicroError, ValueError)),
                         (lambda: mx.pack(torch.nn.Parameter(x)), RuntimeError),
                         (lambda: mx.linear(x, q, out=torch.nn.Parameter(out)), RuntimeError)]:
         with pytest.raises(error):

@@ -30,7 +30,7 @@ def test_structures_match_the_header(tmp_path):
             assert int(got[f"{st.__name__}.{f}"]) == getattr(st, f).offset
 
 
-@pytest.mark.parametrize("rows,cols,want", [(0, 0, (0, 0)), (1, 1, (128, 8)), (3, 256, (384, 24)), (3, 257, (768, 48)),
+@pytest.mark.parametrize("rows,cols,want", [(0, 0, (0, 0)), (1, 1, (64, 4)), (3, 128, (192, 12)), (3, 129, (384, 24)),
                                             (2 ** 24, 2 ** 24, (2 ** 47, 2 ** 43)), (5, 0, (0, 0))])
 def test_bytes(rows, cols, want):
     assert _lib.micro_mx4_bytes(rows, cols) == want
@@ -75,7 +75,7 @@ def matrix(codes=1 << 20, scales=1 << 24, rows=10, cols=40):
     ((1 << 30) + 2, 0, 40, 10, 40, matrix(), None, EINVAL), (1 << 30, 0, 40, 10, 40, matrix(rows=11), None, EINVAL),
     (1 << 30, 0, 40, 10, 40, None, matrix(), EINVAL), (1 << 30, 0, 40, 10, 40, matrix(codes=0), None, EINVAL),
     (1 << 30, 0, 40, 10, 40, matrix(codes=(1 << 20) + 8), None, EINVAL),
-    (1 << 30, 0, 40, 10, 40, matrix(scales=(1 << 24) + 4), None, EINVAL),
+    (1 << 30, 0, 40, 10, 40, matrix(scales=(1 << 24) + 2), None, EINVAL),
     (1 << 20, 0, 40, 10, 40, matrix(), None, EINVAL), (1 << 30, 0, 40, 10, 40, matrix(scales=1 << 20), None, EINVAL),
     (1 << 30, 0, 40, 10, 40, matrix(), matrix(rows=40, cols=10), EINVAL), (1 << 30, 0, 40, -1, 40, matrix(), None, EINVAL),
     (1 << 30, 0, (1 << 32) + 1, 10, 40, matrix(), None, EINVAL), (1 << 30, 0, 40, 2 ** 24 + 1, 40, matrix(), None, ERANGE)])
@@ -103,10 +103,10 @@ def test_products_that_are_refused(handle):
 
 def test_packed_matrices_of_other_shapes_and_types_are_refused():
     u8 = torch.uint8
-    m = PackedMatrix(torch.zeros(3, 256, dtype=u8), torch.zeros(2, 3, 8, dtype=u8), 3, 300)
+    m = PackedMatrix(torch.zeros(3, 3, 64, dtype=u8), torch.zeros(3, 3, 4, dtype=u8), 3, 300)
     assert m.shape == (3, 300) and m.device.type == "cpu"
-    for codes, scales, error in ((torch.zeros(3, 128, dtype=u8), m.scales, ValueError), (m.codes, torch.zeros(3, 2, 8, dtype=u8), ValueError),
-                                 (m.codes.char(), m.scales, TypeError), (torch.zeros(256, 3, dtype=u8).t(), m.scales, TypeError),
+    for codes, scales, error in ((torch.zeros(3, 192, dtype=u8), m.scales, ValueError), (m.codes, torch.zeros(2, 3, 4, dtype=u8), ValueError),
+                                 (m.codes.char(), m.scales, TypeError), (torch.zeros(3, 64, 3, dtype=u8).transpose(1, 2), m.scales, TypeError),
                                  (m.codes, None, TypeError)):
         with pytest.raises(error):
             PackedMatrix(codes, scales, 3, 300)
