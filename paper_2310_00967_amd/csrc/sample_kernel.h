@@ -26,6 +26,7 @@ struct SampleCall {
     micro_sampling sampling;
     TokenIds ids;      // out
     float* logprobs;   // out, may be null
+    int compute_units;
 };
 
 hipError_t launch_sample(const SampleCall& call, hipStream_t stream);

@@ -7,9 +7,17 @@
 // Weights are computed in binary64 and rounded to whole multiples of 2^-f; their
 // sums are of 64-bit integers and exact, so the token does not depend on how a row
 // is divided, and a border between two tokens lies where binary64 sums have it
-// to 2^-f.  The two cuts along the order are found without sorting, by histograms
-// over the logits' bits: each level spreads the interval that holds the cut over
-// kBins bins of counts (top_k) or weights (top_p).
+// to 2^-f.
+//
+// A workgroup takes a row and reads it again for each step (from the second time on out
+// of the caches).  A small top_k needs two readings: the k-th largest of the threads'
+// maxima is a lower bound of the k-th logit, and the few logits above it are sorted in
+// shared memory, where all else follows.  Else the weights are added into bins that
+// divide the range of logits that weigh anything, which finds the bin where top_p cuts;
+// its few logits are sorted; a third reading adds what is kept by the wavefronts' runs of
+// indices; and the run that holds the token is walked.  A cut that these lists do not
+// hold (thousands of equal logits) and a large top_k are found by histograms over the
+// logits' bits.
 #include "sample_kernel.h"
 
 #include "launch.h"
@@ -18,31 +26,18 @@
 namespace micro {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kBinBits = 11, kBins = 1 << kBinBits;
-constexpr int kExpSteps = 64;  // of the table of 2^(j / 64)
+constexpr int kBins = 4096, kKeyBits = 12;  // 2^kKeyBits of them for a level over keys
+constexpr int kBatches = 4096;              // of a row, at most
+constexpr int kExpSteps = 64;               // of the table of 2^(j / 64)
+constexpr float kLowest = -3.40282346638528859812e+38f;
 
-// Bits of a logit in its order: larger logits have larger keys, equal ones (-0
-// and 0) the same; 0 where it has no part (-inf, NaN).
-template <class T>
-__device__ __forceinline__ uint32_t key_of(T x) {
-    if constexpr (sizeof(T) == 4) {
-        const uint32_t u = __float_as_uint(x + 0.0f);
-        return x > -__builtin_inff() ? u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u) : 0u;
-    } else {
-        const uint16_t u = __builtin_bit_cast(uint16_t, x);
-        const uint32_t v = u == 0x8000u ? 0u : u;
-        return static_cast<float>(x) > -__builtin_inff() ? v ^ ((v >> 15) ? 0xffffu : 0x8000u) : 0u;
-    }
+// Bits of a logit in its order: larger logits have larger keys, -0 and 0 the same.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
-template <class T>
 __device__ __forceinline__ float logit_of(uint32_t key) {
-    if constexpr (sizeof(T) == 4) {
-        return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
-    } else {
-        const uint16_t u = static_cast<uint16_t>(key ^ ((key >> 15) ? 0x8000u : 0xffffu));
-        return static_cast<float>(__builtin_bit_cast(T, u));
-    }
+    return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
 }
 
 // floor(f * x) and ceil(f * x) of a binary64 f in [0, 1], exactly.
@@ -69,175 +64,286 @@ __device__ __forceinline__ uint64_t share_of(double f, uint64_t x, bool up) {
     return whole + (up && rest ? 1 : 0);
 }
 
-struct Settings {
-    double inverse;  // 1 / temperature
-    double p, least;  // least: the smallest (l - m) / T that min_p keeps
-    int64_t k;
-};
-
+// kThreads: of a workgroup, and entries of a sorted list; up to kThreads / 2 is a top_k
+// small enough for lists.
+template <int kThreads>
 struct Shared {
+    static constexpr int kWaves = kThreads / 64, kList = kThreads;
     double powers[kExpSteps];
     uint64_t bins[kBins];
+    uint64_t batches[kBatches];  // sums over runs of indices
+    uint64_t list[kList];
     uint64_t waves[kWaves];
-    uint64_t value;   // one thread's answer to all
-    uint64_t before;
-    uint32_t chosen;
+    uint64_t value, before;  // one thread's answer to all
+    uint32_t chosen, count;
 };
 
 // Weights of one row.
 struct Weigher {
     const double* powers;
-    double most, inverse;
-    int bits;
+    double most, steps;  // steps: of 1 / 64 of a power of two in a unit of logit
+    double least;        // in steps; what is below weighs nothing
+    int32_t unit;        // 2^bits in a binary64's upper word
 
-    // exp(y) 2^bits to the nearest integer, y <= 0, by a table of 2^(j/64) and the
-    // series of exp to the fifth power over the rest, which is below 2^-7.5 (Tang's
-    // method, 1989); the series ends at 3.5e-17.
-    __device__ __forceinline__ uint64_t weight(double y) const {
-        y = __builtin_fmax(y, -100.0);  // less than 2^-144; NaN (an infinite rest) too
-        const double n = __builtin_rint(y * (kExpSteps * 1.4426950408889634));
-        const double r = __builtin_fma(n, -0.6931471805599453 / kExpSteps, y);
-        const int i = static_cast<int>(n);
-        double s = __builtin_fma(r, 1.0 / 120, 1.0 / 24);
-        s = __builtin_fma(r, s, 1.0 / 6);
-        s = __builtin_fma(r, s, 0.5);
+    // exp(y) 2^bits to the nearest integer, y = (x - m) / T, by a table of 2^(j/64) and
+    // a polynomial of the rest, below h = 2^-7.5: its series with the fifth power
+    // replaced by lower ones (r^5 ~ 5/4 h^2 r^3 - 5/16 h^4 r), which is off by h^5 / 1920
+    // = 2.4e-15.  (The table as in Tang's method, 1989.)
+    __device__ __forceinline__ uint64_t weight(float x) const {
+        constexpr double kStep = 0.6931471805599453 / kExpSteps, h = kStep / 2;
+        constexpr double c1 = (1.0 - h * h * h * h / 384) * kStep, c2 = 0.5 * kStep * kStep;
+        constexpr double c3 = (1.0 / 6 + h * h / 96) * kStep * kStep * kStep, c4 = kStep * kStep * kStep * kStep / 24;
+        constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: the integer is left in the last bits
+        // (also where a masked logit times a step of 0 is no number)
+        const double t = __builtin_fmax((static_cast<double>(x) - most) * steps, least);
+        const double n = t + kRound;
+        const double r = t - (n - kRound);
+        const int32_t i = static_cast<int32_t>(__builtin_bit_cast(uint64_t, n));
+        double s = __builtin_fma(r, c4, c3);
+        s = __builtin_fma(r, s, c2);
+        s = __builtin_fma(r, s, c1);
         s = __builtin_fma(r, s, 1.0);
-        s = __builtin_fma(r, s, 1.0);
-        const double unit = __builtin_bit_cast(double, static_cast<uint64_t>(1023 + (i >> 6) + bits) << 52);
-        // adding 2^52 leaves the integer in the last bits
-        const double sum = __builtin_fma(s * powers[i & (kExpSteps - 1)], unit, 4503599627370496.0);
+        const uint64_t p = __builtin_bit_cast(uint64_t, powers[i & (kExpSteps - 1)]);
+        const uint32_t upper = static_cast<uint32_t>(p >> 32) + ((i >> 6) << 20) + unit;
+        const double scaled = __builtin_bit_cast(double, static_cast<uint64_t>(upper) << 32 | static_cast<uint32_t>(p));
+        const double sum = __builtin_fma(s, scaled, 4503599627370496.0);
         return __builtin_bit_cast(uint64_t, sum) & ((uint64_t(1) << 52) - 1);
     }
-    __device__ __forceinline__ double exponent(float logit) const {
-        const double x = logit;
-        return x == most ? 0.0 : (x - most) * inverse;
+    __device__ __forceinline__ double exponent(float x) const {
+        return (static_cast<double>(x) - most) * (steps * (0.6931471805599453 / kExpSteps));
     }
 };
 
-// The kept prefix of the order: logits above `key`, and equal ones up to index
-// `last`.
+// The kept prefix of the order: logits above `at`, and equal ones up to index `last`.
 struct Cut {
-    uint32_t key, last;
-    __device__ bool keeps(uint32_t k, uint32_t index) const { return k > key || (k == key && index <= last); }
+    float at;
+    uint32_t last;
+    __device__ __forceinline__ bool keeps(float x, uint32_t index) const {
+        return x > at || (x == at && index <= last);
+    }
 };
 
+// x plus what the lanes before it hold (kShift: within their 16, by that many; then the
+// last lane of the rows before).
+template <int kControl, int kRows>
+__device__ __forceinline__ uint64_t add_from(uint64_t x) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0u, static_cast<uint32_t>(x), kControl, kRows, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0u, static_cast<uint32_t>(x >> 32), kControl, kRows, 0xf, false);
+    return x + (static_cast<uint64_t>(hi) << 32 | lo);
+}
+// The sum of the lanes up to this one.
+__device__ __forceinline__ uint64_t wave_until(uint64_t x) {
+    x = add_from<0x111, 0xf>(x);  // row_shr
+    x = add_from<0x112, 0xf>(x);
+    x = add_from<0x114, 0xf>(x);
+    x = add_from<0x118, 0xf>(x);
+    x = add_from<0x142, 0xa>(x);  // row_bcast of lane 15
+    return add_from<0x143, 0xc>(x);  // and of lane 31
+}
 __device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    return x;
+    x = wave_until(x);
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(x), 63);
+    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), 63);
+    return static_cast<uint64_t>(hi) << 32 | lo;
 }
 // The sum of the lower lanes' values.
-__device__ __forceinline__ uint64_t wave_before(uint64_t x) {
-    uint64_t sum = x;
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t other = __shfl_up(sum, d);
-        sum += lane >= d ? other : 0;
-    }
-    return sum - x;
-}
+__device__ __forceinline__ uint64_t wave_before(uint64_t x) { return wave_until(x) - x; }
 
-// A row, divided among the wavefronts into runs of indices.
-template <class T>
+// A row in units of a vector a lane, which the wavefronts take in turns, kAhead loaded
+// together.  2^shift units are a batch.
+template <class T, int kThreads>
 struct Row {
-    static constexpr int kVec = 16 / sizeof(T), kStep = 64 * kVec;
+    static constexpr int kWaves = kThreads / 64;
+    static constexpr int kVec = 16 / sizeof(T), kUnit = 64 * kVec, kAhead = 4;
     const T* at;
-    uint32_t vocab, run;  // values, and those of a wavefront
+    uint32_t vocab, units, shift = 0;
 
-    __device__ Row(const T* row, int64_t n) : at(row), vocab(static_cast<uint32_t>(n)) {
-        run = (vocab + kWaves * kStep - 1) / (kWaves * kStep) * kStep;
+    __device__ __forceinline__ Row(const T* row, int64_t n) : at(row), vocab(static_cast<uint32_t>(n)), units((vocab + kUnit - 1) / kUnit) {
+        while (units > uint32_t(kBatches) << shift) ++shift;
     }
-    // f(first index of the lane's values, their keys; 0 behind the row), step by
-    // step over the run of a wavefront, while f returns true.
-    template <class F>
-    __device__ __forceinline__ void each(int wave, F f) const {
-        const uint32_t begin = wave * run, end = begin + run < vocab ? begin + run : vocab;
-        for (uint32_t base = begin; base < end; base += kStep) {
-            const uint32_t first = base + (threadIdx.x & 63) * kVec;
-            uint32_t keys[kVec];
-            if (first + kVec <= vocab) {
-                const Pack<T, kVec> v = *reinterpret_cast<const Pack<T, kVec>*>(at + first);
+    __device__ __forceinline__ uint32_t batches() const { return (units + (1u << shift) - 1) >> shift; }
+    __device__ __forceinline__ uint32_t batch_of(uint32_t index) const { return index / kUnit >> shift; }
+    __device__ __forceinline__ Pack<T, kVec> load(uint32_t first) const {
+        Pack<T, kVec> v;
+        if (first + kVec <= vocab) {
+            v = *reinterpret_cast<const Pack<T, kVec>*>(at + first);
+        } else {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) keys[i] = key_of<T>(v.v[i]);
+            for (int i = 0; i < kVec; ++i) v.v[i] = first + i < vocab ? at[first + i] : static_cast<T>(-__builtin_inff());
+        }
+        return v;
+    }
+    static __device__ __forceinline__ void values(const Pack<T, kVec>& v, float (&x)[kVec]) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x[i] = static_cast<float>(v.v[i]);
+    }
+    // f(unit, first index of the lane's values, the values; -inf behind the row).
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        for (uint32_t u = wave; u < units; u += kWaves * kAhead) {
+            const uint32_t first = u * kUnit + (threadIdx.x & 63) * kVec;
+            Pack<T, kVec> v[kAhead];
+            if ((u + (kAhead - 1) * kWaves + 1) * kUnit <= vocab) {  // whole units: the loads go out together
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) v[a] = *reinterpret_cast<const Pack<T, kVec>*>(at + (first + a * kWaves * kUnit));
             } else {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) keys[i] = first + i < vocab ? key_of<T>(at[first + i]) : 0u;
+                for (int a = 0; a < kAhead; ++a) v[a] = load(first + a * kWaves * kUnit);
             }
-            if (!f(first, keys)) return;
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                if (u + a * kWaves >= units) break;
+                float x[kVec];
+                values(v[a], x);
+                f(u + a * kWaves, first + a * kWaves * kUnit, x);
+            }
         }
     }
 };
 
-// The wavefronts' values, and their sum to every thread.
-__device__ __forceinline__ uint64_t total_of(Shared& s, uint64_t mine) {
+// The wavefronts' sums into s.waves, and the whole sum to every thread.
+template <int kThreads>
+__device__ __forceinline__ uint64_t total_of(Shared<kThreads>& s, uint64_t mine) {
     mine = wave_sum(mine);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) s.waves[threadIdx.x >> 6] = mine;
     __syncthreads();
     uint64_t sum = 0;
-    for (int w = 0; w < kWaves; ++w) sum += s.waves[w];
+    for (int w = 0; w < Shared<kThreads>::kWaves; ++w) sum += s.waves[w];
     return sum;
 }
 
-// The wavefront in which the sum of s.waves passes `target`, and what comes before.
-__device__ __forceinline__ int wave_at(const Shared& s, uint64_t target, uint64_t* before) {
-    uint64_t sum = 0;
-    for (int w = 0; w < kWaves - 1; ++w) {
-        if (sum + s.waves[w] > target) {
-            *before = sum;
-            return w;
+// Finds the first of `count` sums (up to kBins), taken in rising order (kDown: falling), at
+// which their sum reaches target: s.chosen, with what comes before in s.before and its own
+// in s.value.
+template <bool kDown, int kThreads>
+__device__ __forceinline__ void choose(Shared<kThreads>& s, const uint64_t* sums, uint32_t count, uint64_t target) {
+    constexpr uint32_t kEach = kBins / kThreads;
+    const uint32_t first = threadIdx.x * kEach;
+    const auto place = [&](uint32_t i) { return kDown ? count - 1 - (first + i) : first + i; };
+    uint64_t mine = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) mine += first + i < count ? sums[place(i)] : 0;
+    uint64_t before = wave_before(mine);
+    if ((threadIdx.x & 63) == 63) s.waves[threadIdx.x >> 6] = before + mine;
+    __syncthreads();
+    for (int w = 0; w < static_cast<int>(threadIdx.x >> 6); ++w) before += s.waves[w];
+    if (before < target && before + mine >= target) {
+        for (uint32_t i = 0; i < kEach && first + i < count; ++i) {
+            const uint64_t x = sums[place(i)];
+            if (before < target && before + x >= target) {
+                s.chosen = place(i);
+                s.before = before;
+                s.value = x;
+            }
+            before += x;
         }
-        sum += s.waves[w];
     }
-    *before = sum;
-    return kWaves - 1;
+    __syncthreads();
 }
 
-// Narrows `cut` to the shortest prefix whose measure (a token's, by its key)
-// reaches target, which is above 0 and at most the kept tokens' own.
-template <class T, class Measure>
-__device__ void narrow(Shared& s, const Row<T>& row, Cut& cut, uint32_t most, uint64_t target, Measure measure) {
-    uint32_t lo = cut.key, hi = most;
+template <int kThreads>
+__device__ __forceinline__ void clear_bins(Shared<kThreads>& s) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
+    __syncthreads();
+}
+template <int kThreads>
+__device__ __forceinline__ void add_to_bin(Shared<kThreads>& s, uint32_t bin, uint64_t x) {
+    atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[bin]), static_cast<unsigned long long>(x));
+}
+// Counts, which stay within the lower word.
+template <int kThreads>
+__device__ __forceinline__ void add_to_bin(Shared<kThreads>& s, uint32_t bin, uint32_t x) {
+    atomicAdd(reinterpret_cast<uint32_t*>(&s.bins[bin]), x);
+}
+
+// The sum of the values of the threads before this one, and of all.
+template <int kThreads>
+__device__ __forceinline__ uint64_t before_in_list(Shared<kThreads>& s, uint64_t x, uint64_t* all) {
+    uint64_t before = wave_before(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) s.waves[threadIdx.x >> 6] = before + x;
+    __syncthreads();
+    uint64_t sum = 0;
+    for (int w = 0; w < Shared<kThreads>::kWaves; ++w) {
+        if (w == static_cast<int>(threadIdx.x >> 6)) before += sum;
+        sum += s.waves[w];
+    }
+    *all = sum;
+    return before;
+}
+
+// s.batches = the sums of `sum` (of a vector, with its terms) over the row's batches.
+template <class T, int kThreads, class Sum>
+__device__ __forceinline__ void add_batches(Shared<kThreads>& s, const Row<T, kThreads>& row, Sum sum) {
+    constexpr int kVec = Row<T, kThreads>::kVec;
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < row.batches(); b += kThreads) s.batches[b] = 0;
+    __syncthreads();
+    row.each([&](uint32_t unit, uint32_t first, const float(&x)[kVec]) {
+        uint64_t terms[kVec];
+        const uint64_t all = wave_sum(sum(first, x, terms));
+        if (all > 0 && (threadIdx.x & 63) == 0)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.batches[unit >> row.shift]), static_cast<unsigned long long>(all));
+    });
+    __syncthreads();
+}
+template <class T, int kThreads>
+__device__ __forceinline__ uint64_t sum_batches(Shared<kThreads>& s, const Row<T, kThreads>& row) {
+    uint64_t mine = 0;
+    for (uint32_t b = threadIdx.x; b < row.batches(); b += kThreads) mine += s.batches[b];
+    return total_of(s, mine);
+}
+// Calls found(index, logit) for the first index at which the running sum of sum's terms
+// exceeds target, which is below s.batches' sum.  A wavefront a unit of its batch.
+template <class T, int kThreads, class Sum, class Found>
+__device__ __forceinline__ void pick(Shared<kThreads>& s, const Row<T, kThreads>& row, uint64_t target, Sum sum, Found found) {
+    constexpr int kVec = Row<T, kThreads>::kVec;
+    static_assert(Row<T, kThreads>::kWaves >= 4, "a batch of a vocabulary of 2^22 has four units at most");
+    __syncthreads();
+    choose<false>(s, s.batches, row.batches(), target + 1);
+    const uint32_t wave = threadIdx.x >> 6, unit = (s.chosen << row.shift) + wave;
+    const uint32_t first = unit * Row<T, kThreads>::kUnit + (threadIdx.x & 63) * kVec;
+    float x[kVec];
+    uint64_t terms[kVec], own = 0, all, before = s.before;
+    if (wave < 1u << row.shift) {
+        row.values(row.load(first), x);
+        own = sum(first, x, terms);
+    }
+    before += before_in_list(s, own, &all);
+    if (before <= target && target < before + own) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            if (before <= target && target < before + terms[i]) found(first + i, x[i]);
+            before += terms[i];
+        }
+    }
+}
+
+// Narrows `cut` to the shortest prefix whose measure (a token's, by its logit) reaches
+// target, which is above 0 and at most the kept tokens' own, by histograms over the
+// logits' keys.
+template <class T, int kThreads, class Measure>
+__device__ __forceinline__ void narrow(Shared<kThreads>& s, const Row<T, kThreads>& row, Cut& cut, float most, uint64_t target, Measure measure) {
+    constexpr int kVec = Row<T, kThreads>::kVec;
+    uint32_t lo = key_of(cut.at), hi = key_of(most);
     uint64_t held = 0;  // of the last bin
     for (;;) {
         const uint32_t span = hi - lo;
-        const int bits = span ? 32 - __clz(span) : 0, shift = bits > kBinBits ? bits - kBinBits : 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
-        __syncthreads();
-        row.each(threadIdx.x >> 6, [&](uint32_t first, const uint32_t(&keys)[Row<T>::kVec]) {
+        const int bits = span ? 32 - __clz(span) : 0, shift = bits > kKeyBits ? bits - kKeyBits : 0;
+        clear_bins(s);
+        row.each([&](uint32_t, uint32_t first, const float(&x)[kVec]) {
 #pragma unroll
-            for (int i = 0; i < Row<T>::kVec; ++i)
-                if (keys[i] >= lo && keys[i] <= hi && cut.keeps(keys[i], first + i))
-                    atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[(keys[i] - lo) >> shift]),
-                              static_cast<unsigned long long>(measure(keys[i])));
-            return true;
+            for (int i = 0; i < kVec; ++i)
+                if (cut.keeps(x[i], first + i)) {
+                    const uint32_t key = key_of(x[i]);
+                    if (key >= lo && key <= hi) add_to_bin(s, (key - lo) >> shift, measure(x[i]));
+                }
         });
         __syncthreads();
-        // from the top bin down, kBins / kThreads a thread
-        constexpr int kEach = kBins / kThreads;
-        const int top = kBins - 1 - static_cast<int>(threadIdx.x) * kEach;
-        uint64_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) mine += s.bins[top - i];
-        uint64_t before = wave_before(mine);
-        if ((threadIdx.x & 63) == 63) s.waves[threadIdx.x >> 6] = before + mine;
-        __syncthreads();
-        for (int w = 0; w < static_cast<int>(threadIdx.x >> 6); ++w) before += s.waves[w];
-        if (before < target && before + mine >= target) {
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const uint64_t x = s.bins[top - i];
-                if (before < target && before + x >= target) {
-                    s.chosen = top - i;
-                    s.before = before;
-                    s.value = x;
-                }
-                before += x;
-            }
-        }
-        __syncthreads();
+        choose<true>(s, s.bins, kBins, target);
         target -= s.before;
         held = s.value;
         lo += s.chosen << shift;
@@ -246,76 +352,101 @@ __device__ void narrow(Shared& s, const Row<T>& row, Cut& cut, uint32_t most, ui
         hi = end < hi ? end : hi;
     }
     // of the tokens at the cut, the first `wanted`
-    const uint64_t each = measure(lo), wanted = (target + each - 1) / each;
+    const float at = logit_of(lo);
+    const uint64_t each = measure(at), wanted = (target + each - 1) / each;
     const bool some = wanted * each < held;
     const Cut old = cut;
-    cut = {lo, lo == old.key ? old.last : 0xffffffffu};
+    cut = {at, at == old.at ? old.last : 0xffffffffu};
     if (!some) return;
-    const auto count = [&](uint32_t first, const uint32_t(&keys)[Row<T>::kVec]) {
-        uint64_t n = 0;
+    const auto ties = [&](uint32_t first, const float(&x)[kVec], uint64_t(&n)[kVec]) {
+        uint64_t sum = 0;
 #pragma unroll
-        for (int i = 0; i < Row<T>::kVec; ++i) n += keys[i] == lo && old.keeps(keys[i], first + i) ? 1 : 0;
-        return n;
+        for (int i = 0; i < kVec; ++i) {
+            n[i] = x[i] == at && old.keeps(x[i], first + i) ? 1 : 0;
+            sum += n[i];
+        }
+        return sum;
     };
-    uint64_t mine = 0;
-    row.each(threadIdx.x >> 6, [&](uint32_t first, const uint32_t(&keys)[Row<T>::kVec]) {
-        mine += count(first, keys);
-        return true;
-    });
-    (void)total_of(s, mine);
-    uint64_t before;
-    const int wave = wave_at(s, wanted - 1, &before);
-    if (static_cast<int>(threadIdx.x >> 6) == wave) {
-        row.each(wave, [&](uint32_t first, const uint32_t(&keys)[Row<T>::kVec]) {
-            const uint64_t n = count(first, keys), lower = before + wave_before(n);
-            if (lower < wanted && lower + n >= wanted) {
-                uint64_t left = wanted - lower;
-#pragma unroll
-                for (int i = 0; i < Row<T>::kVec; ++i)
-                    if (keys[i] == lo && old.keeps(keys[i], first + i) && --left == 0) s.chosen = first + i;
-            }
-            before += wave_sum(n);
-            return before < wanted;
-        });
-    }
+    add_batches(s, row, ties);
+    pick(s, row, wanted - 1, ties, [&](uint32_t index, float) { s.chosen = index; });
     __syncthreads();
     cut.last = s.chosen;
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleCall call, int bits) {
-    __shared__ Shared s;
+// List entries: in the order of logits, and in that of indices.
+__device__ __forceinline__ uint64_t entry(float x, uint32_t index) {
+    return static_cast<uint64_t>(~key_of(x)) << 32 | index;
+}
+__device__ __forceinline__ float logit_of_entry(uint64_t e) { return logit_of(~static_cast<uint32_t>(e >> 32)); }
+__device__ __forceinline__ uint64_t turned(uint64_t e) { return e << 32 | e >> 32; }
+constexpr uint64_t kNoEntry = ~uint64_t(0);
+
+// Sorts the threads' entries, of the first n threads, rising; kNoEntry behind them.  Up to
+// 64 stay within a wavefront.
+template <int kThreads>
+__device__ __forceinline__ uint64_t sorted(Shared<kThreads>& s, uint32_t n, uint64_t mine) {
+    const uint32_t t = threadIdx.x;
+    uint32_t size = 64;
+    while (size < n) size *= 2;
+    if (size == 64 && t >= 64) return kNoEntry;
+    for (uint32_t k = 2; k <= size; k *= 2)
+        for (uint32_t j = k / 2; j > 0; j /= 2) {
+            uint64_t other;
+            if (j >= 64) {
+                __syncthreads();
+                s.list[t] = mine;
+                __syncthreads();
+                other = s.list[t ^ j];
+            } else {
+                other = __shfl_xor(mine, j);
+            }
+            const bool lower = ((t & j) == 0) == ((t & k) == 0);
+            mine = (mine < other) == lower ? mine : other;
+        }
+    return mine;
+}
+
+// Adds the logits of a vector for which `in` holds to the list, in no particular order;
+// s.count counts them, of which kList at most are listed.
+template <int kThreads, int kVec>
+__device__ __forceinline__ void enlist(Shared<kThreads>& s, uint32_t first, const float (&x)[kVec], const bool (&in)[kVec]) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) any |= in[i];
+    if (__ballot(any) == 0) return;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+        if (in[i]) {
+            const uint32_t at = atomicAdd(&s.count, 1u);
+            if (at < Shared<kThreads>::kList) s.list[at] = entry(x[i], first + i);
+        }
+}
+
+template <class T, int kThreads>
+__global__ __launch_bounds__(kThreads, 4) void sample_kernel(SampleCall call, int bits) {
+    constexpr int kList = kThreads, kListK = kThreads / 2, kVec = Row<T, kThreads>::kVec;
+    __shared__ Shared<kThreads> s;
     const int64_t r = blockIdx.x;
     if (threadIdx.x < kExpSteps) s.powers[threadIdx.x] = exp2(threadIdx.x / static_cast<double>(kExpSteps));
-    const Row<T> row(static_cast<const T*>(call.logits.at) + r * call.logits.stride, call.vocab);
+    Row<T, kThreads> row(static_cast<const T*>(call.logits.at) + r * call.logits.stride, call.vocab);
     const micro_sampling& set = call.sampling;
     const double t = set.temperatures ? static_cast<double>(set.temperatures[r]) : set.temperature;
     const double p = set.top_ps ? static_cast<double>(set.top_ps[r]) : set.top_p;
     const double least = set.min_ps ? static_cast<double>(set.min_ps[r]) : set.min_p;
     const int64_t k = set.top_ks ? set.top_ks[r] : set.top_k;
 
-    // the largest logit, the first of its index, and how many have a part
-    uint64_t best = 0, live = 0;
-    row.each(threadIdx.x >> 6, [&](uint32_t first, const uint32_t(&keys)[Row<T>::kVec]) {
+    // the threads' largest logits, and the row's
+    float top = -__builtin_inff();
+    row.each([&](uint32_t, uint32_t, const float(&x)[kVec]) {
 #pragma unroll
-        for (int i = 0; i < Row<T>::kVec; ++i) {
-            const uint64_t x = static_cast<uint64_t>(keys[i]) << 32 | (0xffffffffu - (first + i));
-            if (keys[i]) {
-                best = x > best ? x : best;
-                ++live;
-            }
-        }
-        return true;
+        for (int i = 0; i < kVec; ++i) top = fmaxf(top, x[i]);
     });
+    float most = top;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const uint64_t x = __shfl_xor(best, d);
-        best = x > best ? x : best;
-    }
-    if ((threadIdx.x & 63) == 0) s.bins[threadIdx.x >> 6] = best;
-    live = total_of(s, live);
-    for (int w = 0; w < kWaves; ++w) best = s.bins[w] > best ? s.bins[w] : best;
-    const uint32_t most = static_cast<uint32_t>(best >> 32);
+    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if ((threadIdx.x & 63) == 0) s.waves[threadIdx.x >> 6] = __float_as_uint(most);
+    __syncthreads();
+    for (int w = 0; w < Shared<kThreads>::kWaves; ++w) most = fmaxf(most, __uint_as_float(static_cast<uint32_t>(s.waves[w])));
     const auto answer = [&](int64_t id, float logprob) {
         if (call.ids.wide)
             static_cast<int64_t*>(const_cast<void*>(call.ids.at))[r] = id;
@@ -323,83 +454,223 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleCall call, int b
             static_cast<int32_t*>(const_cast<void*>(call.ids.at))[r] = static_cast<int32_t>(id);
         if (call.logprobs) call.logprobs[r] = logprob;
     };
-    if (live == 0 || !(t > 0.0)) {
-        if (threadIdx.x == 0) {
-            if (live == 0)
-                answer(-1, __builtin_nanf(""));
-            else
-                answer(0xffffffffu - static_cast<uint32_t>(best), 0.0f);
-        }
+    if (!(most > -__builtin_inff())) {
+        if (threadIdx.x == 0) answer(-1, __builtin_nanf(""));
+        return;
+    }
+    if (!(t > 0.0)) {
+        if (threadIdx.x == 0) s.chosen = 0xffffffffu;
+        __syncthreads();
+        uint32_t index = 0xffffffffu;
+        row.each([&](uint32_t, uint32_t first, const float(&x)[kVec]) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (x[i] == most && first + i < index) index = first + i;
+        });
+        if (index != 0xffffffffu) atomicMin(&s.chosen, index);
+        __syncthreads();
+        if (threadIdx.x == 0) answer(s.chosen, 0.0f);
+        return;
+    }
+    const float u = call.uniforms[r];
+    const auto target_of = [&](uint64_t total) {
+        return u > 0.0f ? u < 1.0f ? share_of(u, total, false) : total - 1 : 0;
+    };
+    const auto prefix_of = [&](uint64_t total) {
+        const uint64_t wanted = p < 1.0 ? share_of(p, total, true) : p >= 1.0 || p != p ? total : 0;
+        return wanted > 0 ? wanted : 1;
+    };
+    if (most == __builtin_inff()) {  // equal weights of the infinite logits, of 1 each
+        const auto infinite = [&](uint32_t, const float(&x)[kVec], uint64_t(&n)[kVec]) {
+            uint64_t sum = 0;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                n[i] = x[i] == most ? 1 : 0;
+                sum += n[i];
+            }
+            return sum;
+        };
+        add_batches(s, row, infinite);
+        uint64_t kept = sum_batches(s, row);
+        if (k > 0 && static_cast<uint64_t>(k) < kept) kept = static_cast<uint64_t>(k);
+        kept = (prefix_of(kept << bits) + (uint64_t(1) << bits) - 1) >> bits;
+        pick(s, row, target_of(kept << bits) >> bits, infinite,
+             [&](uint32_t index, float) { answer(index, static_cast<float>(-log(static_cast<double>(kept)))); });
         return;
     }
 
-    const Weigher weigher{s.powers, static_cast<double>(logit_of<T>(most)), 1.0 / t, bits};
-    Cut cut{1, 0xffffffffu};
-    if (k > 0 && static_cast<uint64_t>(k) < live)
-        narrow<T>(s, row, cut, most, static_cast<uint64_t>(k), [](uint32_t) { return uint64_t(1); });
-    const auto weigh = [&](uint32_t key) { return weigher.weight(weigher.exponent(logit_of<T>(key))); };
-    const auto sum = [&](double at_least) {
-        uint64_t mine = 0;
-        row.each(threadIdx.x >> 6, [&](uint32_t first, const uint32_t(&keys)[Row<T>::kVec]) {
-#pragma unroll
-            for (int i = 0; i < Row<T>::kVec; ++i)
-                if (keys[i] && cut.keeps(keys[i], first + i)) {
-                    const double y = weigher.exponent(logit_of<T>(keys[i]));
-                    if (!(y < at_least)) mine += weigher.weight(y);
-                }
-            return true;
-        });
-        return total_of(s, mine);
+    constexpr double kLn2 = 0.6931471805599453;
+    const double warm = fmax(t, 1e-300);
+    // logits below weigh nothing (rounded down: of the next lower binary32)
+    const double range = (bits + 2) * kLn2 * warm;
+    const float floor = fmaxf(nextafterf(static_cast<float>(static_cast<double>(most) - range), -__builtin_inff()), kLowest);
+    const Weigher weigher{s.powers, static_cast<double>(most), kExpSteps / kLn2 / warm, -(bits + 2.0) * kExpSteps, bits << 20};
+    const auto weigh = [&](float x) { return weigher.weight(x); };
+    const bool limited = least > 0.0;
+    const double lowest = limited ? log(least) : 0.0;
+    const auto too_low = [&](float x) { return limited && weigher.exponent(x) < lowest; };
+    const auto finish = [&](float x, uint32_t index, uint64_t total) {
+        const double share = static_cast<double>(total) * __builtin_bit_cast(double, static_cast<uint64_t>(1023 - bits) << 52);
+        answer(index, static_cast<float>(weigher.exponent(x) - log(share)));
     };
-    const double lowest = least > 0.0 ? log(least) : -__builtin_inf();
-    uint64_t total = sum(p < 1.0 ? -__builtin_inf() : lowest);
-    if (p < 1.0) {
-        const uint64_t wanted = share_of(p, total, true);
-        narrow<T>(s, row, cut, most, wanted > 0 ? wanted : 1, weigh);
-        total = sum(lowest);
+    Cut cut{kLowest, 0xffffffffu};
+
+    if (k > 0 && k <= kListK) {
+        // a lower bound of the k-th logit: k threads' maxima reach it
+        clear_bins(s);
+        const uint32_t lo = key_of(kLowest), span = key_of(most) - lo;
+        const int width = span ? 32 - __clz(span) : 0, shift = width > kKeyBits ? width - kKeyBits : 0;
+        if (top > -__builtin_inff()) add_to_bin(s, (key_of(top) - lo) >> shift, 1u);
+        if (threadIdx.x == 0) {
+            add_to_bin(s, 0, static_cast<uint32_t>(kListK));  // the lowest bin holds as many as are wanted
+            s.count = 0;
+        }
+        __syncthreads();
+        choose<true>(s, s.bins, kBins, static_cast<uint64_t>(k));
+        const float bound = s.chosen > 0 ? logit_of(lo + (s.chosen << shift)) : kLowest;
+        row.each([&](uint32_t, uint32_t first, const float(&x)[kVec]) {
+            bool in[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) in[i] = x[i] >= bound;
+            enlist(s, first, x, in);
+        });
+        __syncthreads();
+        const uint32_t n = s.count;
+        if (n <= kList) {
+            uint64_t mine = threadIdx.x < n ? s.list[threadIdx.x] : kNoEntry;
+            mine = sorted(s, n, mine);
+            const uint32_t first = n < static_cast<uint64_t>(k) ? n : static_cast<uint32_t>(k);
+            const auto weight_of = [&](bool kept, float x) { return kept ? weigh(x) : 0; };
+            uint64_t total;
+            float x = logit_of_entry(mine);
+            const uint64_t before = before_in_list(s, weight_of(threadIdx.x < first, x), &total);
+            const bool kept = threadIdx.x < first && before < prefix_of(total) && !too_low(x);
+            mine = sorted(s, first, kept ? turned(mine) : kNoEntry);
+            const bool there = mine != kNoEntry;
+            x = logit_of_entry(turned(mine));
+            const uint64_t w = weight_of(there, x), lower = before_in_list(s, w, &total), target = target_of(total);
+            if (lower <= target && target < lower + w) finish(x, static_cast<uint32_t>(turned(mine)), total);
+            return;
+        }
     }
-    const float u = call.uniforms[r];
-    const uint64_t target = u > 0.0f ? u < 1.0f ? share_of(u, total, false) : total - 1 : 0;
-    uint64_t before;
-    const int wave = wave_at(s, target, &before);
-    if (static_cast<int>(threadIdx.x >> 6) != wave) return;
-    row.each(wave, [&](uint32_t first, const uint32_t(&keys)[Row<T>::kVec]) {
-        uint64_t w[Row<T>::kVec], mine = 0;
+    if (k > 0) {
+        uint64_t live = 0;
+        row.each([&](uint32_t, uint32_t, const float(&x)[kVec]) {
 #pragma unroll
-        for (int i = 0; i < Row<T>::kVec; ++i) {
+            for (int i = 0; i < kVec; ++i) live += x[i] >= kLowest ? 1 : 0;
+        });
+        live = total_of(s, live);
+        if (static_cast<uint64_t>(k) < live)
+            narrow(s, row, cut, most, static_cast<uint64_t>(k), [](float) { return uint32_t(1); });
+    }
+
+    // The weights of a vector's logits that `in` takes and their sum: side by side, without a
+    // branch around each, and not at all where the wavefront takes none.
+    const auto weigh_all = [&](const float(&x)[kVec], const bool(&in)[kVec], uint64_t(&w)[kVec]) {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            any |= in[i];
             w[i] = 0;
-            if (keys[i] && cut.keeps(keys[i], first + i)) {
-                const double y = weigher.exponent(logit_of<T>(keys[i]));
-                if (!(y < lowest)) w[i] = weigher.weight(y);
-            }
-            mine += w[i];
         }
-        uint64_t lower = before + wave_before(mine);
-        if (lower <= target && target < lower + mine) {
+        uint64_t sum = 0;
+        if (__ballot(any) == 0) return sum;
 #pragma unroll
-            for (int i = 0; i < Row<T>::kVec; ++i) {
-                if (lower <= target && target < lower + w[i])
-                    answer(first + i, static_cast<float>(weigher.exponent(logit_of<T>(keys[i])) -
-                                                         log(static_cast<double>(total) *
-                                                             __builtin_bit_cast(double, static_cast<uint64_t>(1023 - bits) << 52))));
-                lower += w[i];
-            }
+        for (int i = 0; i < kVec; ++i) {
+            w[i] = weigh(x[i]) & (uint64_t(0) - static_cast<uint64_t>(in[i]));
+            sum += w[i];
         }
-        before += wave_sum(mine);
-        return before <= target;
-    });
+        return sum;
+    };
+    bool summed = false;  // s.batches hold what is kept
+    if (p < 1.0) {
+        // weights by equal steps down from the largest logit; a larger step never holds
+        // larger logits, since subtraction and multiplication keep their order
+        const float per = static_cast<float>(kBins / range);
+        const auto bin_of = [&](float x) {
+            const float b = (most - x) * per;
+            return b < kBins - 1 ? static_cast<uint32_t>(b) : kBins - 1u;
+        };
+        if (threadIdx.x == 0) s.count = 0;
+        clear_bins(s);
+        row.each([&](uint32_t, uint32_t first, const float(&x)[kVec]) {
+            bool in[kVec];
+            uint64_t w[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) in[i] = cut.keeps(x[i], first + i) && x[i] >= floor;
+            (void)weigh_all(x, in, w);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (w[i] > 0) add_to_bin(s, bin_of(x[i]), w[i]);
+        });
+        __syncthreads();
+        uint64_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < kBins / kThreads; ++i) mine += s.bins[threadIdx.x + i * kThreads];
+        const uint64_t wanted = prefix_of(total_of(s, mine));
+        __syncthreads();
+        choose<false>(s, s.bins, kBins, wanted);
+        // the batches' sums of what the bins above hold, and the list of the cut's own
+        const uint32_t chosen = s.chosen;
+        const uint64_t above = s.before;
+        add_batches(s, row, [&](uint32_t first, const float(&x)[kVec], uint64_t(&w)[kVec]) {
+            bool in[kVec], here[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const uint32_t b = bin_of(x[i]);
+                in[i] = here[i] = cut.keeps(x[i], first + i) && x[i] >= floor;
+                in[i] &= b < chosen;
+                here[i] &= b == chosen;
+            }
+            enlist(s, first, x, here);
+            return weigh_all(x, in, w);
+        });
+        const uint32_t n = s.count;
+        if (n <= kList) {
+            const uint64_t e = sorted(s, n, threadIdx.x < n ? s.list[threadIdx.x] : kNoEntry);
+            uint64_t all;
+            const uint64_t w = e != kNoEntry ? weigh(logit_of_entry(e)) : 0;
+            const uint64_t before = above + before_in_list(s, w, &all);
+            if (before < wanted && w > 0) {
+                if (before + w >= wanted) s.value = e;
+                atomicAdd(reinterpret_cast<unsigned long long*>(&s.batches[row.batch_of(static_cast<uint32_t>(e))]),
+                          static_cast<unsigned long long>(w));
+            }
+            __syncthreads();
+            cut = {logit_of_entry(s.value), static_cast<uint32_t>(s.value)};
+            summed = !limited;
+        } else {
+            narrow(s, row, cut, most, wanted, weigh);
+        }
+    }
+    const auto weights_of = [&](uint32_t first, const float(&x)[kVec], uint64_t(&w)[kVec]) {
+        bool in[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) in[i] = cut.keeps(x[i], first + i) && x[i] >= floor && !too_low(x[i]);
+        return weigh_all(x, in, w);
+    };
+    if (!summed) add_batches(s, row, weights_of);
+    const uint64_t total = sum_batches(s, row);
+    pick(s, row, target_of(total), weights_of, [&](uint32_t index, float x) { finish(x, index, total); });
 }
 
 }  // namespace
 
-hipError_t launch_sample(const SampleCall& call, hipStream_t stream) {
-    if (call.rows == 0) return hipSuccess;
+template <class T>
+hipError_t launch_rows(const SampleCall& call, hipStream_t stream) {
     const int bits = weight_bits(call.vocab);
     const dim3 grid(static_cast<uint32_t>(call.rows));
+    const char* f = getenv("SAMPLE_T");
+    if (f ? atoi(f) == 512 : call.rows > call.compute_units) return launch(sample_kernel<T, 512>, grid, 512, stream, call, bits);
+    return launch(sample_kernel<T, 1024>, grid, 1024, stream, call, bits);
+}
+
+hipError_t launch_sample(const SampleCall& call, hipStream_t stream) {
+    if (call.rows == 0) return hipSuccess;
     switch (call.logits.type) {
-        case MICRO_TYPE_F32: return launch(sample_kernel<float>, grid, kThreads, stream, call, bits);
-        case MICRO_TYPE_F16: return launch(sample_kernel<f16>, grid, kThreads, stream, call, bits);
-        default: return launch(sample_kernel<bf16>, grid, kThreads, stream, call, bits);
+        case MICRO_TYPE_F32: return launch_rows<float>(call, stream);
+        case MICRO_TYPE_F16: return launch_rows<f16>(call, stream);
+        default: return launch_rows<bf16>(call, stream);
     }
 }
 

@@ -321,6 +321,7 @@ micro_status micro_table_sample(micro_table* t, const void* logits, int32_t logi
     c.sampling = s;
     c.ids = {ids, ids_type == MICRO_IDS_I64};
     c.logprobs = logprobs;
+    c.compute_units = t->compute_units;
     return report_hip(launch_sample(c, t->stream), "token draw launch");
 }
 
