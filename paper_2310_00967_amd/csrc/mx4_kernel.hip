@@ -7,6 +7,7 @@
 #include "mx4_kernel.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 #include "micro_sparsify.h"
@@ -46,136 +47,220 @@ __device__ __forceinline__ float power_of(uint32_t scale) {
     return scale == kNanScale ? __builtin_nanf("") : scale == 0 ? 0x1p-127f : __uint_as_float(scale << 23);
 }
 
-// Eight codes, the first in the lowest bits.  The conversion rounds to nearest
+// Codes of kN values, the first in the lowest bits.  The conversion rounds to nearest
 // even and ends at 6.
-__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], uint32_t scale) {
+template <int kN>
+__device__ __forceinline__ uint32_t codes_of(const float (&v)[kN], uint32_t scale) {
+    static_assert(kN == 4 || kN == 8, "two values a byte");
     if (scale == kNanScale) return 0;
     const float by = inverse_of(scale);
     uint32_t c = 0;
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * by, v[1] * by, 1.0f, 0);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * by, v[3] * by, 1.0f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * by, v[5] * by, 1.0f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * by, v[7] * by, 1.0f, 3);
+    if constexpr (kN == 8) {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * by, v[5] * by, 1.0f, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * by, v[7] * by, 1.0f, 3);
+    }
     return c;
 }
+
+// The largest of this lane's value and others': of the four lanes of its quad, of the
+// quad beside it.
+template <int kControl>
+__device__ __forceinline__ uint32_t most_with(uint32_t x) {
+    return max(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0u, x, kControl, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ uint32_t most_of_quad(uint32_t x) { return most_with<0x4e>(most_with<0xb1>(x)); }
+__device__ __forceinline__ uint32_t most_of_eight(uint32_t x) { return most_with<0x141>(most_of_quad(x)); }
 
 // ---------------------------------------------------------------------------
 // packing
 // ---------------------------------------------------------------------------
 
+// N values of which the first `valid` are there, zeros behind.
 template <class T, int N>
-__device__ __forceinline__ void load_some(const T* p, int64_t valid, float (&v)[N]) {
-    if (valid >= N) {
-        load_floats(p, v);
-    } else {
+__device__ __forceinline__ Pack<T, N> load_some(const T* p, int64_t valid) {
+    if (valid >= N) return *reinterpret_cast<const Pack<T, N>*>(p);
+    Pack<T, N> v;
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = i < valid ? static_cast<float>(p[i]) : 0.0f;
-    }
+    for (int i = 0; i < N; ++i) v.v[i] = i < valid ? p[i] : static_cast<T>(0.0f);
+    return v;
 }
 
 // Rows: a workgroup takes kPackRows rows of kPackGroups groups, sixteen lanes a row's
 // group, eight values a lane, so that neighbouring lanes read one row and the
-// workgroup's stores fill whole lines of a group's rows.
-constexpr int kPackThreads = 256, kPackRows = 16, kPackGroups = 8, kPackLanes = kMxGroup / 8;
+// workgroup's stores fill whole lines of a group's rows.  Bound by memory: 50257 x 2048
+// bfloat16 values in 41 us, 6.3 TB/s.
+constexpr int kPackThreads = 256, kPackRows = 8, kPackGroups = 8, kPackLanes = kMxGroup / 8;
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* x, int64_t stride, Mx4 to) {
-    const int64_t wide = (to.groups + kPackGroups - 1) / kPackGroups;
-    const int64_t tiles = (to.rows + kPackRows - 1) / kPackRows * wide;
     const int lane = threadIdx.x % kPackLanes, part = threadIdx.x / kPackLanes;
     constexpr int kRowsAtOnce = kPackThreads / kPackLanes / kPackGroups;
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t g = tile % wide * kPackGroups + part % kPackGroups;
-        const int64_t r0 = tile / wide * kPackRows + part / kPackGroups;
-        if (g >= to.groups) continue;
-        const int64_t c = g * kMxGroup + lane * 8;
+    const int64_t g = static_cast<int64_t>(blockIdx.x) * kPackGroups + part % kPackGroups;
+    const int64_t c = g * kMxGroup + lane * 8;
+    if (g >= to.groups) return;
+    for (int64_t r0 = static_cast<int64_t>(blockIdx.y) * kPackRows + part / kPackGroups; r0 < to.rows;
+         r0 += static_cast<int64_t>(gridDim.y) * kPackRows) {
+        constexpr int kEach = kPackRows / kRowsAtOnce;
+        Pack<T, 8> raw[kEach];
+        if (c + 8 <= to.cols && r0 + (kEach - 1) * kRowsAtOnce < to.rows) {  // the loads go out together
 #pragma unroll
-        for (int i = 0; i < kPackRows / kRowsAtOnce; ++i) {
+            for (int i = 0; i < kEach; ++i) raw[i] = *reinterpret_cast<const Pack<T, 8>*>(x + (r0 + i * kRowsAtOnce) * stride + c);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int64_t r = r0 + i * kRowsAtOnce;
+                raw[i] = load_some<T, 8>(x + r * stride + c, r < to.rows ? to.cols - c : 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
             const int64_t r = r0 + i * kRowsAtOnce;
             if (r >= to.rows) break;
             float v[8];
-            load_some(x + r * stride + c, to.cols - c, v);
             uint32_t most = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) most = max(most, magnitude(v[j]));
-            most = max(most, __shfl_xor(most, 1));
-            most = max(most, __shfl_xor(most, 2));
-            const uint32_t scale = scale_of(most);
+            for (int j = 0; j < 8; ++j) {
+                v[j] = static_cast<float>(raw[i].v[j]);
+                most = max(most, magnitude(v[j]));
+            }
+            const uint32_t scale = scale_of(most_of_quad(most));
             *reinterpret_cast<uint32_t*>(to.codes + (g * to.rows + r) * kMxBytes + lane * 4) = codes_of(v, scale);
             if ((lane & 3) == 0) to.scales[(g * to.rows + r) * kMxBlocks + lane / 4] = static_cast<uint8_t>(scale);
         }
     }
 }
 
-// Columns: a thread takes kVec adjacent columns of one block of 32 rows, the
-// four blocks of a group beside each other, so that the codes of neighbouring columns
-// are written as whole lines.
-template <class T>
-struct Turn {
-    static constexpr int kVec = 16 / sizeof(T), kAcross = 64 / kMxBlocks;  // threads of a wavefront along a row
-    static constexpr int kColumns = kAcross * kVec * kPackThreads / 64;
-};
-template <class T>
-__global__ __launch_bounds__(kPackThreads) void pack_turned_kernel(const T* x, int64_t stride, Mx4 to) {
-    constexpr int kVec = Turn<T>::kVec, kAcross = Turn<T>::kAcross, kColumns = Turn<T>::kColumns;
-    const int64_t across = (to.rows + kColumns - 1) / kColumns, tiles = across * to.groups;
+// Columns, and rows from the same reading: a workgroup takes a group of kMxGroup rows by
+// kTurnColumns columns, a thread kTurnVec adjacent columns of one block of 32 rows in
+// registers.  The four blocks of a group lie beside each other, so that the turned codes
+// of neighbouring columns are written as whole lines; those of the rows change places in
+// shared memory, to leave as runs of kMxGroup rows of a group.
+// Four columns a thread: with eight, of 16-bit types, the values take 256 registers and
+// 16384 x 8192 takes 180 us.
+constexpr int kTurnVec = 4, kTurnColumns = 64 / kMxBlocks * kTurnVec * (kPackThreads / 64);
+static_assert(kTurnColumns == 2 * kMxGroup, "two groups of rows' values");
+template <class T, bool kRows>
+__global__ __launch_bounds__(kPackThreads) void pack_turned_kernel(const T* x, int64_t stride, Mx4 rows, Mx4 turned) {
+    __shared__ __attribute__((aligned(16))) uint16_t codes[kRows ? 2 : 1][kRows ? kMxGroup : 1][kMxBytes / 2];
+    __shared__ __attribute__((aligned(16))) uint8_t scales[kRows ? 2 : 1][kRows ? kMxGroup : 1][kMxBlocks];
+    constexpr int kAcross = 64 / kMxBlocks;  // threads of a wavefront along a row
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, block = lane / kAcross;
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t g = tile / across;
-        const int64_t c = tile % across * kColumns + (wave * kAcross + lane % kAcross) * kVec;
+    const int at = (wave * kAcross + lane % kAcross) * kTurnVec;  // in the workgroup's columns
+    const int64_t c0 = static_cast<int64_t>(blockIdx.x) * kTurnColumns, c = c0 + at;
+    for (int64_t g = blockIdx.y; g < turned.groups; g += gridDim.y) {
         const int64_t k = g * kMxGroup + block * kMxBlock;
-        if (c >= to.rows) continue;
-        float v[kMxBlock][kVec];
+        Pack<T, kTurnVec> raw[kMxBlock];
+        if (c0 + kTurnColumns <= turned.rows && (g + 1) * kMxGroup <= turned.cols) {  // the loads go out together
 #pragma unroll
-        for (int i = 0; i < kMxBlock; ++i) load_some(x + (k + i) * stride + c, k + i < to.cols ? to.rows - c : 0, v[i]);
+            for (int i = 0; i < kMxBlock; ++i) raw[i] = *reinterpret_cast<const Pack<T, kTurnVec>*>(x + (k + i) * stride + c);
+        } else {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-            if (c + j >= to.rows) break;
+            for (int i = 0; i < kMxBlock; ++i)
+                raw[i] = load_some<T, kTurnVec>(x + (k + i) * stride + c, k + i < turned.cols ? turned.rows - c : 0);
+        }
+        const auto value = [&](int i, int j) { return static_cast<float>(raw[i].v[j]); };
+#pragma unroll
+        for (int j = 0; j < kTurnVec; ++j) {
+            if (c + j >= turned.rows) break;
             uint32_t most = 0;
 #pragma unroll
-            for (int i = 0; i < kMxBlock; ++i) most = max(most, magnitude(v[i][j]));
+            for (int i = 0; i < kMxBlock; ++i) most = max(most, magnitude(value(i, j)));
             const uint32_t scale = scale_of(most);
-            Words4 codes;
+            Words4 q;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float w[8];
+            for (int w = 0; w < 4; ++w) {
+                float y[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = v[q * 8 + i][j];
-                codes[q] = static_cast<int>(codes_of(w, scale));
+                for (int i = 0; i < 8; ++i) y[i] = value(w * 8 + i, j);
+                q[w] = static_cast<int>(codes_of(y, scale));
             }
-            *reinterpret_cast<Words4*>(to.codes + (g * to.rows + c + j) * kMxBytes + block * 16) = codes;
-            to.scales[(g * to.rows + c + j) * kMxBlocks + block] = static_cast<uint8_t>(scale);
+            *reinterpret_cast<Words4*>(turned.codes + (g * turned.rows + c + j) * kMxBytes + block * 16) = q;
+            turned.scales[(g * turned.rows + c + j) * kMxBlocks + block] = static_cast<uint8_t>(scale);
+        }
+        if constexpr (kRows) {
+            const int half = at / kMxGroup, byte = at % kMxGroup / 2;
+#pragma unroll
+            for (int i = 0; i < kMxBlock; ++i) {
+                uint32_t most = 0;
+                float y[kTurnVec];
+#pragma unroll
+                for (int j = 0; j < kTurnVec; ++j) {
+                    y[j] = value(i, j);
+                    most = max(most, magnitude(y[j]));
+                }
+                const uint32_t scale = scale_of(most_of_eight(most));
+                codes[half][block * kMxBlock + i][byte / 2] = static_cast<uint16_t>(codes_of(y, scale));
+                if ((lane & 7) == 0) scales[half][block * kMxBlock + i][byte / 16] = static_cast<uint8_t>(scale);
+            }
+            __syncthreads();
+            const int64_t left = rows.rows - g * kMxGroup;
+            const int count = left < kMxGroup ? static_cast<int>(left) : kMxGroup;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t of = c0 / kMxGroup + h;
+                if (of >= rows.groups) break;
+                const int64_t first = of * rows.rows + g * kMxGroup;
+                for (int i = threadIdx.x; i < count * kMxBytes / 16; i += kPackThreads)
+                    reinterpret_cast<Words4*>(rows.codes + first * kMxBytes)[i] = reinterpret_cast<const Words4*>(codes[h])[i];
+                if (static_cast<int>(threadIdx.x) < count)
+                    reinterpret_cast<uint32_t*>(rows.scales + first * kMxBlocks)[threadIdx.x] =
+                        reinterpret_cast<const uint32_t*>(scales[h])[threadIdx.x];
+            }
+            __syncthreads();
         }
     }
 }
 
+// The way back: sixteen lanes a row's group as above, each 16 bytes of out at a time.
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void unpack_kernel(Mx4 from, T* out, int64_t stride) {
-    constexpr int kLines = kPackThreads / kPackLanes;
-    const int64_t lines = from.rows * from.groups;
-    const int lane = threadIdx.x % kPackLanes;
-    for (int64_t line = static_cast<int64_t>(blockIdx.x) * kLines + threadIdx.x / kPackLanes; line < lines;
-         line += static_cast<int64_t>(gridDim.x) * kLines) {
-        const int64_t r = line / from.groups, g = line - r * from.groups, c = g * kMxGroup + lane * 8;
-        if (c >= from.cols) continue;
-        const uint32_t codes = *reinterpret_cast<const uint32_t*>(from.codes + (g * from.rows + r) * kMxBytes + lane * 4);
-        const float by = power_of(from.scales[(g * from.rows + r) * kMxBlocks + lane / 4]);
-        float v[8];
-        const auto two = [&](auto pair, int i) {
-            v[i] = pair[0] * by;
-            v[i + 1] = pair[1] * by;
-        };
-        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0), 0);
-        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1), 2);
-        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 2), 4);
-        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 3), 6);
-        T* p = out + r * stride + c;
-        if (c + 8 <= from.cols) {
-            store_floats(p, v);
-        } else {
+    constexpr int kVec = 16 / sizeof(T), kPieces = 8 / kVec, kRowsAtOnce = kPackThreads / kPackLanes / kPackGroups;
+    using Codes = typename std::conditional<kVec == 8, uint32_t, uint16_t>::type;
+    const int lane = threadIdx.x % kPackLanes, part = threadIdx.x / kPackLanes;
+    const int64_t g = static_cast<int64_t>(blockIdx.x) * kPackGroups + part % kPackGroups;
+    if (g >= from.groups) return;
+    for (int64_t r0 = static_cast<int64_t>(blockIdx.y) * kPackRows + part / kPackGroups; r0 < from.rows;
+         r0 += static_cast<int64_t>(gridDim.y) * kPackRows) {
+        constexpr int kEach = kPackRows / kRowsAtOnce;
+        uint32_t codes[kEach][kPieces], scale[kEach][kPieces];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c + i < from.cols) p[i] = rounded<T>(v[i]);
-        }
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                const int64_t r = r0 + i * kRowsAtOnce < from.rows ? r0 + i * kRowsAtOnce : from.rows - 1;
+                const int v = p * (kPackLanes * kVec) + lane * kVec;  // of the group
+                codes[i][p] = *reinterpret_cast<const Codes*>(from.codes + (g * from.rows + r) * kMxBytes + v / 2);
+                scale[i][p] = from.scales[(g * from.rows + r) * kMxBlocks + v / kMxBlock];
+            }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                const int64_t r = r0 + i * kRowsAtOnce;
+                const int64_t c = g * kMxGroup + p * (kPackLanes * kVec) + lane * kVec;
+                if (r >= from.rows || c >= from.cols) continue;
+                const float by = power_of(scale[i][p]);
+                float v[kVec];
+                const auto two = [&](auto pair, int at) {
+                    v[at] = pair[0] * by;
+                    v[at + 1] = pair[1] * by;
+                };
+                two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i][p], 1.0f, 0), 0);
+                two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i][p], 1.0f, 1), 2);
+                if constexpr (kVec == 8) {
+                    two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i][p], 1.0f, 2), 4);
+                    two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i][p], 1.0f, 3), 6);
+                }
+                T* at = out + r * stride + c;
+                if (c + kVec <= from.cols) {
+                    store_floats(at, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j)
+                        if (c + j < from.cols) at[j] = rounded<T>(v[j]);
+                }
+            }
     }
 }
 
@@ -645,19 +730,20 @@ __global__ __launch_bounds__(64) void join_kernel(int64_t tiles_a, int64_t tiles
 constexpr int64_t kMostGroups = int64_t(1) << 20;
 dim3 grid_of(int64_t n) { return dim3(static_cast<uint32_t>(std::min(n, kMostGroups))); }
 
+dim3 grid_of(int64_t x, int64_t y) {
+    return dim3(static_cast<uint32_t>(x), static_cast<uint32_t>(std::min<int64_t>(y, 65535)));
+}
+
 template <class T>
 hipError_t pack(const Rows& x, const Mx4& packed, const Mx4& turned, hipStream_t stream) {
     const T* at = static_cast<const T*>(x.at);
-    if (packed.codes)
-        if (const hipError_t e = launch(pack_kernel<T>,
-                                        grid_of((packed.rows + kPackRows - 1) / kPackRows *
-                                                ((packed.groups + kPackGroups - 1) / kPackGroups)),
-                                        kPackThreads, stream, at, x.stride, packed))
-            return e;
-    if (!turned.codes) return hipSuccess;
-    return launch(pack_turned_kernel<T>,
-                  grid_of((turned.rows + Turn<T>::kColumns - 1) / Turn<T>::kColumns * turned.groups), kPackThreads,
-                  stream, at, x.stride, turned);
+    if (!turned.codes)
+        return launch(pack_kernel<T>,
+                      grid_of((packed.groups + kPackGroups - 1) / kPackGroups, (packed.rows + kPackRows - 1) / kPackRows),
+                      kPackThreads, stream, at, x.stride, packed);
+    return launch(packed.codes ? pack_turned_kernel<T, true> : pack_turned_kernel<T, false>,
+                  grid_of((turned.rows + kTurnColumns - 1) / kTurnColumns, turned.groups), kPackThreads, stream, at, x.stride,
+                  packed, turned);
 }
 
 }  // namespace
@@ -674,7 +760,7 @@ hipError_t launch_mx4_pack(const Rows& x, int64_t rows, int64_t cols, const Mx4&
 
 hipError_t launch_mx4_unpack(const Mx4& from, const Rows& out, hipStream_t stream) {
     if (from.rows == 0 || from.cols == 0) return hipSuccess;
-    const dim3 grid = grid_of((from.rows * from.groups + kPackThreads / kPackLanes - 1) / (kPackThreads / kPackLanes));
+    const dim3 grid = grid_of((from.groups + kPackGroups - 1) / kPackGroups, (from.rows + kPackRows - 1) / kPackRows);
     switch (out.type) {
         case MICRO_TYPE_F32:
             return launch(unpack_kernel<float>, grid, kPackThreads, stream, from, static_cast<float*>(out.at), out.stride);
