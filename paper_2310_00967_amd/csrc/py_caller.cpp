@@ -228,6 +228,7 @@ PyObject* caller_new(PyTypeObject* type, PyObject* args, PyObject*) {
 struct TableCaller {
     PyObject_HEAD
     decltype(&micro_table_lookup) lookup;
+    decltype(&micro_table_sample) sample;
     micro_table* table;
     int64_t vocab, dim;
     at::ScalarType type;
@@ -271,16 +272,85 @@ PyObject* table_lookup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// TableCaller(lookup, table, vocab, dim, type, device, stream): type is a
+// A number, or a tensor of one value a row, as one of sample's settings.
+template <class Number>
+bool setting(PyObject* from, int device, int64_t rows, at::ScalarType type, Number* number, const void** array) {
+    if (THPVariable_CheckExact(from)) {
+        const at::Tensor& t = THPVariable_Unpack(from);
+        if (!t.is_cuda() || t.get_device() != device || !t.is_contiguous() || t.scalar_type() != type || t.numel() != rows)
+            return false;
+        *array = t.data_ptr();
+        return true;
+    }
+    if constexpr (std::is_same<Number, double>::value) return real(from, number);
+    if (!PyLong_CheckExact(from)) return false;
+    int overflow = 0;
+    *number = PyLong_AsLongLongAndOverflow(from, &overflow);
+    return overflow == 0;
+}
+
+// sample(logits, uniforms, temperature, top_k, top_p, min_p): (ids, logprobs); None and an
+// int as above.
+PyObject* table_sample(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    TableCaller* c = reinterpret_cast<TableCaller*>(self);
+    HANDLE_TH_ERRORS
+    if (n != 6 || !THPVariable_CheckExact(args[0]) || !THPVariable_CheckExact(args[1])) Py_RETURN_NONE;
+    const at::Tensor& logits = THPVariable_Unpack(args[0]);
+    const at::Tensor& uniforms = THPVariable_Unpack(args[1]);
+    const auto plain = [&](const at::Tensor& t) {
+        return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == c->device && t.is_contiguous();
+    };
+    const int64_t rows = uniforms.numel();
+    const auto kind = logits.scalar_type();
+    const int32_t type = kind == at::kFloat ? MICRO_TYPE_F32 : kind == at::kHalf ? MICRO_TYPE_F16
+                         : kind == at::kBFloat16 ? MICRO_TYPE_BF16 : -1;
+    if (!plain(logits) || !plain(uniforms) || type < 0 || uniforms.scalar_type() != at::kFloat || logits.dim() < 1 ||
+        logits.size(-1) != c->vocab || logits.numel() != rows * c->vocab || logits.requires_grad() ||
+        logits._fw_grad(/*level=*/0).defined())
+        Py_RETURN_NONE;
+    micro_sampling s{};
+    const void *temperatures = nullptr, *top_ks = nullptr, *top_ps = nullptr, *min_ps = nullptr;
+    if (!setting(args[2], c->device, rows, at::kFloat, &s.temperature, &temperatures) ||
+        !setting(args[3], c->device, rows, at::kInt, &s.top_k, &top_ks) ||
+        !setting(args[4], c->device, rows, at::kFloat, &s.top_p, &top_ps) ||
+        !setting(args[5], c->device, rows, at::kFloat, &s.min_p, &min_ps))
+        Py_RETURN_NONE;
+    s.temperatures = static_cast<const float*>(temperatures);
+    s.top_ks = static_cast<const int32_t*>(top_ks);
+    s.top_ps = static_cast<const float*>(top_ps);
+    s.min_ps = static_cast<const float*>(min_ps);
+    const c10::Device device(c10::DeviceType::CUDA, static_cast<c10::DeviceIndex>(c->device));
+    if (c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getStream(device).id() != c->stream) Py_RETURN_NONE;
+    at::Tensor ids = at::empty(uniforms.sizes(), uniforms.options().dtype(at::kLong));
+    at::Tensor logprobs = at::empty(uniforms.sizes(), uniforms.options());
+    const void* from = logits.data_ptr();
+    const float* u = static_cast<const float*>(uniforms.data_ptr());
+    void* to = ids.data_ptr();
+    float* p = static_cast<float*>(logprobs.data_ptr());
+    micro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = c->sample(c->table, from, type, c->vocab, rows, u, &s, to, MICRO_IDS_I64, p);
+    Py_END_ALLOW_THREADS
+    if (st != MICRO_OK) return PyLong_FromLong(st);
+    THPObjectPtr first(THPVariable_Wrap(std::move(ids)));
+    if (!first.get()) return nullptr;
+    THPObjectPtr second(THPVariable_Wrap(std::move(logprobs)));
+    if (!second.get()) return nullptr;
+    return PyTuple_Pack(2, first.get(), second.get());
+    END_HANDLE_TH_ERRORS
+}
+
+// TableCaller(lookup, sample, table, vocab, dim, type, device, stream): type is a
 // MICRO_TYPE_*.
 PyObject* table_caller_new(PyTypeObject* type, PyObject* args, PyObject*) {
-    unsigned long long lookup, table;
+    unsigned long long lookup, sample, table;
     long long vocab, dim, stream;
     int value_type, device;
-    if (!PyArg_ParseTuple(args, "KKLLiiL", &lookup, &table, &vocab, &dim, &value_type, &device, &stream)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KKKLLiiL", &lookup, &sample, &table, &vocab, &dim, &value_type, &device, &stream)) return nullptr;
     TableCaller* c = reinterpret_cast<TableCaller*>(type->tp_alloc(type, 0));
     if (!c) return nullptr;
     c->lookup = reinterpret_cast<decltype(c->lookup)>(lookup);
+    c->sample = reinterpret_cast<decltype(c->sample)>(sample);
     c->table = reinterpret_cast<micro_table*>(table);
     c->vocab = vocab;
     c->dim = dim;
@@ -292,9 +362,173 @@ PyObject* table_caller_new(PyTypeObject* type, PyObject* args, PyObject*) {
 
 PyMethodDef table_methods[] = {
     {"lookup", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(table_lookup)), METH_FASTCALL, nullptr},
+    {"sample", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(table_sample)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyTypeObject table_caller_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
+// ---------------------------------------------------------------------------
+// MxCaller: the 4-bit calls in the plain case: contiguous tensors on the device, called
+// on the handle's stream, with outputs of their own.
+struct MxCaller {
+    PyObject_HEAD
+    decltype(&micro_mx4_pack) pack;
+    decltype(&micro_mx4_product) product;
+    decltype(&micro_mx4_linear) linear;
+    micro_mx4* mx;
+    int device;
+    int64_t stream;  // c10's id of the handle's stream
+};
+
+constexpr int64_t kGroup = 128, kGroupBytes = 64, kGroupBlocks = 4;
+
+int32_t type_of(at::ScalarType t) {
+    return t == at::kFloat ? MICRO_TYPE_F32 : t == at::kHalf ? MICRO_TYPE_F16 : t == at::kBFloat16 ? MICRO_TYPE_BF16 : -1;
+}
+
+bool plain_values(const at::Tensor& t, int device) {
+    return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == device && t.is_contiguous() && t.dim() >= 1 &&
+           t.size(-1) > 0 && t.numel() > 0 && !t.requires_grad() && !t._fw_grad(/*level=*/0).defined() &&
+           type_of(t.scalar_type()) >= 0;
+}
+
+bool on_stream(int device, int64_t stream) {
+    const c10::Device d(c10::DeviceType::CUDA, static_cast<c10::DeviceIndex>(device));
+    return c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getStream(d).id() == stream;
+}
+
+struct PackedTensors {
+    at::Tensor codes, scales;
+    micro_mx4_matrix matrix;
+    void make(int64_t rows, int64_t cols, const at::TensorOptions& like) {
+        const int64_t groups = (cols + kGroup - 1) / kGroup;
+        codes = at::empty({groups, rows, kGroupBytes}, like.dtype(at::kByte));
+        scales = at::empty({groups, rows, kGroupBlocks}, like.dtype(at::kByte));
+        matrix = {codes.data_ptr(), scales.data_ptr(), rows, cols};
+    }
+};
+
+// The matrix of a (codes, scales, rows, cols) tuple.
+bool matrix_of(PyObject* t, int device, micro_mx4_matrix* m) {
+    if (!PyTuple_CheckExact(t) || PyTuple_GET_SIZE(t) != 4) return false;
+    PyObject *codes = PyTuple_GET_ITEM(t, 0), *scales = PyTuple_GET_ITEM(t, 1);
+    if (!THPVariable_CheckExact(codes) || !THPVariable_CheckExact(scales)) return false;
+    const at::Tensor &c = THPVariable_Unpack(codes), &s = THPVariable_Unpack(scales);
+    if (!c.is_cuda() || c.get_device() != device) return false;
+    *m = {c.data_ptr(), s.data_ptr(), PyLong_AsLongLong(PyTuple_GET_ITEM(t, 2)), PyLong_AsLongLong(PyTuple_GET_ITEM(t, 3))};
+    return true;
+}
+
+// pack(x, straight, turned): (codes, scales, rows, cols) or None for each of the two;
+// None: not the plain case; an int: the call's status.
+PyObject* mx_pack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    MxCaller* c = reinterpret_cast<MxCaller*>(self);
+    HANDLE_TH_ERRORS
+    if (n != 3 || !THPVariable_CheckExact(args[0])) Py_RETURN_NONE;
+    const at::Tensor& x = THPVariable_Unpack(args[0]);
+    if (!plain_values(x, c->device) || !on_stream(c->device, c->stream)) Py_RETURN_NONE;
+    const int64_t cols = x.size(-1), rows = x.numel() / cols;
+    const bool straight = args[1] == Py_True, turned = args[2] == Py_True;
+    PackedTensors p, t;
+    if (straight) p.make(rows, cols, x.options());
+    if (turned) t.make(cols, rows, x.options());
+    const void* at = x.data_ptr();
+    const int32_t type = type_of(x.scalar_type());
+    micro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = c->pack(c->mx, at, type, cols, rows, cols, straight ? &p.matrix : nullptr, turned ? &t.matrix : nullptr);
+    Py_END_ALLOW_THREADS
+    if (st != MICRO_OK) return PyLong_FromLong(st);
+    const auto wrap = [](bool made, PackedTensors& m) -> PyObject* {
+        if (!made) return Py_NewRef(Py_None);
+        THPObjectPtr codes(THPVariable_Wrap(std::move(m.codes)));
+        THPObjectPtr scales(codes.get() ? THPVariable_Wrap(std::move(m.scales)) : nullptr);
+        if (!scales.get()) return nullptr;
+        return Py_BuildValue("(OOLL)", codes.get(), scales.get(), static_cast<long long>(m.matrix.rows),
+                             static_cast<long long>(m.matrix.cols));
+    };
+    THPObjectPtr first(wrap(straight, p));
+    if (!first.get()) return nullptr;
+    THPObjectPtr second(wrap(turned, t));
+    if (!second.get()) return nullptr;
+    return PyTuple_Pack(2, first.get(), second.get());
+    END_HANDLE_TH_ERRORS
+}
+
+// product(a, b, type): a b^T of two tuples as above into a tensor of its own, of a
+// MICRO_TYPE_*; None and an int as above.
+PyObject* mx_product(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    MxCaller* c = reinterpret_cast<MxCaller*>(self);
+    HANDLE_TH_ERRORS
+    micro_mx4_matrix a, b;
+    if (n != 3 || !matrix_of(args[0], c->device, &a) || !matrix_of(args[1], c->device, &b) || !on_stream(c->device, c->stream))
+        Py_RETURN_NONE;
+    const long type = PyLong_AsLong(args[2]);
+    if (a.cols != b.cols || type < 0 || type > MICRO_TYPE_BF16) Py_RETURN_NONE;
+    const at::ScalarType kind = type == MICRO_TYPE_F32 ? at::kFloat : type == MICRO_TYPE_F16 ? at::kHalf : at::kBFloat16;
+    at::Tensor out = at::empty({a.rows, b.rows}, THPVariable_Unpack(PyTuple_GET_ITEM(args[0], 0)).options().dtype(kind));
+    void* to = out.data_ptr();
+    micro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = c->product(c->mx, &a, &b, 0, to, static_cast<int32_t>(type), b.rows);
+    Py_END_ALLOW_THREADS
+    if (st != MICRO_OK) return PyLong_FromLong(st);
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// linear(x, b, type): x b^T, x packed on the way.
+PyObject* mx_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    MxCaller* c = reinterpret_cast<MxCaller*>(self);
+    HANDLE_TH_ERRORS
+    micro_mx4_matrix b;
+    if (n != 3 || !THPVariable_CheckExact(args[0]) || !matrix_of(args[1], c->device, &b)) Py_RETURN_NONE;
+    const at::Tensor& x = THPVariable_Unpack(args[0]);
+    if (!plain_values(x, c->device) || x.size(-1) != b.cols || !on_stream(c->device, c->stream)) Py_RETURN_NONE;
+    const long type = PyLong_AsLong(args[2]);
+    if (type < 0 || type > MICRO_TYPE_BF16) Py_RETURN_NONE;
+    const at::ScalarType kind = type == MICRO_TYPE_F32 ? at::kFloat : type == MICRO_TYPE_F16 ? at::kHalf : at::kBFloat16;
+    PackedTensors p;
+    p.make(x.numel() / b.cols, b.cols, x.options());
+    c10::SmallVector<int64_t, 6> shape(x.sizes().begin(), x.sizes().end());
+    shape.back() = b.rows;
+    at::Tensor out = at::empty(shape, x.options().dtype(kind));
+    const void* from = x.data_ptr();
+    void* to = out.data_ptr();
+    const int32_t x_type = type_of(x.scalar_type());
+    micro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = c->linear(c->mx, from, x_type, b.cols, &p.matrix, &b, 0, to, static_cast<int32_t>(type), b.rows);
+    Py_END_ALLOW_THREADS
+    if (st != MICRO_OK) return PyLong_FromLong(st);
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// MxCaller(pack, product, linear, mx, device, stream).
+PyObject* mx_caller_new(PyTypeObject* type, PyObject* args, PyObject*) {
+    unsigned long long pack, product, linear, mx;
+    int device;
+    long long stream;
+    if (!PyArg_ParseTuple(args, "KKKKiL", &pack, &product, &linear, &mx, &device, &stream)) return nullptr;
+    MxCaller* c = reinterpret_cast<MxCaller*>(type->tp_alloc(type, 0));
+    if (!c) return nullptr;
+    c->pack = reinterpret_cast<decltype(c->pack)>(pack);
+    c->product = reinterpret_cast<decltype(c->product)>(product);
+    c->linear = reinterpret_cast<decltype(c->linear)>(linear);
+    c->mx = reinterpret_cast<micro_mx4*>(mx);
+    c->device = device;
+    c->stream = stream;
+    return reinterpret_cast<PyObject*>(c);
+}
+
+PyMethodDef mx_methods[] = {
+    {"pack", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(mx_pack)), METH_FASTCALL, nullptr},
+    {"product", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(mx_product)), METH_FASTCALL, nullptr},
+    {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(mx_linear)), METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr}};
+
+PyTypeObject mx_caller_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
 PyMethodDef caller_methods[] = {
     {"step", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(caller_step)), METH_FASTCALL, nullptr},
@@ -321,10 +555,17 @@ PyMODINIT_FUNC PyInit__caller() {
     table_caller_type.tp_methods = table_methods;
     table_caller_type.tp_new = table_caller_new;
     if (PyType_Ready(&table_caller_type) < 0) return nullptr;
+    mx_caller_type.tp_name = "paper_2310_00967_amd._caller.MxCaller";
+    mx_caller_type.tp_basicsize = sizeof(MxCaller);
+    mx_caller_type.tp_flags = Py_TPFLAGS_DEFAULT;
+    mx_caller_type.tp_methods = mx_methods;
+    mx_caller_type.tp_new = mx_caller_new;
+    if (PyType_Ready(&mx_caller_type) < 0) return nullptr;
     PyObject* m = PyModule_Create(&module);
     if (!m) return nullptr;
     if (PyModule_AddObject(m, "Caller", Py_NewRef(reinterpret_cast<PyObject*>(&caller_type))) < 0 ||
-        PyModule_AddObject(m, "TableCaller", Py_NewRef(reinterpret_cast<PyObject*>(&table_caller_type))) < 0) {
+        PyModule_AddObject(m, "TableCaller", Py_NewRef(reinterpret_cast<PyObject*>(&table_caller_type))) < 0 ||
+        PyModule_AddObject(m, "MxCaller", Py_NewRef(reinterpret_cast<PyObject*>(&mx_caller_type))) < 0) {
         Py_DECREF(m);
         return nullptr;
     }

@@ -219,9 +219,9 @@ class TokenTable(_Enqueued):
         self._loss_fn, self._loss_grad_fn = lib.micro_table_loss, lib.micro_table_loss_grad
         self._sample_fn = lib.micro_table_sample
         self._value_types = types
-        # the native marshalling of the lookup's plain case
+        # the native marshalling of the plain case of lookup and sample
         self._caller = _lib.load_caller("TableCaller")(
-            ctypes.cast(self._lookup_fn, ctypes.c_void_p).value, self._handle.value, self.vocab, self.dim,
+            *(ctypes.cast(fn, ctypes.c_void_p).value for fn in (self._lookup_fn, self._sample_fn)), self._handle.value, self.vocab, self.dim,
             types[self.dtype], self._index, self.stream.stream_id)
         self._ids_types = {torch.int32: _lib.MICRO_IDS_I32, torch.int64: _lib.MICRO_IDS_I64}
 
@@ -375,6 +375,12 @@ class TokenTable(_Enqueued):
         temperature 0 takes the first largest logit.  Logits of -inf or NaN have no
         part; a row without any other gives -1 and NaN."""
         handle = self._open()
+        if out is None:
+            done = self._caller.sample(logits, uniforms, temperature, top_k, top_p, min_p)
+            if isinstance(done, tuple):
+                return done
+            if done is not None:
+                _lib.check(done)
         foreign = self._foreign()
         torch = self._torch
         if not isinstance(uniforms, self._tensor) or uniforms.dtype is not torch.float32 or not uniforms.is_cuda \

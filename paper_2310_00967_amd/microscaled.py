@@ -19,7 +19,7 @@ class PackedMatrix:
     4), the exponents of 2 plus 127; groups = cols / 128, rounded up.  Values behind
     cols are 0.  Both are contiguous and may be saved and loaded as they are."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "_c")
+    __slots__ = ("codes", "scales", "rows", "cols", "_parts")
 
     def __init__(self, codes, scales, rows, cols):
         import torch
@@ -36,7 +36,18 @@ class PackedMatrix:
         if codes.device != scales.device:
             raise TypeError("codes and scales must be on one device")
         self.codes, self.scales = codes, scales
-        self._c = _lib.micro_mx4_matrix(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols)
+        self._parts = (codes, scales, self.rows, self.cols)
+
+    @classmethod
+    def _made(cls, parts):
+        """Of a call's own outputs."""
+        m = cls.__new__(cls)
+        m.codes, m.scales, m.rows, m.cols = m._parts = parts
+        return m
+
+    @property
+    def _c(self):
+        return _lib.micro_mx4_matrix(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
 
     @property
     def device(self):
@@ -71,9 +82,14 @@ class Microscaled(_Enqueued):
         self._types = _value_types()
         self._pack_fn, self._unpack_fn = lib.micro_mx4_pack, lib.micro_mx4_unpack
         self._product_fn, self._linear_fn = lib.micro_mx4_product, lib.micro_mx4_linear
+        # the native marshalling of the plain case of pack, product and linear
+        self._caller = _lib.load_caller("MxCaller")(
+            *(ctypes.cast(fn, ctypes.c_void_p).value for fn in (self._pack_fn, self._product_fn, self._linear_fn)),
+            self._handle.value, self._index, self.stream.stream_id)
 
     def close(self):
         if getattr(self, "_handle", None) is not None:
+            self._caller = None
             _lib.micro_mx4_free(self._handle)
             self._handle = None
 
@@ -95,7 +111,7 @@ class Microscaled(_Enqueued):
     def _packed(self, m, name):
         if not isinstance(m, PackedMatrix) or m.codes.get_device() != self._index:
             raise TypeError(f"{name} must be a PackedMatrix on {self.device}")
-        return ctypes.byref(m._c)
+        return m._c
 
     def _new(self, rows, cols, foreign):
         groups = -(-cols // GROUP)
@@ -112,12 +128,18 @@ class Microscaled(_Enqueued):
 
     def _pack(self, x, straight, transposed):
         handle = self._open()
+        done = self._caller.pack(x, straight, transposed)
+        if isinstance(done, tuple):
+            return (None if done[0] is None else PackedMatrix._made(done[0]),
+                    None if done[1] is None else PackedMatrix._made(done[1]))
+        if done is not None:
+            _lib.check(done)
         foreign = self._foreign()
         at, stride, rows, cols = self._values(x, "x")
         q = self._new(rows, cols, foreign) if straight else None
         t = self._new(cols, rows, foreign) if transposed else None
-        _lib.check(self._pack_fn(handle, at, self._types[x.dtype], stride, rows, cols, ctypes.byref(q._c) if q else None,
-                                 ctypes.byref(t._c) if t else None))
+        _lib.check(self._pack_fn(handle, at, self._types[x.dtype], stride, rows, cols, q._c if q else None,
+                                 t._c if t else None))
         if foreign:
             self._kept(x)
         return q, t
@@ -125,7 +147,7 @@ class Microscaled(_Enqueued):
     def pack(self, x, transposed=False):
         """x's rows in 4 bits; transposed: those of its transpose, in blocks along
         x's columns."""
-        return self._pack(x, not transposed, transposed)[1 if transposed else 0]
+        return self._pack(x, not transposed, bool(transposed))[1 if transposed else 0]
 
     def pack_both(self, x):
         """(pack(x), pack(x, transposed=True)) from one read of x."""
@@ -161,6 +183,12 @@ class Microscaled(_Enqueued):
         """a b^T of two packed matrices with rows of one length (dtype: float32);
         accumulate adds to the given out."""
         handle = self._open()
+        if out is None and not accumulate and a.__class__ is b.__class__ is PackedMatrix:
+            done = self._caller.product(a._parts, b._parts, self._types.get(dtype or self._torch.float32, -1))
+            if isinstance(done, self._tensor):
+                return done
+            if done is not None:
+                _lib.check(done)
         foreign = self._foreign()
         ca, cb = self._packed(a, "a"), self._packed(b, "b")
         if accumulate and out is None:
@@ -174,6 +202,12 @@ class Microscaled(_Enqueued):
     def linear(self, x, weight, dtype=None, out=None, accumulate=False):
         """x weight^T, x packed on the way (dtype: x's own)."""
         handle = self._open()
+        if out is None and not accumulate and weight.__class__ is PackedMatrix:
+            done = self._caller.linear(x, weight._parts, self._types.get(dtype or getattr(x, "dtype", None), -1))
+            if isinstance(done, self._tensor):
+                return done
+            if done is not None:
+                _lib.check(done)
         foreign = self._foreign()
         cw = self._packed(weight, "weight")
         at, stride, rows, cols = self._values(x, "x")
@@ -183,7 +217,7 @@ class Microscaled(_Enqueued):
             raise ValueError("accumulate needs the out to add to")
         out, to, out_stride = self._out(out, dtype, x.dtype, (*x.shape[:-1], weight.rows), rows, foreign)
         q = self._new(rows, cols, foreign)
-        _lib.check(self._linear_fn(handle, at, self._types[x.dtype], stride, ctypes.byref(q._c), cw,
+        _lib.check(self._linear_fn(handle, at, self._types[x.dtype], stride, q._c, cw,
                                    1 if accumulate else 0, to, self._types[out.dtype], out_stride))
         if foreign:
             self._kept(x, weight, out)
