@@ -151,9 +151,16 @@ __global__ __launch_bounds__(kPackThreads) void pack_turned_kernel(const T* x, i
     for (int64_t g = blockIdx.y; g < turned.groups; g += gridDim.y) {
         const int64_t k = g * kMxGroup + block * kMxBlock;
         Pack<T, kTurnVec> raw[kMxBlock];
-        if (c0 + kTurnColumns <= turned.rows && (g + 1) * kMxGroup <= turned.cols) {  // the loads go out together
+        if (turned.rows % kTurnVec == 0) {
+            // from the nearest place in x, all at once; what lies outside is 0
+            const T* from = x + (c < turned.rows ? c : turned.rows - kTurnVec);
 #pragma unroll
-            for (int i = 0; i < kMxBlock; ++i) raw[i] = *reinterpret_cast<const Pack<T, kTurnVec>*>(x + (k + i) * stride + c);
+            for (int i = 0; i < kMxBlock; ++i)
+                raw[i] = *reinterpret_cast<const Pack<T, kTurnVec>*>(from + (k + i < turned.cols ? k + i : turned.cols - 1) * stride);
+            if (c0 + kTurnColumns > turned.rows || (g + 1) * kMxGroup > turned.cols)
+#pragma unroll
+                for (int i = 0; i < kMxBlock; ++i)
+                    if (c >= turned.rows || k + i >= turned.cols) raw[i] = Pack<T, kTurnVec>{};
         } else {
 #pragma unroll
             for (int i = 0; i < kMxBlock; ++i)

@@ -373,6 +373,7 @@ PyTypeObject table_caller_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 struct MxCaller {
     PyObject_HEAD
     decltype(&micro_mx4_pack) pack;
+    decltype(&micro_mx4_unpack) unpack;
     decltype(&micro_mx4_product) product;
     decltype(&micro_mx4_linear) linear;
     micro_mx4* mx;
@@ -455,6 +456,30 @@ PyObject* mx_pack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+at::ScalarType scalar_of(long type) {
+    return type == MICRO_TYPE_F32 ? at::kFloat : type == MICRO_TYPE_F16 ? at::kHalf : at::kBFloat16;
+}
+
+// unpack(m, type): the values of a tuple as above in a tensor of its own, of a
+// MICRO_TYPE_*; None and an int as above.
+PyObject* mx_unpack(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    MxCaller* c = reinterpret_cast<MxCaller*>(self);
+    HANDLE_TH_ERRORS
+    micro_mx4_matrix m;
+    if (n != 2 || !matrix_of(args[0], c->device, &m) || !on_stream(c->device, c->stream)) Py_RETURN_NONE;
+    const long type = PyLong_AsLong(args[1]);
+    if (type < 0 || type > MICRO_TYPE_BF16) Py_RETURN_NONE;
+    at::Tensor out = at::empty({m.rows, m.cols}, THPVariable_Unpack(PyTuple_GET_ITEM(args[0], 0)).options().dtype(scalar_of(type)));
+    void* to = out.data_ptr();
+    micro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = c->unpack(c->mx, &m, to, static_cast<int32_t>(type), m.cols);
+    Py_END_ALLOW_THREADS
+    if (st != MICRO_OK) return PyLong_FromLong(st);
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
 // product(a, b, type): a b^T of two tuples as above into a tensor of its own, of a
 // MICRO_TYPE_*; None and an int as above.
 PyObject* mx_product(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -465,8 +490,7 @@ PyObject* mx_product(PyObject* self, PyObject* const* args, Py_ssize_t n) {
         Py_RETURN_NONE;
     const long type = PyLong_AsLong(args[2]);
     if (a.cols != b.cols || type < 0 || type > MICRO_TYPE_BF16) Py_RETURN_NONE;
-    const at::ScalarType kind = type == MICRO_TYPE_F32 ? at::kFloat : type == MICRO_TYPE_F16 ? at::kHalf : at::kBFloat16;
-    at::Tensor out = at::empty({a.rows, b.rows}, THPVariable_Unpack(PyTuple_GET_ITEM(args[0], 0)).options().dtype(kind));
+    at::Tensor out = at::empty({a.rows, b.rows}, THPVariable_Unpack(PyTuple_GET_ITEM(args[0], 0)).options().dtype(scalar_of(type)));
     void* to = out.data_ptr();
     micro_status st;
     Py_BEGIN_ALLOW_THREADS
@@ -487,12 +511,11 @@ PyObject* mx_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     if (!plain_values(x, c->device) || x.size(-1) != b.cols || !on_stream(c->device, c->stream)) Py_RETURN_NONE;
     const long type = PyLong_AsLong(args[2]);
     if (type < 0 || type > MICRO_TYPE_BF16) Py_RETURN_NONE;
-    const at::ScalarType kind = type == MICRO_TYPE_F32 ? at::kFloat : type == MICRO_TYPE_F16 ? at::kHalf : at::kBFloat16;
     PackedTensors p;
     p.make(x.numel() / b.cols, b.cols, x.options());
     c10::SmallVector<int64_t, 6> shape(x.sizes().begin(), x.sizes().end());
     shape.back() = b.rows;
-    at::Tensor out = at::empty(shape, x.options().dtype(kind));
+    at::Tensor out = at::empty(shape, x.options().dtype(scalar_of(type)));
     const void* from = x.data_ptr();
     void* to = out.data_ptr();
     const int32_t x_type = type_of(x.scalar_type());
@@ -505,15 +528,16 @@ PyObject* mx_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// MxCaller(pack, product, linear, mx, device, stream).
+// MxCaller(pack, unpack, product, linear, mx, device, stream).
 PyObject* mx_caller_new(PyTypeObject* type, PyObject* args, PyObject*) {
-    unsigned long long pack, product, linear, mx;
+    unsigned long long pack, unpack, product, linear, mx;
     int device;
     long long stream;
-    if (!PyArg_ParseTuple(args, "KKKKiL", &pack, &product, &linear, &mx, &device, &stream)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KKKKKiL", &pack, &unpack, &product, &linear, &mx, &device, &stream)) return nullptr;
     MxCaller* c = reinterpret_cast<MxCaller*>(type->tp_alloc(type, 0));
     if (!c) return nullptr;
     c->pack = reinterpret_cast<decltype(c->pack)>(pack);
+    c->unpack = reinterpret_cast<decltype(c->unpack)>(unpack);
     c->product = reinterpret_cast<decltype(c->product)>(product);
     c->linear = reinterpret_cast<decltype(c->linear)>(linear);
     c->mx = reinterpret_cast<micro_mx4*>(mx);
@@ -524,6 +548,7 @@ PyObject* mx_caller_new(PyTypeObject* type, PyObject* args, PyObject*) {
 
 PyMethodDef mx_methods[] = {
     {"pack", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(mx_pack)), METH_FASTCALL, nullptr},
+    {"unpack", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(mx_unpack)), METH_FASTCALL, nullptr},
     {"product", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(mx_product)), METH_FASTCALL, nullptr},
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(mx_linear)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

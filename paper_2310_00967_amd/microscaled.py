@@ -82,9 +82,9 @@ class Microscaled(_Enqueued):
         self._types = _value_types()
         self._pack_fn, self._unpack_fn = lib.micro_mx4_pack, lib.micro_mx4_unpack
         self._product_fn, self._linear_fn = lib.micro_mx4_product, lib.micro_mx4_linear
-        # the native marshalling of the plain case of pack, product and linear
+        # the native marshalling of the plain case of these
         self._caller = _lib.load_caller("MxCaller")(
-            *(ctypes.cast(fn, ctypes.c_void_p).value for fn in (self._pack_fn, self._product_fn, self._linear_fn)),
+            *(ctypes.cast(fn, ctypes.c_void_p).value for fn in (self._pack_fn, self._unpack_fn, self._product_fn, self._linear_fn)),
             self._handle.value, self._index, self.stream.stream_id)
 
     def close(self):
@@ -156,6 +156,12 @@ class Microscaled(_Enqueued):
     def unpack(self, packed, dtype=None, out=None):
         """The values that a packed matrix stands for (dtype: float32)."""
         handle = self._open()
+        if out is None and packed.__class__ is PackedMatrix:
+            done = self._caller.unpack(packed._parts, self._types.get(dtype or self._torch.float32, -1))
+            if isinstance(done, self._tensor):
+                return done
+            if done is not None:
+                _lib.check(done)
         foreign = self._foreign()
         m = self._packed(packed, "packed")
         out, at, stride = self._out(out, dtype, self._torch.float32, (packed.rows, packed.cols), packed.rows, foreign)
