@@ -9,11 +9,13 @@ sparsified gradients, from token ids to the sparse model update:
     sp.ef_step(flat * rate, residual, ...)              the worker's sparsified step
     sp.sparse_update(params, idx, val, world)           the model update
 
+    table.sample(mx.linear(hidden, packed table))       and its answers, from weights in 4 bits
+
 The weights of the forward pass are bfloat16 copies of one flat binary32
 vector, which the updates go to.  The data is a synthetic chain: a token's
 successor is a fixed random one nine times out of ten, else any.
 
-    python examples/tied_language_model.py [--steps 200] [--vocab 2000] [--dim 128]
+    python examples/tied_language_model.py [--steps 200] [--vocab 2000] [--dim 128] [--answer 16]
 """
 import argparse
 import math
@@ -72,9 +74,35 @@ def batches(vocab, tokens, seed, device="cuda"):
         yield x, torch.where(keep, successor[x], any_token)
 
 
-def train(vocab=2000, dim=128, tokens=4096, steps=200, rate=100.0, max_norm=0.05, density=0.05, seed=0, report=None):
-    """Trains and returns the losses of every step."""
-    model = TiedLanguageModel(vocab, dim, tokens, seed)
+class Answers:
+    """Continuations of a trained model, whose weights are packed to 4 bits."""
+
+    def __init__(self, model):
+        self.model, self.mx = model, micro.Microscaled()
+        self.weight = self.mx.pack(model.weight)
+        self.mix = self.mx.pack(model.mix, transposed=True)  # rows @ mix is rows (mix^T)^T
+
+    def logits(self, tokens):
+        rows = self.model.table.lookup(self.model.weight, tokens)
+        hidden = self.mx.linear(rows, self.mix)
+        return self.mx.linear(hidden, self.weight, dtype=torch.float32)
+
+    def continued(self, tokens, length, seed=0, **settings):
+        """Tokens (one a continuation) followed by `length` drawn ones: int64, (length +
+        1, continuations).  settings: those of TokenTable.sample."""
+        gen = torch.Generator(device=tokens.device).manual_seed(seed)
+        out = [tokens]
+        for _ in range(length):
+            u = torch.rand(tokens.numel(), generator=gen, device=tokens.device)
+            ids, _ = self.model.table.sample(self.logits(out[-1]), u, **settings)
+            out.append(ids)
+        return torch.stack(out)
+
+
+def train(vocab=2000, dim=128, tokens=4096, steps=200, rate=100.0, max_norm=0.05, density=0.05, seed=0, report=None, model=None):
+    """Trains (a model of the given sizes, or a new one) and returns the losses of every
+    step."""
+    model = model if model is not None else TiedLanguageModel(vocab, dim, tokens, seed)
     n = model.params.numel()
     sp = micro.Sparsifier(n)
     flat, residual = torch.empty(n, device="cuda"), torch.zeros(n, device="cuda")
@@ -103,5 +131,11 @@ if __name__ == "__main__":
     ap.add_argument("--vocab", type=int, default=2000)
     ap.add_argument("--dim", type=int, default=128)
     ap.add_argument("--tokens", type=int, default=4096)
+    ap.add_argument("--answer", type=int, default=16, help="tokens to continue with after the training")
     a = ap.parse_args()
-    train(vocab=a.vocab, dim=a.dim, tokens=a.tokens, steps=a.steps, report=max(1, a.steps // 10))
+    trained = TiedLanguageModel(a.vocab, a.dim, a.tokens)
+    train(vocab=a.vocab, dim=a.dim, tokens=a.tokens, steps=a.steps, report=max(1, a.steps // 10), model=trained)
+    if a.answer > 0:
+        starts = torch.arange(4, device="cuda")
+        for run in Answers(trained).continued(starts, a.answer, temperature=0.8, top_k=50, top_p=0.95).t().tolist():
+            print(" ".join(map(str, run)))
