@@ -62,12 +62,9 @@ micro_status check_product(const micro_mx4_matrix* a, const micro_mx4_matrix* b,
     return check_values(out, type, stride, a->rows, b->rows);
 }
 
-micro_status run_product(micro_mx4* mx, const micro_mx4_matrix* a, const micro_mx4_matrix* b, int32_t accumulate,
-                         void* out, int32_t type, int64_t stride) {
-    return report_hip(launch_mx4_product({matrix_of(*a), matrix_of(*b), {out, stride, type}, accumulate != 0,
-                                          mx->compute_units, mx->parts},
-                                         mx->stream),
-                      "4-bit product launch");
+Mx4Product product_of(const micro_mx4* mx, const micro_mx4_matrix* a, const micro_mx4_matrix* b, int32_t accumulate,
+                      void* out, int32_t type, int64_t stride) {
+    return {matrix_of(*a), matrix_of(*b), {out, stride, type}, accumulate != 0, mx->compute_units, mx->parts};
 }
 
 }  // namespace
@@ -145,7 +142,7 @@ micro_status micro_mx4_product(micro_mx4* mx, const micro_mx4_matrix* a, const m
                               {values_of(out, type, stride, a->rows, b->rows), true}};
     if (micro_status st = check_apart(regions)) return st;
     CallDevice scope(mx->device);
-    return run_product(mx, a, b, accumulate, out, type, stride);
+    return report_hip(launch_mx4_product(product_of(mx, a, b, accumulate, out, type, stride), mx->stream), "4-bit product launch");
 }
 
 micro_status micro_mx4_linear(micro_mx4* mx, const void* x, int32_t x_type, int64_t x_stride, const micro_mx4_matrix* a,
@@ -158,10 +155,9 @@ micro_status micro_mx4_linear(micro_mx4* mx, const void* x, int32_t x_type, int6
                               {values_of(out, type, stride, a->rows, b->rows), true}};
     if (micro_status st = check_apart(regions)) return st;
     CallDevice scope(mx->device);
-    if (const hipError_t e = launch_mx4_pack({const_cast<void*>(x), x_stride, x_type}, a->rows, a->cols, matrix_of(*a),
-                                             Mx4{}, mx->stream))
-        return report_hip(e, "4-bit packing launch");
-    return run_product(mx, a, b, accumulate, out, type, stride);
+    return report_hip(launch_mx4_linear({const_cast<void*>(x), x_stride, x_type},
+                                        product_of(mx, a, b, accumulate, out, type, stride), mx->stream),
+                      "4-bit product launch");
 }
 
 void micro_mx4_free(micro_mx4* mx) {

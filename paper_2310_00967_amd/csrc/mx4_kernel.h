@@ -35,5 +35,7 @@ struct Mx4Product {
 };
 constexpr int64_t kMxParts = 256 * 256;
 hipError_t launch_mx4_product(const Mx4Product& call, hipStream_t stream);
+// The same of x, whose packed form goes into call.a if anywhere.
+hipError_t launch_mx4_linear(const Rows& x, const Mx4Product& call, hipStream_t stream);
 
 }  // namespace micro

@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kPackThreads) void pack_turned_kernel(const T* x, i
 
 // The way back: sixteen lanes a row's group as above, each 16 bytes of out at a time, a row
 // after the other, so that workgroups in their order write memory in its order: 50257 x
-// 2048 bfloat16 values in 49 us (5.4 TB/s), by workgroups of 8 rows and 8 groups in 68.
+// 2048 bfloat16 values in 56 us (4.7 TB/s), by workgroups of 8 rows and 8 groups in 68.
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void unpack_kernel(Mx4 from, T* out, int64_t stride) {
     constexpr int kVec = 16 / sizeof(T), kPieces = 8 / kVec, kLines = kPackThreads / kPackLanes;
@@ -286,55 +286,135 @@ struct Side {
     }
 };
 
-// A tile of 32 x 32 a workgroup, whose four wavefronts take every fourth group
-// and add their sums in shared memory.
-constexpr int kTile = 32, kFewWaves = 4, kPadded = kTile + 4;
+// A tile of 32 x 32 a workgroup, whose four wavefronts take every fourth group, two at a
+// time, and add their sums in shared memory.  Bound by one read of b: 1 x 2048 x 50257 in
+// 13.8 us (4.0 TB/s of 55 MB from memory), 32 rows in 18.2; one group at a time 14.6 and
+// 21.5, four 14.0 and 17.6 but 7.5 for 6.2 at 1 x 1024 x 30522.
+constexpr int kTile = 32, kFewWaves = 4, kFewAhead = 2, kPadded = kTile + 4;
+struct FewOut {
+    void* at;
+    int64_t stride, rows, columns;
+    bool accumulate;
+};
+using FewSums = float[kFewWaves][kTile][kPadded];
+
 template <class T>
-__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(Mx4 a, Mx4 b, T* out, int64_t stride, bool accumulate) {
-    __shared__ __attribute__((aligned(16))) float sums[kFewWaves][kTile][kPadded];
-    const int64_t down = (a.rows + kTile - 1) / kTile, tiles = down * ((b.rows + kTile - 1) / kTile);
+__device__ __forceinline__ void finish_few(FewSums& sums, const Acc& acc, const FewOut& out, int64_t i0, int64_t j0) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(&sums[wave][lane & 31][q * 8 + half * 4]) =
+            make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+    __syncthreads();
+    const int64_t i = i0 + threadIdx.x / 8, j = j0 + threadIdx.x % 8 * 4;
+    if (i >= out.rows || j >= out.columns) return;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += sums[w][threadIdx.x / 8][threadIdx.x % 8 * 4 + q];
+    T* p = static_cast<T*>(out.at) + i * out.stride + j;
+    if (j + 4 <= out.columns) {
+        if (out.accumulate) {
+            float old[4];
+            load_floats(p, old);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] += old[q];
+        }
+        store_floats(p, v);
+    } else {
+        for (int q = 0; q < 4; ++q)
+            if (j + q < out.columns) p[q] = rounded<T>(out.accumulate ? v[q] + static_cast<float>(p[q]) : v[q]);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(Mx4 a, Mx4 b, FewOut out) {
+    __shared__ __attribute__((aligned(16))) FewSums sums;
+    const int64_t down = (a.rows + kTile - 1) / kTile, tiles = down * ((b.rows + kTile - 1) / kTile);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t i0 = tile % down * kTile, j0 = tile / down * kTile;
         const Side sa(a, i0 + (lane & 31), half), sb(b, j0 + (lane & 31), half);
         Acc acc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-        for (int64_t g = wave; g < a.groups; g += kFewWaves) {
-            Words4 ca[2], cb[2];
-            uint32_t xa, xb;
-            sb.load(g, cb, xb);
-            sa.load(g, ca, xa);
-            acc = mma<0>(cb[0], xb, ca[0], xa, acc);
-            acc = mma<1>(cb[1], xb, ca[1], xa, acc);
+        for (int64_t g = wave; g < a.groups; g += kFewWaves * kFewAhead) {
+            Words4 ca[kFewAhead][2], cb[kFewAhead][2];
+            uint32_t xa[kFewAhead], xb[kFewAhead];
+#pragma unroll
+            for (int i = 0; i < kFewAhead; ++i)
+                if (g + i * kFewWaves < a.groups) {
+                    sb.load(g + i * kFewWaves, cb[i], xb[i]);
+                    sa.load(g + i * kFewWaves, ca[i], xa[i]);
+                }
+#pragma unroll
+            for (int i = 0; i < kFewAhead; ++i)
+                if (g + i * kFewWaves < a.groups) {
+                    acc = mma<0>(cb[i][0], xb[i], ca[i][0], xa[i], acc);
+                    acc = mma<1>(cb[i][1], xb[i], ca[i][1], xa[i], acc);
+                }
         }
-        __syncthreads();
+        finish_few<T>(sums, acc, out, i0, j0);
+    }
+}
+
+// The same for up to 32 rows of x that have kOwnValues values, in whole groups, at most:
+// each workgroup packs them for itself, under its first loads of b, which takes less than
+// a launch that packs them once (a workgroup's share is 32 values a thread).
+constexpr int kOwnValues = 8192;
+template <class X, class T>
+__global__ __launch_bounds__(64 * kFewWaves) void few_linear_kernel(const X* x, int64_t stride, int rows, Mx4 b, FewOut out) {
+    __shared__ __attribute__((aligned(16))) FewSums sums;
+    __shared__ __attribute__((aligned(16))) char codes[kOwnValues / 2];
+    __shared__ __attribute__((aligned(16))) uint8_t scales[kOwnValues / kMxBlock];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int64_t j0 = static_cast<int64_t>(blockIdx.x) * kTile;
+    const int groups = static_cast<int>(b.groups), units = groups * kPackLanes;  // of eight values, of a row
+    const Side sb(b, j0 + (lane & 31), half);
+    Words4 cb[kFewAhead][2];
+    uint32_t xb[kFewAhead];
+    const auto load = [&](int g) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<float4*>(&sums[wave][lane & 31][q * 8 + half * 4]) =
-                make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
-        __syncthreads();
-        const int64_t i = i0 + threadIdx.x / 8, j = j0 + threadIdx.x % 8 * 4;
-        if (i >= a.rows || j >= b.rows) continue;
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < kFewAhead; ++i)
+            if (g + i * kFewWaves < groups) sb.load(g + i * kFewWaves, cb[i], xb[i]);
+    };
+    load(wave);
+    for (int u = threadIdx.x; u < rows * units; u += 64 * kFewWaves) {
+        const int r = u / units, c = (u - r * units) * 8;
+        const Pack<X, 8> raw = load_some<X, 8>(x + r * stride + c, b.cols - c);
+        float v[8];
+        uint32_t most = 0;
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w)
+        for (int j = 0; j < 8; ++j) {
+            v[j] = static_cast<float>(raw.v[j]);
+            most = max(most, magnitude(v[j]));
+        }
+        const uint32_t scale = scale_of(most_of_quad(most));
+        *reinterpret_cast<uint32_t*>(codes + u * 4) = codes_of(v, scale);
+        if ((u & 3) == 0) scales[u / 4] = static_cast<uint8_t>(scale);
+    }
+    __syncthreads();
+    const int row = (lane & 31) < rows ? lane & 31 : rows - 1;
+    const char* own = codes + row * groups * kMxBytes + half * 32;
+    const uint8_t* own_scales = scales + row * groups * kMxBlocks + half * 2;
+    Acc acc;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] += sums[w][threadIdx.x / 8][threadIdx.x % 8 * 4 + q];
-        T* p = out + i * stride + j;
-        if (j + 4 <= b.rows) {
-            if (accumulate) {
-                float old[4];
-                load_floats(p, old);
+    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+    for (int g = wave; g < groups; g += kFewWaves * kFewAhead) {
+        if (g != wave) load(g);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] += old[q];
-            }
-            store_floats(p, v);
-        } else {
-            for (int q = 0; q < 4; ++q)
-                if (j + q < b.rows) p[q] = rounded<T>(accumulate ? v[q] + static_cast<float>(p[q]) : v[q]);
+        for (int i = 0; i < kFewAhead; ++i) {
+            const int of = g + i * kFewWaves;
+            if (of >= groups) break;
+            const uint32_t xa = *reinterpret_cast<const uint16_t*>(own_scales + of * kMxBlocks);
+            const Words4* ca = reinterpret_cast<const Words4*>(own + of * kMxBytes);
+            acc = mma<0>(cb[i][0], xb[i], ca[0], xa, acc);
+            acc = mma<1>(cb[i][1], xb[i], ca[1], xa, acc);
         }
     }
+    finish_few<T>(sums, acc, out, 0, j0);
 }
 
 // Larger tiles: the operands in shared memory, two groups of k a step, in two stages
@@ -804,16 +884,33 @@ double rounds(int64_t tiles, int64_t grid, double full, double rest) {
 
 // Tiles of 32 x 32 that are better off one a workgroup, whose wavefronts share the sum,
 // while they and their groups are few: 256 x 1024 x 2048 takes 4.7 us for 9.5 in middle
-// tiles, 256 x 4096 x 2048 9.3 for 9.7, 512 x 4096 x 2048 14.9 for 10.2; with short sums
-// 512 x 4096 x 256 6.0 for 6.5, 1024 x 4096 x 256 9.0 for 7.3.
-constexpr int64_t kFewTiles = 4096, kFewGroups = 32768;
+// tiles, 256 x 4096 x 2048 9.3 for 9.7, 256 x 1024 x 8192 12.3 for 14.6, but 512 x 4096 x
+// 2048 14.9 for 10.2 and 256 x 1024 x 16384 21.3 for 18.3; with short sums 512 x 4096 x 256
+// 6.0 for 6.5 and 1024 x 4096 x 256 9.0 for 7.3.  Rows that the workgroups pack
+// themselves save a launch: twice as many groups (1 x 2048 x 50257 13.2 us for 16.6).
+constexpr int64_t kFewTiles = 2048, kFewGroups = 16384, kOwnGroups = 2 * kFewGroups;
+
+int64_t few_tiles(const Mx4Product& c) {
+    return (c.a.rows + kTile - 1) / kTile * ((c.b.rows + kTile - 1) / kTile);
+}
+bool takes_few(const Mx4Product& c, int64_t most_groups = kFewGroups) {
+    const int64_t few = few_tiles(c);
+    return (few <= kFewTiles && few * c.a.groups <= most_groups) || c.a.groups == 0;
+}
+FewOut few_out(const Mx4Product& c) { return {c.out.at, c.out.stride, c.a.rows, c.b.rows, c.accumulate}; }
+
+template <class X>
+hipError_t few_linear(const X* x, int64_t stride, const Mx4Product& c, hipStream_t stream) {
+    const auto kernel = c.out.type == MICRO_TYPE_F32   ? few_linear_kernel<X, float>
+                        : c.out.type == MICRO_TYPE_F16 ? few_linear_kernel<X, f16>
+                                                       : few_linear_kernel<X, bf16>;
+    return launch(kernel, grid_of(few_tiles(c)), 64 * kFewWaves, stream, x, stride, static_cast<int>(c.a.rows), c.b, few_out(c));
+}
 
 template <class T>
 hipError_t product(const Mx4Product& c, hipStream_t stream) {
-    const int64_t few = (c.a.rows + kTile - 1) / kTile * ((c.b.rows + kTile - 1) / kTile);
-    if ((few <= kFewTiles && few * c.a.groups <= kFewGroups) || c.a.groups == 0)
-        return launch(few_kernel<T>, grid_of(few), 64 * kFewWaves, stream, c.a, c.b, static_cast<T*>(c.out.at), c.out.stride,
-                      c.accumulate);
+    if (takes_few(c))
+        return launch(few_kernel<T>, grid_of(few_tiles(c)), 64 * kFewWaves, stream, c.a, c.b, few_out(c));
     const auto count = [&](int64_t a, int64_t b) { return (c.b.rows + a - 1) / a * ((c.a.rows + b - 1) / b); };
     const double middle = rounds(count(Middle::kA, Middle::kB), c.compute_units * kMxPerUnit<Middle>, 1.1, 0.7);
     const double wide = rounds(count(Wide::kA, Wide::kB), c.compute_units * kMxPerUnit<Wide>, 1.77, 1.25);
@@ -821,6 +918,19 @@ hipError_t product(const Mx4Product& c, hipStream_t stream) {
 }
 
 }  // namespace
+
+hipError_t launch_mx4_linear(const Rows& x, const Mx4Product& c, hipStream_t stream) {
+    if (c.a.rows > 0 && c.a.rows <= kTile && c.b.rows > 0 && c.a.groups > 0 && c.a.rows * c.a.groups * kMxGroup <= kOwnValues &&
+        takes_few(c, kOwnGroups)) {
+        switch (x.type) {
+            case MICRO_TYPE_F32: return few_linear(static_cast<const float*>(x.at), x.stride, c, stream);
+            case MICRO_TYPE_F16: return few_linear(static_cast<const f16*>(x.at), x.stride, c, stream);
+            default: return few_linear(static_cast<const bf16*>(x.at), x.stride, c, stream);
+        }
+    }
+    if (const hipError_t e = launch_mx4_pack(x, c.a.rows, c.a.cols, c.a, Mx4{}, stream)) return e;
+    return launch_mx4_product(c, stream);
+}
 
 hipError_t launch_mx4_product(const Mx4Product& c, hipStream_t stream) {
     if (c.a.rows == 0 || c.b.rows == 0) return hipSuccess;

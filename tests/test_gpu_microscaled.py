@@ -143,6 +143,34 @@ def test_product(dtype, m, n, k):
     assert bool((whole[:, :5] == 3).all()) and bool((whole[:, 5 + n:] == 3).all())
 
 
+@pytest.mark.parametrize("x_type", TYPES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 70, 2048), (4, 300, 2041), (5, 33, 1500), (32, 100, 256), (31, 40, 129),
+                                   (33, 40, 100), (1, 40, 8192), (1, 40, 8193), (2, 1, 4096)])
+def test_linear_of_few_rows(x_type, dtype, m, n, k):
+    """Rows that the workgroups pack themselves (up to 32 of 8192 values in whole groups
+    together) and more: as what is packed first."""
+    base = draw(m, k + 6, x_type, m + k).to(DEV)
+    base = base / 2.0 ** 9
+    x = base[:, 3:3 + k]
+    w = draw(n, k, torch.float32, n) / 2.0 ** 9
+    mx = micro.Microscaled()
+    q, qx = mx.pack(w.to(DEV)), mx.pack(x)
+    check_packed(qx, x.cpu())
+    got = mx.linear(x, q, dtype=dtype)
+    want, bound = ref.product(ref.packed_values(x.cpu()), ref.packed_values(w), dtype)
+    assert got.dtype == dtype and language_reference.excess(got, want, bound) <= 1.0
+    assert torch.equal(got, mx.product(qx, q, dtype=dtype))
+    whole = torch.full((m, n + 9), 3.0, dtype=dtype, device=DEV)
+    mx.linear(x, q, out=whole[:, 5:5 + n], accumulate=True)
+    want, bound = ref.product(ref.packed_values(x.cpu()), ref.packed_values(w), dtype, torch.full((m, n), 3.0))
+    assert language_reference.excess(whole[:, 5:5 + n], want, bound) <= 1.0
+    assert bool((whole[:, :5] == 3).all()) and bool((whole[:, 5 + n:] == 3).all())
+    x[0, k // 2] = float("nan")
+    got = mx.linear(x, q, dtype=dtype)
+    assert bool(got[0].isnan().all()) and not bool(got[1:].isnan().any())
+
+
 # (rows, columns, length): middle tiles in one round and in several, wide ones in one and
 # in two, each with an odd number of groups, edges on both sides and a tail cut along the sum
 LARGE_PRODUCTS = [(2000, 2300, 130), (1500, 3001, 300), (2000, 9000, 40), (2050, 9000, 257), (500, 1000, 9000),
