@@ -441,6 +441,9 @@ __device__ __forceinline__ void enlist(Shared<kThreads>& s, uint32_t first, cons
         }
 }
 
+// Bound by vector arithmetic, 25 instructions for each weight: 2048 rows of 50257 bfloat16
+// logits in 129 us, with top_p 0.95 261, with top_k 50 96 and with T = 0, two readings
+// alone, 68 (6.1 TB/s); one binary32 row in 22, 41, 17 and 7 us.
 template <class T, int kThreads>
 __global__ __launch_bounds__(kThreads, 4) void sample_kernel(SampleCall call, int bits) {
     constexpr int kList = kThreads, kListK = kThreads / 2, kVec = Row<T, kThreads>::kVec;
@@ -699,7 +702,7 @@ hipError_t launch_rows(const SampleCall& call, hipStream_t stream) {
     const dim3 grid(static_cast<uint32_t>(call.rows));
     // Rows for every compute unit: two workgroups each, one at work while the other waits
     // (2048 rows of 50257 bfloat16 logits, top_p 0.95, in 302 us for 418), unless a top_k
-    // for all needs the larger workgroup's list.
+    // for all needs the larger workgroup's list (top_k 500 in 251 us for 369).
     const bool longer = !call.sampling.top_ks && call.sampling.top_k > 256 && call.sampling.top_k <= 512;
     if (call.rows > call.compute_units && !longer) return launch(sample_kernel<T, 512>, grid, 512, stream, call, bits);
     return launch(sample_kernel<T, 1024>, grid, 1024, stream, call, bits);
