@@ -282,7 +282,12 @@ bool setting(PyObject* from, int device, int64_t rows, at::ScalarType type, Numb
         *array = t.data_ptr();
         return true;
     }
-    if constexpr (std::is_same<Number, double>::value) return real(from, number);
+    if constexpr (std::is_same<Number, double>::value) {
+        if (!PyLong_CheckExact(from)) return real(from, number);
+        *number = PyLong_AsDouble(from);
+        PyErr_Clear();  // (too large for one: -1, which is refused)
+        return true;
+    }
     if (!PyLong_CheckExact(from)) return false;
     int overflow = 0;
     *number = PyLong_AsLongLongAndOverflow(from, &overflow);
