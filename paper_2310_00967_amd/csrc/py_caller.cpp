@@ -285,8 +285,9 @@ bool setting(PyObject* from, int device, int64_t rows, at::ScalarType type, Numb
     if constexpr (std::is_same<Number, double>::value) {
         if (!PyLong_CheckExact(from)) return real(from, number);
         *number = PyLong_AsDouble(from);
-        PyErr_Clear();  // (too large for one: -1, which is refused)
-        return true;
+        if (!PyErr_Occurred()) return true;
+        PyErr_Clear();  // too large for one
+        return false;
     }
     if (!PyLong_CheckExact(from)) return false;
     int overflow = 0;

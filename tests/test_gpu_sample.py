@@ -209,6 +209,22 @@ def test_another_stream_and_a_captured_graph():
         assert torch.equal(ids, want[0]) and torch.equal(logprobs, want[1])
 
 
+@pytest.mark.parametrize("settings", [{"temperature": 1, "top_p": 1, "min_p": 0}, {"temperature": 0}, {"min_p": 1},
+                                      {"temperature": 2, "top_k": 64}])
+def test_whole_numbers(settings):
+    vocab = 1000
+    table = micro.TokenTable(vocab, 1, 4)
+    logits, uniforms = rows_of(4, vocab, torch.float32, 3)
+    ids, logprobs = check(table, logits, uniforms, **settings)
+    same = table.sample(logits.to(DEV), uniforms.to(DEV), **{k: v if k == "top_k" else float(v) for k, v in settings.items()})
+    assert torch.equal(ids, same[0]) and torch.equal(logprobs, same[1])
+    for wrong, error in [({"temperature": -1}, micro.MicroError), ({"top_p": 0}, micro.MicroError),
+                         ({"top_p": 2}, micro.MicroError), ({"min_p": -1}, micro.MicroError),
+                         ({"temperature": 10 ** 400}, (OverflowError, TypeError))]:
+        with pytest.raises(error):
+            table.sample(logits.to(DEV), uniforms.to(DEV), **wrong)
+
+
 def test_refusals():
     vocab = 100
     logits, uniforms = rows_of(4, vocab, torch.float32, 1)
