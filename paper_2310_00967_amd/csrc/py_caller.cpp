@@ -236,6 +236,9 @@ struct TableCaller {
     int64_t stream;  // c10's id of the handle's stream
 };
 
+// Neither requires its gradient nor carries a tangent.
+bool outside_autograd(const at::Tensor& t) { return !t.requires_grad() && !t._fw_grad(/*level=*/0).defined(); }
+
 // lookup(weight, ids, scale): the rows; None: not the plain case; an int: the
 // call's status.
 PyObject* table_lookup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -248,7 +251,7 @@ PyObject* table_lookup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor& ids = THPVariable_Unpack(args[1]);
     const auto plain = [&](const at::Tensor& t) {
         return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == c->device && t.is_contiguous() &&
-               !t.requires_grad() && !t._fw_grad(/*level=*/0).defined();
+               outside_autograd(t);
     };
     const bool wide = ids.scalar_type() == at::kLong;
     if (!plain(weight) || !plain(ids) || weight.scalar_type() != c->type || weight.dim() != 2 ||
@@ -277,7 +280,8 @@ template <class Number>
 bool setting(PyObject* from, int device, int64_t rows, at::ScalarType type, Number* number, const void** array) {
     if (THPVariable_CheckExact(from)) {
         const at::Tensor& t = THPVariable_Unpack(from);
-        if (!t.is_cuda() || t.get_device() != device || !t.is_contiguous() || t.scalar_type() != type || t.numel() != rows)
+        if (!t.is_cuda() || t.get_device() != device || !t.is_contiguous() || t.scalar_type() != type || t.numel() != rows ||
+            !outside_autograd(t))
             return false;
         *array = t.data_ptr();
         return true;
@@ -304,15 +308,15 @@ PyObject* table_sample(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     const at::Tensor& logits = THPVariable_Unpack(args[0]);
     const at::Tensor& uniforms = THPVariable_Unpack(args[1]);
     const auto plain = [&](const at::Tensor& t) {
-        return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == c->device && t.is_contiguous();
+        return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == c->device && t.is_contiguous() &&
+               outside_autograd(t);
     };
     const int64_t rows = uniforms.numel();
     const auto kind = logits.scalar_type();
     const int32_t type = kind == at::kFloat ? MICRO_TYPE_F32 : kind == at::kHalf ? MICRO_TYPE_F16
                          : kind == at::kBFloat16 ? MICRO_TYPE_BF16 : -1;
     if (!plain(logits) || !plain(uniforms) || type < 0 || uniforms.scalar_type() != at::kFloat || logits.dim() < 1 ||
-        logits.size(-1) != c->vocab || logits.numel() != rows * c->vocab || logits.requires_grad() ||
-        logits._fw_grad(/*level=*/0).defined())
+        logits.size(-1) != c->vocab || logits.numel() != rows * c->vocab)
         Py_RETURN_NONE;
     micro_sampling s{};
     const void *temperatures = nullptr, *top_ks = nullptr, *top_ps = nullptr, *min_ps = nullptr;
@@ -395,8 +399,7 @@ int32_t type_of(at::ScalarType t) {
 
 bool plain_values(const at::Tensor& t, int device) {
     return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == device && t.is_contiguous() && t.dim() >= 1 &&
-           t.size(-1) > 0 && t.numel() > 0 && !t.requires_grad() && !t._fw_grad(/*level=*/0).defined() &&
-           type_of(t.scalar_type()) >= 0;
+           t.size(-1) > 0 && t.numel() > 0 && outside_autograd(t) && type_of(t.scalar_type()) >= 0;
 }
 
 bool on_stream(int device, int64_t stream) {

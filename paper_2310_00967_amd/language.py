@@ -356,6 +356,7 @@ class TokenTable(_Enqueued):
             return None
         if value.dtype != dtype or not value.is_cuda or value.get_device() != self._index or not value.is_contiguous():
             raise TypeError(f"{name} must be a number or a contiguous {dtype} tensor on {self.device}")
+        self._outside_autograd(value, name)
         if value.numel() != rows:
             raise ValueError(f"{name} must hold {rows} values")
         setattr(sampling, name + "s", value.data_ptr())
@@ -386,6 +387,7 @@ class TokenTable(_Enqueued):
         if not isinstance(uniforms, self._tensor) or uniforms.dtype is not torch.float32 or not uniforms.is_cuda \
                 or uniforms.get_device() != self._index or not uniforms.is_contiguous():
             raise TypeError(f"uniforms must be a contiguous float32 tensor on {self.device}")
+        self._outside_autograd(uniforms, "uniforms")
         rows = uniforms.numel()
         if not isinstance(logits, self._tensor) or logits.dtype not in self._value_types or not logits.is_cuda \
                 or logits.get_device() != self._index:
