@@ -352,6 +352,9 @@ class TokenTable(_Enqueued):
         """Enters one of sample's settings: a number, or a tensor of one a row,
         which is returned."""
         if not isinstance(value, self._tensor):
+            # (ctypes takes a whole number modulo 2^64)
+            if isinstance(value, int) and dtype == self._torch.int32 and not -2 ** 63 <= value < 2 ** 63:
+                raise OverflowError(f"{name} does not fit 64 bits")
             setattr(sampling, name, value)
             return None
         if value.dtype != dtype or not value.is_cuda or value.get_device() != self._index or not value.is_contiguous():

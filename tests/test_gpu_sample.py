@@ -252,3 +252,23 @@ def test_refusals():
         table.sample(logits, uniforms, out=logits.view(-1)[:8].view(torch.int64))
     torch.cuda.synchronize()
     assert bool((out == 7).all())
+
+
+@pytest.mark.parametrize("given", [False, True], ids=["", "out"])  # the native way, and the other
+def test_a_top_k_past_64_bits(given):
+    """The number is refused, not taken without its upper bits; what 64 bits hold is
+    taken as it is."""
+    vocab = 50
+    table = micro.TokenTable(vocab, 1, 4)
+    logits, uniforms = rows_of(4, vocab, torch.float32, 13)
+    logits, uniforms = logits.to(DEV), uniforms.to(DEV)
+    out = torch.full((4,), 7, dtype=torch.int64, device=DEV) if given else None
+    for top_k in (2 ** 63, 2 ** 64, 2 ** 64 + 1, 2 ** 64 + 5, -2 ** 63 - 1, -2 ** 64 + 1, 10 ** 400):
+        with pytest.raises(OverflowError, match="top_k"):
+            table.sample(logits, uniforms, top_k=top_k, out=out)
+    torch.cuda.synchronize()
+    assert out is None or bool((out == 7).all())
+    want = table.sample(logits, uniforms)
+    for top_k in (2 ** 63 - 1, 2 ** 32 + 1, vocab, 0, -1, -2 ** 63):
+        got = table.sample(logits, uniforms, top_k=top_k, out=out)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

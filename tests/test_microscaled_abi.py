@@ -8,7 +8,7 @@ import subprocess
 import pytest
 import torch
 
-from paper_2310_00967_amd import PackedMatrix, _lib
+from paper_2310_00967_amd import PackedMatrix, TokenTable, _lib
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 EINVAL, ERANGE = _lib.MICRO_EINVAL, _lib.MICRO_ERANGE
@@ -112,3 +112,20 @@ def test_packed_matrices_of_other_shapes_and_types_are_refused():
             PackedMatrix(codes, scales, 3, 300)
     with pytest.raises(ValueError):
         PackedMatrix(m.codes, m.scales, -3, 300)
+
+
+def test_a_whole_number_past_64_bits_is_refused_as_a_setting():
+    """A ctypes structure takes one modulo 2^64."""
+    table = TokenTable.__new__(TokenTable)  # a setting that is a number looks at no handle
+    table._torch, table._tensor = torch, torch.Tensor
+    s = _lib.micro_sampling()
+    for top_k in (2 ** 63, 2 ** 64, 2 ** 64 + 5, -2 ** 63 - 1, 10 ** 400):
+        with pytest.raises(OverflowError, match="top_k"):
+            table._setting(s, "top_k", top_k, torch.int32, 4)
+        assert s.top_k == 0
+    for top_k in (2 ** 63 - 1, -2 ** 63, 5):
+        assert table._setting(s, "top_k", top_k, torch.int32, 4) is None and s.top_k == top_k
+    with pytest.raises(OverflowError):
+        table._setting(s, "temperature", 10 ** 400, torch.float32, 4)
+    table._setting(s, "temperature", 2 ** 64, torch.float32, 4)
+    assert s.temperature == 2.0 ** 64
