@@ -17,45 +17,62 @@ class PackedMatrix:
 
     codes: uint8, (groups, rows, 64), two values a byte; scales: uint8, (groups, rows,
     4), the exponents of 2 plus 127; groups = cols / 128, rounded up.  Values behind
-    cols are 0.  Both are contiguous and may be saved and loaded as they are."""
+    cols are 0.  Both are contiguous and may be saved and loaded as they are.  A
+    matrix keeps the tensors that it was made of: others make another matrix."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "_parts")
+    __slots__ = ("_parts",)  # (codes, scales, rows, cols), which every call goes by
 
     def __init__(self, codes, scales, rows, cols):
         import torch
-        self.rows, self.cols = int(rows), int(cols)
-        if self.rows < 0 or self.cols < 0:
+        rows, cols = int(rows), int(cols)
+        if rows < 0 or cols < 0:
             raise ValueError("a side is negative")
-        groups = -(-self.cols // GROUP)
-        for t, name, shape in ((codes, "codes", (groups, self.rows, GROUP // 2)),
-                               (scales, "scales", (groups, self.rows, BLOCKS))):
+        groups = -(-cols // GROUP)
+        for t, name, shape in ((codes, "codes", (groups, rows, GROUP // 2)),
+                               (scales, "scales", (groups, rows, BLOCKS))):
             if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous():
                 raise TypeError(f"{name} must be a contiguous uint8 tensor")
             if tuple(t.shape) != shape:
-                raise ValueError(f"{name} of a {self.rows} x {self.cols} matrix must have the shape {shape}")
+                raise ValueError(f"{name} of a {rows} x {cols} matrix must have the shape {shape}")
         if codes.device != scales.device:
             raise TypeError("codes and scales must be on one device")
-        self.codes, self.scales = codes, scales
-        self._parts = (codes, scales, self.rows, self.cols)
+        self._parts = (codes, scales, rows, cols)
 
     @classmethod
     def _made(cls, parts):
         """Of a call's own outputs."""
         m = cls.__new__(cls)
-        m.codes, m.scales, m.rows, m.cols = m._parts = parts
+        m._parts = parts
         return m
 
     @property
+    def codes(self):
+        return self._parts[0]
+
+    @property
+    def scales(self):
+        return self._parts[1]
+
+    @property
+    def rows(self):
+        return self._parts[2]
+
+    @property
+    def cols(self):
+        return self._parts[3]
+
+    @property
     def _c(self):
-        return _lib.micro_mx4_matrix(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
+        codes, scales, rows, cols = self._parts
+        return _lib.micro_mx4_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols)
 
     @property
     def device(self):
-        return self.codes.device
+        return self._parts[0].device
 
     @property
     def shape(self):
-        return self.rows, self.cols
+        return self._parts[2:]
 
     def __repr__(self):
         return f"PackedMatrix({self.rows} x {self.cols}, {self.device})"

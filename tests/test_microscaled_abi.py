@@ -1,8 +1,10 @@
 """The 4-bit matrices' and the token draw's entry points without a device:
 refusals before any HIP call, sizes, and the binding's structures against the
 header."""
+import copy
 import ctypes
 import os
+import pickle
 import subprocess
 
 import pytest
@@ -129,3 +131,27 @@ def test_a_whole_number_past_64_bits_is_refused_as_a_setting():
         table._setting(s, "temperature", 10 ** 400, torch.float32, 4)
     table._setting(s, "temperature", 2 ** 64, torch.float32, 4)
     assert s.temperature == 2.0 ** 64
+
+
+def packed_on_the_cpu(rows=3, cols=300):
+    groups = -(-cols // 128)
+    gen = torch.Generator().manual_seed(rows)
+    return PackedMatrix(torch.randint(256, (groups, rows, 64), generator=gen, dtype=torch.uint8),
+                        torch.randint(255, (groups, rows, 4), generator=gen, dtype=torch.uint8), rows, cols)
+
+
+def test_a_packed_matrix_is_one_state():
+    """What the calls marshalled natively take and what the others do is the same,
+    and stays so: its parts are not assigned."""
+    m, other = packed_on_the_cpu(), packed_on_the_cpu(4, 300)
+    for name in ("codes", "scales", "rows", "cols", "shape", "device"):
+        with pytest.raises(AttributeError):
+            setattr(m, name, getattr(other, name))
+    assert m.shape == (m.rows, m.cols) == (3, 300)
+    for same in (m, copy.copy(m), copy.deepcopy(m), pickle.loads(pickle.dumps(m))):
+        codes, scales, rows, cols = same._parts
+        assert codes is same.codes and scales is same.scales and (rows, cols) == (same.rows, same.cols)
+        c = same._c
+        assert (c.codes, c.scales, c.rows, c.cols) == (codes.data_ptr(), scales.data_ptr(), 3, 300)
+        assert torch.equal(codes, m.codes) and torch.equal(scales, m.scales)
+    assert copy.deepcopy(m).codes.data_ptr() != m.codes.data_ptr()
