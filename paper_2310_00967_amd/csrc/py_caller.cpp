@@ -418,14 +418,21 @@ struct PackedTensors {
     }
 };
 
-// The matrix of a (codes, scales, rows, cols) tuple.
+// The matrix of a (codes, scales, rows, cols) tuple, whose tensors may have been resized,
+// or been given other memory, since they were checked.
 bool matrix_of(PyObject* t, int device, micro_mx4_matrix* m) {
     if (!PyTuple_CheckExact(t) || PyTuple_GET_SIZE(t) != 4) return false;
     PyObject *codes = PyTuple_GET_ITEM(t, 0), *scales = PyTuple_GET_ITEM(t, 1);
     if (!THPVariable_CheckExact(codes) || !THPVariable_CheckExact(scales)) return false;
     const at::Tensor &c = THPVariable_Unpack(codes), &s = THPVariable_Unpack(scales);
-    if (!c.is_cuda() || c.get_device() != device) return false;
-    *m = {c.data_ptr(), s.data_ptr(), PyLong_AsLongLong(PyTuple_GET_ITEM(t, 2)), PyLong_AsLongLong(PyTuple_GET_ITEM(t, 3))};
+    const int64_t rows = PyLong_AsLongLong(PyTuple_GET_ITEM(t, 2)), cols = PyLong_AsLongLong(PyTuple_GET_ITEM(t, 3));
+    const auto holds = [&](const at::Tensor& x, int64_t bytes) {
+        return x.layout() == at::kStrided && x.is_cuda() && x.get_device() == device && x.scalar_type() == at::kByte &&
+               x.is_contiguous() && x.dim() == 3 && x.size(0) == (cols + kGroup - 1) / kGroup && x.size(1) == rows &&
+               x.size(2) == bytes;
+    };
+    if (!holds(c, kGroupBytes) || !holds(s, kGroupBlocks)) return false;
+    *m = {c.data_ptr(), s.data_ptr(), rows, cols};
     return true;
 }
 

@@ -23,10 +23,16 @@ class PackedMatrix:
     __slots__ = ("_parts",)  # (codes, scales, rows, cols), which every call goes by
 
     def __init__(self, codes, scales, rows, cols):
-        import torch
         rows, cols = int(rows), int(cols)
         if rows < 0 or cols < 0:
             raise ValueError("a side is negative")
+        self._check(codes, scales, rows, cols)
+        self._parts = (codes, scales, rows, cols)
+
+    @staticmethod
+    def _check(codes, scales, rows, cols):
+        """(Again at every call: a tensor can be resized, or given other memory.)"""
+        import torch
         groups = -(-cols // GROUP)
         for t, name, shape in ((codes, "codes", (groups, rows, GROUP // 2)),
                                (scales, "scales", (groups, rows, BLOCKS))):
@@ -36,7 +42,6 @@ class PackedMatrix:
                 raise ValueError(f"{name} of a {rows} x {cols} matrix must have the shape {shape}")
         if codes.device != scales.device:
             raise TypeError("codes and scales must be on one device")
-        self._parts = (codes, scales, rows, cols)
 
     @classmethod
     def _made(cls, parts):
@@ -64,6 +69,7 @@ class PackedMatrix:
     @property
     def _c(self):
         codes, scales, rows, cols = self._parts
+        self._check(*self._parts)
         return _lib.micro_mx4_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols)
 
     @property

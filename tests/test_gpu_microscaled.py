@@ -8,6 +8,7 @@ import paper_2310_00967_amd as micro
 
 import language_reference
 import microscaled_reference as ref
+from test_microscaled_abi import changes_in_place
 
 pytestmark = pytest.mark.gpu
 
@@ -368,3 +369,33 @@ def test_refusals():
     mx.close()
     with pytest.raises(RuntimeError, match="closed"):
         mx.pack(x)
+
+
+@pytest.mark.parametrize("change,error", changes_in_place())
+def test_matrices_whose_tensors_were_changed_in_place_are_refused(change, error):
+    """On the native way and on the other, before anything is read."""
+    mx = micro.Microscaled()
+    x = torch.ones(40, 300, device=DEV)
+    whole = mx.pack(x)
+    out = torch.full((40, 40), 7.0, device=DEV)
+    values = torch.full((40, 300), 7.0, device=DEV)
+    for call in (lambda m: mx.product(m, whole), lambda m: mx.product(whole, m), lambda m: mx.linear(x, m), lambda m: mx.unpack(m),
+                 lambda m: mx.product(m, whole, out=out), lambda m: mx.product(whole, m, out=out, accumulate=True),
+                 lambda m: mx.linear(x, m, out=out), lambda m: mx.unpack(m, out=values)):
+        m = mx.pack(x)
+        change(m)
+        with pytest.raises(error):
+            call(m)
+    for part in ("codes", "scales"):  # memory of the host
+        m = mx.pack(x)
+        getattr(m, part).data = getattr(m, part).cpu()
+        for call in (lambda: mx.product(m, whole), lambda: mx.unpack(m), lambda: mx.linear(x, m, out=out)):
+            with pytest.raises(TypeError):
+                call()
+    torch.cuda.synchronize()
+    assert bool((out == 7).all()) and bool((values == 7).all())
+    # other memory of the same shape is read from then on
+    m = mx.pack(x)
+    m.codes.data = mx.pack(x * 1.5).codes.clone()
+    assert torch.equal(mx.unpack(m), x * 1.5) and torch.equal(mx.unpack(m, out=values), x * 1.5)
+    assert torch.equal(mx.product(m, whole), torch.full((40, 40), 450.0, device=DEV))

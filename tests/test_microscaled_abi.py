@@ -155,3 +155,23 @@ def test_a_packed_matrix_is_one_state():
         assert (c.codes, c.scales, c.rows, c.cols) == (codes.data_ptr(), scales.data_ptr(), 3, 300)
         assert torch.equal(codes, m.codes) and torch.equal(scales, m.scales)
     assert copy.deepcopy(m).codes.data_ptr() != m.codes.data_ptr()
+
+
+def changes_in_place():
+    """What may happen to a matrix's tensors behind its back, and the error of a call
+    that would read them."""
+    return [(lambda m: m.codes.resize_(0), ValueError), (lambda m: m.scales.resize_(1, 1, 4), ValueError),
+            (lambda m: m.codes.unsqueeze_(0), ValueError), (lambda m: m.codes.transpose_(0, 1), (TypeError, ValueError)),
+            (lambda m: m.scales.set_(torch.zeros(2, dtype=torch.uint8, device=m.device)), ValueError),
+            (lambda m: setattr(m.codes, "data", m.codes[:, :1].contiguous()), ValueError),
+            (lambda m: setattr(m.codes, "data", m.codes.float()), TypeError)]
+
+
+@pytest.mark.parametrize("change,error", changes_in_place())
+def test_a_matrix_whose_tensors_were_changed_in_place_is_refused(change, error):
+    m = packed_on_the_cpu()
+    assert m._c.codes == m.codes.data_ptr()
+    change(m)
+    with pytest.raises(error):
+        m._c  # noqa: B018
+
