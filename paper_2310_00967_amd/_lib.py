@@ -143,7 +143,7 @@ def load():
 
 
 def load_caller(name="Caller"):
-    """A type of the native marshalling: Caller or TableCaller (never builds it)."""
+    """A type of the native marshalling: Caller, TableCaller or MxCaller (never builds it)."""
     import torch  # noqa: F401  (its libraries before the module that links to them)
     try:
         from . import _caller

@@ -90,7 +90,7 @@ __device__ __forceinline__ Pack<T, N> load_some(const T* p, int64_t valid) {
 // Rows: a workgroup takes kPackRows rows of kPackGroups groups, sixteen lanes a row's
 // group, eight values a lane, so that neighbouring lanes read one row and the
 // workgroup's stores fill whole lines of a group's rows.  Bound by memory: 50257 x 2048
-// bfloat16 values in 41 us, 6.3 TB/s.
+// bfloat16 values in 49 to 57 us, 4.6 to 5.4 TB/s.
 constexpr int kPackThreads = 256, kPackRows = 8, kPackGroups = 8, kPackLanes = kMxGroup / 8;
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* x, int64_t stride, Mx4 to) {
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const T* x, int64_t 
 // of neighbouring columns are written as whole lines; those of the rows change places in
 // shared memory, to leave as runs of kMxGroup rows of a group.
 // Four columns a thread: with eight, of 16-bit types, the values take 256 registers and
-// 16384 x 8192 takes 180 us.
+// 16384 x 8192 takes 180 us for 69 (rows alone 65, both ways 90 to 108).
 constexpr int kTurnVec = 4, kTurnColumns = 64 / kMxBlocks * kTurnVec * (kPackThreads / 64);
 static_assert(kTurnColumns == 2 * kMxGroup, "two groups of rows' values");
 template <class T, bool kRows>
@@ -221,7 +221,8 @@ __global__ __launch_bounds__(kPackThreads) void pack_turned_kernel(const T* x, i
 
 // The way back: sixteen lanes a row's group as above, each 16 bytes of out at a time, a row
 // after the other, so that workgroups in their order write memory in its order: 50257 x
-// 2048 bfloat16 values in 56 us (4.7 TB/s), by workgroups of 8 rows and 8 groups in 68.
+// 2048 bfloat16 values in 55 to 58 us (4.5 to 4.7 TB/s; 73 where each call writes other
+// memory), by workgroups of 8 rows and 8 groups in 68.
 template <class T>
 __global__ __launch_bounds__(kPackThreads) void unpack_kernel(Mx4 from, T* out, int64_t stride) {
     constexpr int kVec = 16 / sizeof(T), kPieces = 8 / kVec, kLines = kPackThreads / kPackLanes;
@@ -289,7 +290,8 @@ struct Side {
 // A tile of 32 x 32 a workgroup, whose four wavefronts take every fourth group, two at a
 // time, and add their sums in shared memory.  Bound by one read of b: 1 x 2048 x 50257 in
 // 13.8 us (4.0 TB/s of 55 MB from memory), 32 rows in 18.2; one group at a time 14.6 and
-// 21.5, four 14.0 and 17.6 but 7.5 for 6.2 at 1 x 1024 x 30522.
+// 21.5, four 14.0 and 17.6 but 7.5 for 6.2 at 1 x 1024 x 30522.  (Sizes of products are
+// rows x length of the sums x columns, here and below.)
 constexpr int kTile = 32, kFewWaves = 4, kFewAhead = 2, kPadded = kTile + 4;
 struct FewOut {
     void* at;
@@ -732,10 +734,12 @@ template <class S>
 constexpr int kMxPerUnit = 160 * 1024 / (kMxStages * kMxStep * (S::kA + S::kB) * (kMxBytes + kMxBlocks));
 
 // Bound by the matrix cores, which are busy 57 to 67% of the cycles of a long sum, at a
-// clock that sinks to 1.8 GHz under them: 8192 x 8192 x 8192 in 240 us (4.6 PFLOP/s), 16384
-// x 2048 x 8192 in 124 to 127 (middle tiles 157), 16384 x 8192 x 2048 in 152 (195), where a
-// tile's eight steps take 13 us and its stores 6.  One group a step through four stages,
-// with twice the barriers: 127, 163 and, in middle tiles, 190 for 157.
+// clock that sinks to 1.8 GHz under them: 8192 x 8192 x 8192 in 236 to 240 us (4.6 to 4.7
+// PFLOP/s), 16384 x 8192 x 2048 in 123 to 128 (middle tiles 149 to 157), 16384 x 2048 x
+// 8192, busy 44%, in 152 to 160 (191 to 195): a tile's eight steps take 13 us and its stores
+// 6.  One group a step through four stages, with twice the barriers: 16384 x 8192 x 2048 in
+// 127 where two groups took 124 (in middle tiles 190 for 157), 16384 x 2048 x 8192 in 163
+// for 152.
 template <class S, class T>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Mx4 a, Mx4 b, MxOut out) {
     using Tiles = MxTiles<S>;
@@ -868,8 +872,8 @@ hipError_t tiles(const Mx4Product& c, hipStream_t stream) {
     MxOut out{c.out.at, c.out.stride, c.a.rows, c.b.rows, c.accumulate, c.parts, 1};
     // The tiles behind the last full round are cut along the sum where they are a quarter
     // of the grid at most and a part keeps kPartGroups: writing and adding the parts costs
-    // more than it saves else (1024 x 1024 x 16384 in 23.6 us for 41.5, but 1024 x 4096 x
-    // 8192 in 34.2 for 26.7).
+    // more than it saves else (1024 x 16384 x 1024 in 23.6 us for 41.5, but 1024 x 8192 x
+    // 4096 in 34.2 for 26.7).
     const int64_t tail = ta * tb % grid;
     if (tail > 0 && tail * 4 <= grid) out.most_splits = std::min(grid / tail, std::max<int64_t>(c.a.groups / kPartGroups, 1));
     if (const hipError_t e = launch(product_kernel<S, T>, dim3(static_cast<uint32_t>(grid)), S::kThreads, stream, c.b, c.a, out))
@@ -880,19 +884,34 @@ hipError_t tiles(const Mx4Product& c, hipStream_t stream) {
 }
 
 // How long `tiles` tiles take: rounds of a full grid, and the less that the last one
-// takes when it is not full, in microseconds for each step of long sums (16384 x 4096 x
-// 16384: 8 rounds of middle tiles in 571 us, 4 of wide ones in 452; one round that is
-// not full 0.6 to 0.7 and 1.2).
+// takes when it is not full, in microseconds for each step of long sums (16384 x 16384 x
+// 4096: 8 rounds of middle tiles in 565 us, 4 of wide ones in 459; one round that is not
+// full 0.6 to 0.7 and 1.2).  Where the stores weigh as much as the sums the same side is
+// the faster one at what was measured: 4096 x 2048 x 50257 in wide tiles 313 us, in middle
+// ones 338, 16384 x 2048 x 8192 153 and 191, 1000 x 1024 x 4096 12.6 and 8.8, 1024 x 256 x
+// 4096 9.3 and 7.2.
 double rounds(int64_t tiles, int64_t grid, double full, double rest) {
     return tiles / grid * full + (tiles % grid ? rest : 0.0);
 }
 
 // Tiles of 32 x 32 that are better off one a workgroup, whose wavefronts share the sum,
-// while they and their groups are few: 256 x 1024 x 2048 takes 4.7 us for 9.5 in middle
-// tiles, 256 x 4096 x 2048 9.3 for 9.7, 256 x 1024 x 8192 12.3 for 14.6, but 512 x 4096 x
-// 2048 14.9 for 10.2 and 256 x 1024 x 16384 21.3 for 18.3; with short sums 512 x 4096 x 256
-// 6.0 for 6.5 and 1024 x 4096 x 256 9.0 for 7.3.  Rows that the workgroups pack
-// themselves save a launch: twice as many groups (1 x 2048 x 50257 13.2 us for 16.6).
+// while they and their groups are few: 256 x 2048 x 1024 takes 4.6 us for 9.4 in middle
+// tiles, 256 x 8192 x 1024 9.7 for 16.5, 256 x 2048 x 4096 9.7 both, 512 x 2048 x 4096 14.7
+// for 10.2, 1024 x 256 x 4096 10.8 for 7.2.  The border is not that of every shape: 256 x
+// 16384 x 1024, behind it, takes 18.3 in middle tiles and would take 15.1.
+//   Rows that the workgroups pack themselves save a launch: twice as many groups.  Calls
+// from x, of tables that come from memory, in us by rows of their own / by a packing launch
+// and middle tiles:
+//   1 x 2048 x 30522    7.8 / 14.1      1 x 4096 x 50257   23.3 / 28.3
+//   1 x 2048 x 50257   13.3 / 18.4      1 x 2048 x 131072  31.9 / 34.2
+//   1 x 2048 x 65536   16.6 / 19.0      1 x 1024 x 262144  32.2 / 39.0
+//   4 x 2048 x 65536   19.5 / 19.7      1 x 4096 x 131072  60.7 / 57.3 (5.0 TB/s)
+// and of up to 32 rows that a launch packs, in tiles of 32 x 32 / middle ones:
+//   19 x 2048 x 30522  12.8 / 15.0      19 x 4096 x 50257  30.8 / 27.5
+//   19 x 2048 x 50257  19.3 / 19.2      19 x 2048 x 131072 40.5 / 35.1
+//   32 x 2048 x 50257  21.2 / 19.7      19 x 4096 x 131072 75.5 / 60.5
+// Behind the limits (the right column; 19 and 32 x 2048 x 50257) middle tiles are what
+// runs: one to four rows lose up to a fifth by it, more rows gain.
 constexpr int64_t kFewTiles = 2048, kFewGroups = 16384, kOwnGroups = 2 * kFewGroups;
 
 int64_t few_tiles(const Mx4Product& c) {

@@ -1,6 +1,7 @@
 // Marshalling of the Python binding's calls on a context (Caller.step, .ef_step
-// and .sweep) and on a token table (TableCaller.lookup): they check the tensors, call the C
-// ABI of include/micro_sparsify.h and wrap the results.  They take the plain case
+// and .sweep), on a token table (TableCaller.lookup and .sample) and on 4-bit matrices
+// (MxCaller): they check the tensors, call the C ABI of include/micro_sparsify.h and wrap
+// the results.  They take the plain case
 // only (exact torch.Tensor buffers, Python floats and ints, every check
 // passed) and return None otherwise, with nothing called: the Python methods
 // then go their own way, which names what is wrong.  A nonzero status comes
@@ -221,10 +222,9 @@ PyObject* caller_new(PyTypeObject* type, PyObject* args, PyObject*) {
     return reinterpret_cast<PyObject*>(c);
 }
 
-// TableCaller: the lookup of a token table's rows, whose kernel takes 2 us, in
-// the plain case: a contiguous table and ids, called on the handle's stream,
-// with an output of its own.  (In Python the same checks, the allocation and the
-// call took 9 us.)
+// TableCaller: the lookup of a token table's rows, whose kernel takes 2 us, and the draw of
+// tokens in the plain case: contiguous tensors, called on the handle's stream, with outputs
+// of their own.  (In Python the lookup's checks, the allocation and the call took 9 us.)
 struct TableCaller {
     PyObject_HEAD
     decltype(&micro_table_lookup) lookup;

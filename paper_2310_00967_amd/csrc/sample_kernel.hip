@@ -479,8 +479,10 @@ __device__ __forceinline__ void enlist(Shared<kThreads>& s, uint32_t first, cons
 }
 
 // Bound by vector arithmetic, 25 instructions for each weight: 2048 rows of 50257 bfloat16
-// logits in 129 us, with top_p 0.95 261, with top_k 50 85 and with T = 0, two readings
-// alone, 68 (6.1 TB/s); one binary32 row in 22, 40, 14 and 7 us.
+// logits in 138 to 148 us, with top_p 0.95 269, with top_k 50 98 and with T = 0, two
+// readings alone, 79 (5.2 TB/s); one binary32 row in 21, 41, 13.4 and 7 us.  (Logits from
+// memory; of one batch drawn from again and again, which the last cache holds in part,
+// 129, 261, 85 and 68.)
 template <class T, int kThreads>
 __global__ __launch_bounds__(kThreads, 4) void sample_kernel(SampleCall call, int bits) {
     constexpr int kList = kThreads, kListK = kThreads / 2, kVec = Row<T, kThreads>::kVec;
@@ -738,8 +740,9 @@ hipError_t launch_rows(const SampleCall& call, hipStream_t stream) {
     const int bits = weight_bits(call.vocab);
     const dim3 grid(static_cast<uint32_t>(call.rows));
     // Rows for every compute unit: two workgroups each, one at work while the other waits
-    // (2048 rows of 50257 bfloat16 logits, top_p 0.95, in 302 us for 418), unless a top_k
-    // for all needs the larger workgroup's list (top_k 500 in 251 us for 369).
+    // (2048 rows of 50257 bfloat16 logits, top_p 0.95, in 269 us for 379; 300 rows in 76
+    // for 92), unless a top_k for all needs the larger workgroup's list (top_k 500 in 264
+    // us for 380; one a row, which the host does not see, takes the 380).
     const bool longer = !call.sampling.top_ks && call.sampling.top_k > 256 && call.sampling.top_k <= 512;
     if (call.rows > call.compute_units && !longer) return launch(sample_kernel<T, 512>, grid, 512, stream, call, bits);
     return launch(sample_kernel<T, 1024>, grid, 1024, stream, call, bits);
