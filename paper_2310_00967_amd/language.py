@@ -12,6 +12,7 @@ caller's record_stream.
 """
 import ctypes
 import math
+import operator
 
 from . import _lib
 
@@ -352,9 +353,10 @@ class TokenTable(_Enqueued):
         """Enters one of sample's settings: a number, or a tensor of one a row,
         which is returned."""
         if not isinstance(value, self._tensor):
-            # (ctypes takes a whole number modulo 2^64)
-            if isinstance(value, int) and dtype == self._torch.int32 and not -2 ** 63 <= value < 2 ** 63:
-                raise OverflowError(f"{name} does not fit 64 bits")
+            if dtype == self._torch.int32:
+                value = operator.index(value)
+                if not -2 ** 63 <= value < 2 ** 63:  # (ctypes takes one modulo 2^64)
+                    raise OverflowError(f"{name} does not fit 64 bits")
             setattr(sampling, name, value)
             return None
         if value.dtype != dtype or not value.is_cuda or value.get_device() != self._index or not value.is_contiguous():

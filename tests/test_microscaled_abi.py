@@ -3,10 +3,12 @@ refusals before any HIP call, sizes, and the binding's structures against the
 header."""
 import copy
 import ctypes
+import operator
 import os
 import pickle
 import subprocess
 
+import numpy as np
 import pytest
 import torch
 
@@ -116,17 +118,32 @@ def test_packed_matrices_of_other_shapes_and_types_are_refused():
         PackedMatrix(m.codes, m.scales, -3, 300)
 
 
+class Whole:
+    """A whole number that is no int."""
+
+    def __init__(self, value):
+        self.value = value
+
+    def __index__(self):
+        return self.value
+
+
 def test_a_whole_number_past_64_bits_is_refused_as_a_setting():
     """A ctypes structure takes one modulo 2^64."""
     table = TokenTable.__new__(TokenTable)  # a setting that is a number looks at no handle
     table._torch, table._tensor = torch, torch.Tensor
     s = _lib.micro_sampling()
-    for top_k in (2 ** 63, 2 ** 64, 2 ** 64 + 5, -2 ** 63 - 1, 10 ** 400):
+    for top_k in (2 ** 63, 2 ** 64, 2 ** 64 + 5, -2 ** 63 - 1, 10 ** 400, Whole(2 ** 64 + 5), np.uint64(2 ** 64 - 1)):
         with pytest.raises(OverflowError, match="top_k"):
             table._setting(s, "top_k", top_k, torch.int32, 4)
         assert s.top_k == 0
     for top_k in (2 ** 63 - 1, -2 ** 63, 5):
         assert table._setting(s, "top_k", top_k, torch.int32, 4) is None and s.top_k == top_k
+    for whole in (Whole(5), True, np.int64(5), np.uint8(5)):
+        assert table._setting(s, "top_k", whole, torch.int32, 4) is None and s.top_k == int(operator.index(whole))
+    for wrong in (2.5, "5", None, 5.0):
+        with pytest.raises(TypeError):
+            table._setting(s, "top_k", wrong, torch.int32, 4)
     with pytest.raises(OverflowError):
         table._setting(s, "temperature", 10 ** 400, torch.float32, 4)
     table._setting(s, "temperature", 2 ** 64, torch.float32, 4)
