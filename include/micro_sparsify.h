@@ -406,15 +406,17 @@ MICRO_API void micro_sparsify_free(micro_ctx *ctx);
 /* ------------------------------------------------------------------------
  * Around the step on a language model: the global norm and clipping of a
  * model's gradients into the flat vector that the step reads, the lookup of
- * token rows with its gradient, and the softmax cross entropy over the token
- * table with its gradients.
+ * token rows with its gradient, the softmax cross entropy over the token table
+ * with its gradients, the draw of tokens from logits, and matrices in 4 bits.
  *
  * Every call below is enqueued on its handle's stream and returns after the
  * launches; device inputs must be ready on that stream and stay allocated
  * until it has run.  Messages of a refusal come from micro_last_error(NULL) on
  * the calling thread; a refusal (MICRO_EINVAL, MICRO_ECAPACITY, MICRO_ERANGE)
  * comes before any device work, with nothing modified.  One handle must not be
- * used from two threads at once.  Results are the same on every run.
+ * used from two threads at once.  Calls share their handle's scratch, those that a
+ * graph has captured too: they must not run at once, and the handle must be freed
+ * after the graph's last replay.  Results are the same on every run.
  * ------------------------------------------------------------------------ */
 
 /* Types of the tensors' values. */

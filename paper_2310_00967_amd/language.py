@@ -8,7 +8,9 @@ be ready on that stream.  Outputs that a call allocates belong to that stream.
 Where another stream is current during a call, its tensors are kept from reuse
 until the handle's stream is done with them; where the handle's own is current,
 as with torch's operators, a tensor that another stream allocated needs the
-caller's record_stream.
+caller's record_stream.  Calls share their handle's scratch, those that a graph has
+captured too: they must not run at once, and the handle must live until the graph's
+last replay.
 """
 import ctypes
 import math
